@@ -1,8 +1,8 @@
-"""The signature as a differentiable torch operation: sig_compute forward, sig_backward backward.
+"""The signature, and the sequence-model operators behind it, as differentiable torch operations.
 
-Marshalling only: both directions run in libsig's kernels (include/sig.h), and the autograd node is native
-(csrc/sig_torch.cpp), so that the engine's thread never waits for the interpreter.  This is what lets the layer sit
-between trainable layers as in the paper's model (Section 4.2, Eq. 11).
+Marshalling only: both directions run in libsig's kernels (include/sig.h, include/sig_sequence.h), and the autograd nodes are
+native (csrc/sig_torch.cpp, csrc/sig_torch_sequence.cpp), so that the engine's thread never waits for the interpreter.  This is
+what lets the layer sit between trainable layers as in the paper's model (Section 4.2, Eq. 11).
 """
 import torch
 
@@ -37,6 +37,49 @@ def signature(path, depth, stream=False):
     if torch.jit.is_tracing():
         return _Traced.apply(path, depth, stream)
     return (binding._torch_lib or binding.torch_lib()).autograd_signature(path, depth, stream)
+
+
+class _TracedCall(torch.autograd.Function):
+    """A native differentiable call while torch.jit.trace is recording (see _Traced): `call` takes the tensors."""
+
+    @staticmethod
+    def forward(ctx, call, *tensors):
+        ctx.inputs = [t.detach().requires_grad_(t.requires_grad) if torch.is_tensor(t) else t for t in tensors]
+        with torch.enable_grad():
+            ctx.outputs = call(*ctx.inputs)
+        one = torch.is_tensor(ctx.outputs)
+        return ctx.outputs.detach() if one else tuple(t.detach() for t in ctx.outputs)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        outputs = (ctx.outputs,) if torch.is_tensor(ctx.outputs) else ctx.outputs
+        wanted = [t for t in ctx.inputs if torch.is_tensor(t) and t.requires_grad]
+        got = iter(torch.autograd.grad(outputs, wanted, grads))
+        return (None,) + tuple(next(got) if torch.is_tensor(t) and t.requires_grad else None for t in ctx.inputs)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """binding.layer_norm with a gradient with respect to `x`, `weight` and `bias`."""
+    call = (binding._torch_lib or binding.torch_lib()).autograd_layer_norm
+    if torch.jit.is_tracing():
+        return _TracedCall.apply(lambda x, weight, bias: call(x, weight, bias, eps), x, weight, bias)
+    return call(x, weight, bias, eps)
+
+
+def rotary(x, positions, frequencies, interleaved=False, scale=1.0):
+    """binding.rotary with a gradient with respect to `x`."""
+    call = (binding._torch_lib or binding.torch_lib()).autograd_rotary
+    if torch.jit.is_tracing():
+        return _TracedCall.apply(lambda x, p, f: call(x, p, f, interleaved, scale), x, positions, frequencies)
+    return call(x, positions, frequencies, interleaved, scale)
+
+
+def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, return_state=False):
+    """binding.linear_attention with a gradient with respect to `q`, `k`, `v` and `state` (log_decay is a constant of the model)."""
+    call = (binding._torch_lib or binding.torch_lib()).autograd_linear_attention
+    if torch.jit.is_tracing():
+        return _TracedCall.apply(lambda *t: call(*t, scale, return_state), q, k, v, log_decay, state, lengths)
+    return call(q, k, v, log_decay, state, lengths, scale, return_state)
 
 
 def capture(step_fn, warmup=3):

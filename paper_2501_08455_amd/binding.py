@@ -1,4 +1,4 @@
-"""Python binding of libsig.so: the same entry points as include/sig.h, argument marshalling only.
+"""Python binding of libsig.so: the same entry points as include/sig.h and include/sig_sequence.h, argument marshalling only.
 
 torch is used for device memory and streams; every arithmetic step runs in the
 HIP kernels behind the C ABI.  There is no CPU fallback: if the library is not
@@ -20,6 +20,8 @@ SIG_ERR_NO_DEVICE = 5
 
 SIG_ERR_UNSUPPORTED = 6
 SIG_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
+SIG_F32, SIG_BF16, SIG_F16 = 0, 1, 2
+SIG_POSITION_I32, SIG_POSITION_I64, SIG_POSITION_F32, SIG_POSITION_F64 = 0, 1, 2, 3
 SIG_VARIANT_AUTO = 0
 SIG_VARIANT_HBM_STREAMING = 1
 SIG_VARIANT_ON_CHIP = 2
@@ -37,6 +39,13 @@ class sig_plan_t(ctypes.Structure):
     def as_dict(self):
         skip = ("independent_waves", "stagger_ticks", "tile_loader", "shared_chain")
         return {k: int(getattr(self, k)) for k, _ in self._fields_ if k not in skip}
+
+
+class sig_attention_t(ctypes.Structure):
+    """Shape of a sig_linear_attention call (include/sig_sequence.h)."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("heads", ctypes.c_int32), ("shared_heads", ctypes.c_int32),
+                ("key_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
 
 
 class SigError(RuntimeError):
@@ -96,6 +105,17 @@ def load():
     lib.sig_backward_available.argtypes = [i32, i32]
     lib.sig_backward_segments.restype = i32
     lib.sig_backward_segments.argtypes = [ctypes.c_void_p, i64, i64, i32, i32, i32]
+    f64, ppi = ctypes.c_double, ctypes.POINTER(i64)
+    lib.sig_layer_norm.restype = i32
+    lib.sig_layer_norm.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, f64, vp, vp, vp]
+    lib.sig_layer_norm_backward.restype = i32
+    lib.sig_layer_norm_backward.argtypes = [vp, vp, i64, i64, i64, i32, vp, i32, vp, vp, i64, vp, vp, vp, vp]
+    lib.sig_rotary.restype = i32
+    lib.sig_rotary.argtypes = [vp, vp, ppi, vp, ppi, i32, i64, i64, i64, i64, i64, vp, i32, ppi, vp, i32, f64, i32, vp]
+    lib.sig_linear_attention.restype = i32
+    lib.sig_linear_attention.argtypes = [vp, ctypes.POINTER(sig_attention_t)] + [vp] * 9
+    lib.sig_linear_attention_backward.restype = i32
+    lib.sig_linear_attention_backward.argtypes = [vp, ctypes.POINTER(sig_attention_t)] + [vp] * 13
     lib.sig_probe_copy.restype = i32
     lib.sig_probe_copy.argtypes = [vp, vp, i64, vp]
     lib.sig_probe_write.restype = i32
@@ -330,3 +350,34 @@ def signature(path, depth, stream=False, plan=None, ctx=None, out=None):
     if rc != SIG_OK:
         raise SigError(rc, "sig_compute")
     return out
+
+
+# ---------------------------------------------------------------- sequence-model operators (include/sig_sequence.h), without a gradient
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last axis of `x` (float32, bfloat16 or float16, any strides): (x - mean) / sqrt(variance + eps) * weight
+    + bias.  `weight` and `bias` are vectors of float32 or of x's type, or None.  Returns a new tensor of x's type."""
+    return (_torch_lib or torch_lib()).layer_norm(x, weight, bias, eps)
+
+
+def rotary(x, positions, frequencies, interleaved=False, scale=1.0, out=None):
+    """Rotary positions of `x` [batch, length, heads, components]: the first 2 * len(frequencies) components of each head, as pairs
+    (i, i + len(frequencies)), or neighbours with `interleaved`, are turned by position * frequency and multiplied by `scale`; the
+    others are copied.  `positions` is [length] or [batch, length] (int32, int64, or float32, float64 for times), `frequencies`
+    float64 (see sequence.rotary_frequencies).  `out` may be `x`."""
+    return (_torch_lib or torch_lib()).rotary(x, positions, frequencies, interleaved, scale, out)
+
+
+def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, return_state=False):
+    """Linear attention with a decay for each head, S_t = exp(log_decay) S_{t-1} + k_t (x) v_t, o_t = scale q_t S_t.
+
+    `q` [B, T, H, K], `k` [B, T, G, K], `v` [B, T, G, V] of one type (float32, bfloat16, float16), H a multiple of G (heads share
+    keys and values), K and V up to 256; `log_decay` float32 [H]; `state` float32 [B, H, K, V] in front of the first token (None:
+    zeros); `lengths` [B]: tokens from there on give zeros and leave the state alone; `scale` None: K ** -0.5.  Returns o
+    [B, T, H, V], or (o, state behind the last token) with `return_state`."""
+    return (_torch_lib or torch_lib()).linear_attention(q, k, v, log_decay, state, lengths, scale, return_state)
+
+
+def linear_attention_step(q, k, v, log_decay, state, scale=None, out_state=None):
+    """linear_attention of one token: `q` [B, H, K], `k` [B, G, K], `v` [B, G, V].  Updates `state` in place, or writes the new one to
+    `out_state`.  Returns o [B, H, V]."""
+    return (_torch_lib or torch_lib()).linear_attention_step(q, k, v, log_decay, state, scale, out_state)

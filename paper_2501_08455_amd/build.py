@@ -22,7 +22,10 @@ RESOURCES = os.path.join(OBJ, "kernel_resources.json")
 SOURCES = ["sig_api.hip", "sig_streaming.hip", "sig_combine.hip", "sig_onchip_table.hip", "sig_onchip_table_depth2.hip",
            "sig_onchip_table_depth3.hip", "sig_onchip_table_depth4.hip", "sig_onchip_table_depth56.hip", "sig_onchip_table_odd.hip", "sig_onchip_table_wide.hip",
            "sig_stream_rows.hip", "sig_split_rows.hip", "sig_depth2_rows.hip",
+           "sig_layer_norm.hip", "sig_rotary.hip", "sig_attention.hip", "sig_attention_recurrent.hip",
            "sig_backward.hip", "sig_backward_segments.hip", "sig_backward_general.hip", "sig_bracket.hip", "sig_stream_gradient.hip", "sig_levelscan.hip", "sig_levelscan_rows.hip", "sig_probe.hip"]
+
+TORCH_SOURCES = ["sig_torch.cpp", "sig_torch_sequence.cpp"]
 
 # packed FP32 instructions are switched off for every device translation unit
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -58,26 +61,26 @@ def _compile(src):
     return obj, kernels
 
 
-def _compile_torch():
-    """Host code only (no kernels): the extension module that marshals torch tensors into the C ABI."""
+def _compile_torch(src):
+    """Host code only (no kernels): a file of the extension module that marshals torch tensors into the C ABI."""
     import torch
     from torch.utils import cpp_extension
-    obj = os.path.join(OBJ, "sig_torch.o")
+    obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I" + os.path.join(ROOT, "include"),
            "-I" + sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include"]
     for path in cpp_extension.include_paths():
         cmd += ["-isystem", path]
-    res = subprocess.run(cmd + ["-c", os.path.join(CSRC, "sig_torch.cpp"), "-o", obj], capture_output=True, text=True)
+    res = subprocess.run(cmd + ["-c", os.path.join(CSRC, src), "-o", obj], capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("g++ failed for sig_torch.cpp:\n%s\n%s" % (res.stdout, res.stderr))
+        raise RuntimeError("g++ failed for %s:\n%s\n%s" % (src, res.stdout, res.stderr))
     return obj
 
 
-def _link_torch(obj):
+def _link_torch(objs):
     from torch.utils import cpp_extension
     # torch's libraries are in the process before this module is imported; libsig.so lies beside it
-    cmd = ["g++", "-shared", "-o", TORCH_LIB, obj, LIB, "-Wl,-rpath,$ORIGIN"]
+    cmd = ["g++", "-shared", "-o", TORCH_LIB] + objs + [LIB, "-Wl,-rpath,$ORIGIN"]
     cmd += ["-L" + path for path in cpp_extension.library_paths()]
     cmd += ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10"]
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -88,9 +91,9 @@ def _link_torch(obj):
 def build(verbose=False):
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as pool:
-        torch_obj = pool.submit(_compile_torch)
+        torch_objs = [pool.submit(_compile_torch, src) for src in TORCH_SOURCES]
         done = list(pool.map(_compile, SOURCES))
-        torch_obj = torch_obj.result()
+        torch_objs = [obj.result() for obj in torch_objs]
     objs = [obj for obj, _ in done]
     # registers, LDS and private memory of every kernel, for the host test that no kernel spills
     with open(RESOURCES, "w") as f:
@@ -99,7 +102,7 @@ def build(verbose=False):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (res.stdout, res.stderr))
-    _link_torch(torch_obj)
+    _link_torch(torch_objs)
     if verbose:
         print("built", LIB)
         print("built", TORCH_LIB)
