@@ -61,6 +61,16 @@ AttentionArgs pass(const sig_attention_t &s, const float *log_decay, const int64
     return A;
 }
 
+// Up to this many tokens go one after the other: a chunk's products cost as much for one token as for all of it
+constexpr int kRecurrentTokens = 16;
+
+int64_t scratch_floats(const AttentionArgs &A, int type, int cus) { return A.T > kRecurrentTokens ? attention_chunk_scratch_floats(A, type, cus) : 0; }
+
+hipError_t launch(const AttentionArgs &A, int type, int out_type, float *scratch, int cus, hipStream_t st)
+{
+    return A.T > kRecurrentTokens ? launch_attention_chunk(A, type, out_type, scratch, cus, st) : launch_attention_recurrent(A, type, out_type, st);
+}
+
 // the state of `A`, kept [key][value] where its rows are keys, else read as the transpose
 void from_state(AttentionArgs &A, const float *state, float *state_out, bool transposed)
 {
@@ -91,7 +101,14 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     contiguous(A.os, s, s.heads, s.value_dim);
     A.out_scale = s.scale;
     from_state(A, state, state_out, false);
-    return launch_attention_recurrent(A, s.type, s.type, (hipStream_t)hip_stream) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    Scratch scratch;
+    float *work = nullptr;
+    if (const int64_t floats = scratch_floats(A, s.type, ctx->num_cu)) {
+        const int got = scratch.get(ctx, (size_t)floats * sizeof(float), st, &work);
+        if (got != SIG_OK) return got;
+    }
+    return launch(A, s.type, s.type, work, ctx->num_cu, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
@@ -108,58 +125,60 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     int64_t gs[3];
     contiguous(gs, s, s.heads, V);
 
+    // the three passes; shared keys' and values' gradients go to scratch, heads apart, and are added up from there
+    AttentionArgs Q = pass(s, log_decay, lengths, V, K), K_ = Q, V_ = pass(s, log_decay, lengths, K, V);
+    operand(&Q.x, Q.xs, &Q.x_group, grad_out, gs, 1);
+    operand(&Q.y, Q.ys, &Q.y_group, v, s.v_strides, group);
+    operand(&Q.z, Q.zs, &Q.z_group, k, s.k_strides, group);
+    Q.out_scale = s.scale;
+    from_state(Q, state, nullptr, true);
+    operand(&K_.x, K_.xs, &K_.x_group, v, s.v_strides, group);
+    operand(&K_.y, K_.ys, &K_.y_group, grad_out, gs, 1);
+    operand(&K_.z, K_.zs, &K_.z_group, q, s.q_strides, 1);
+    K_.update_scale = s.scale;
+    K_.reversed = 1;
+    from_state(K_, grad_state, nullptr, true);
+    operand(&V_.x, V_.xs, &V_.x_group, k, s.k_strides, group);
+    operand(&V_.y, V_.ys, &V_.y_group, q, s.q_strides, 1);
+    operand(&V_.z, V_.zs, &V_.z_group, grad_out, gs, 1);
+    V_.update_scale = s.scale;
+    V_.reversed = 1;
+    from_state(V_, grad_state, grad_initial, false);
+
+    const int cus = ctx->num_cu;
+    int64_t states = 0;
+    for (const AttentionArgs *A : {&Q, &K_, &V_}) {
+        const int64_t floats = scratch_floats(*A, s.type, cus);
+        if (floats > states) states = floats;
+    }
+    const int64_t parts = group > 1 ? s.B * s.T * s.heads * (K > V ? K : V) : 0;
     Scratch scratch;
-    float *part = nullptr;
-    if (group > 1 && s.T > 0) {
-        rc = scratch.get(ctx, (size_t)(s.B * s.T * s.heads) * (K > V ? K : V) * sizeof(float), st, &part);
+    float *work = nullptr;
+    if (states + parts > 0) {
+        rc = scratch.get(ctx, (size_t)(states + parts) * sizeof(float), st, &work);
         if (rc != SIG_OK) return rc;
     }
-    // the gradient of shared keys or values: heads apart in scratch, then their sum
+    float *part = group > 1 ? work + states : nullptr;
     auto shared_pass = [&](AttentionArgs &A, void *grad, int dim) {
         A.o = part ? (void *)part : grad;
         contiguous(A.os, s, s.heads, dim);
-        hipError_t e = launch_attention_recurrent(A, s.type, part ? (int)SIG_F32 : s.type, st);
-        if (e != hipSuccess || !part) return e;
+        hipError_t e = launch(A, s.type, part ? (int)SIG_F32 : s.type, work, cus, st);
         const int64_t values = s.B * s.T * s.shared_heads * dim, blocks = (values + kThreads - 1) / kThreads;
+        if (e != hipSuccess || !part || values == 0) return e;
         with_type(s.type, [&](auto t) {
             using E = typename decltype(t)::type;
             sig_attention_share_kernel<E><<<(unsigned)(blocks < 65536 ? blocks : 65536), kThreads, 0, st>>>(part, (E *)grad, values, group, dim);
         });
         return hipGetLastError();
     };
-
     hipError_t e = hipSuccess;
     if (s.T > 0) {
-        AttentionArgs A = pass(s, log_decay, lengths, V, K);
-        operand(&A.x, A.xs, &A.x_group, grad_out, gs, 1);
-        operand(&A.y, A.ys, &A.y_group, v, s.v_strides, group);
-        operand(&A.z, A.zs, &A.z_group, k, s.k_strides, group);
-        A.out_scale = s.scale;
-        from_state(A, state, nullptr, true);
-        A.o = grad_q;
-        contiguous(A.os, s, s.heads, K);
-        e = launch_attention_recurrent(A, s.type, s.type, st);
+        Q.o = grad_q;
+        contiguous(Q.os, s, s.heads, K);
+        e = launch(Q, s.type, s.type, work, cus, st);
+        if (e == hipSuccess) e = shared_pass(K_, grad_k, K);
     }
-    if (e == hipSuccess && s.T > 0) {
-        AttentionArgs A = pass(s, log_decay, lengths, V, K);
-        operand(&A.x, A.xs, &A.x_group, v, s.v_strides, group);
-        operand(&A.y, A.ys, &A.y_group, grad_out, gs, 1);
-        operand(&A.z, A.zs, &A.z_group, q, s.q_strides, 1);
-        A.update_scale = s.scale;
-        A.reversed = 1;
-        from_state(A, grad_state, nullptr, true);
-        e = shared_pass(A, grad_k, K);
-    }
-    if (e == hipSuccess) {
-        AttentionArgs A = pass(s, log_decay, lengths, K, V);
-        operand(&A.x, A.xs, &A.x_group, k, s.k_strides, group);
-        operand(&A.y, A.ys, &A.y_group, q, s.q_strides, 1);
-        operand(&A.z, A.zs, &A.z_group, grad_out, gs, 1);
-        A.update_scale = s.scale;
-        A.reversed = 1;
-        from_state(A, grad_state, grad_initial, false);
-        e = shared_pass(A, grad_v, V);
-    }
+    if (e == hipSuccess) e = shared_pass(V_, grad_v, V);
     return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 

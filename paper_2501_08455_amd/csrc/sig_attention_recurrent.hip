@@ -23,7 +23,8 @@ __global__ __launch_bounds__(kThreads) void sig_attention_recurrent_kernel(Atten
     const T *z = (const T *)A.z + b * A.zs[0] + head / A.z_group * A.zs[2];
     O *o = (O *)A.o + b * A.os[0] + head * A.os[2];
     const int64_t state_at = ((int64_t)b * A.heads + head) * A.rows * A.columns;
-    const float decay = expf(A.log_decay[head]);
+    // l = 1 + shrink: the decay itself, rounded, would drift over many tokens where little decays
+    const float shrink = expm1f(A.log_decay[head]);
     const int64_t length = attention_length(A, b);
     const bool in = c < A.columns;    // (with N > 1 the columns are a multiple of N)
 
@@ -56,13 +57,14 @@ __global__ __launch_bounds__(kThreads) void sig_attention_recurrent_kernel(Atten
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int row = group + i * GROUPS;
-            const float xr = row < A.rows ? to_float(x[t * A.xs[1] + row]) : 0.0f;
-            const float yr = row < A.rows ? to_float(y[t * A.ys[1] + row]) : 0.0f;
+            if (row >= A.rows) continue;      // (not 0 x what may be infinite)
+            const float xr = to_float(x[t * A.xs[1] + row]), yr = to_float(y[t * A.ys[1] + row]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                s[i][j] = A.reversed ? fmaf(yr, zs[j], s[i][j]) : fmaf(decay, s[i][j], yr * zs[j]);
+                if (!A.reversed) s[i][j] = fmaf(s[i][j], shrink, s[i][j]);
+                s[i][j] = fmaf(yr, zs[j], s[i][j]);
                 part[j] = fmaf(xr, s[i][j], part[j]);
-                if (A.reversed) s[i][j] *= decay;
+                if (A.reversed) s[i][j] = fmaf(s[i][j], shrink, s[i][j]);
             }
         }
 #pragma unroll

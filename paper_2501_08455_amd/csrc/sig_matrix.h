@@ -1,0 +1,112 @@
+// Matrix products of 16 x 16 tiles on gfx950, for operands kept in bfloat16 or in float32.
+//
+// A fragment is one wavefront's share of a 16 x STEP operand: lane l holds line l % 16 (a row of the left operand, a column of the
+// right one; both have the same layout) at SUB groups of four neighbouring places of the summed axis,
+// 16 sub + 4 (l / 16) + 0..3.  The order along the summed axis is free as long as both operands agree, and this one is that of
+// a result: a product's tile holds, in lane l, column l % 16 at rows 4 (l / 16) + 0..3.  So SUB result tiles are a fragment as they
+// lie (lines = columns, summed axis = rows), without a detour through LDS.
+#ifndef SIG_MATRIX_H
+#define SIG_MATRIX_H
+
+#include "sig_types.h"
+
+namespace sig {
+
+using f4 = __attribute__((ext_vector_type(4))) float;
+using b4 = __attribute__((ext_vector_type(4))) bf16;
+using b8 = __attribute__((ext_vector_type(8))) bf16;
+using s4 = __attribute__((ext_vector_type(4))) short;
+
+template <typename E>
+struct Matrix;
+
+template <>
+struct Matrix<float> {
+    using Frag = f4;
+    static constexpr int STEP = 16, SUB = 1;
+    static constexpr int PAD = 4;        // values behind a row in LDS that keep 16 rows in different banks
+    static constexpr int EXACT = 1;      // fragments that hold a float32 number whole
+
+    // lines = rows of `m` (pitch in values) from `line` on, summed axis = its columns from `at` on
+    static __device__ Frag along_rows(const float *m, int pitch, int line, int at)
+    {
+        const int lane = threadIdx.x % kWaveLanes;
+        return *(const f4 *)(m + (line + lane % 16) * pitch + at + 4 * (lane / 16));
+    }
+    // lines = columns column(0 .. 15) of `m`, summed axis = its rows from `at` on
+    template <typename F>
+    static __device__ Frag along_columns(const float *m, int pitch, int at, F column)
+    {
+        const int lane = threadIdx.x % kWaveLanes;
+        const float *p = m + (at + 4 * (lane / 16)) * pitch + column(lane % 16);
+        return f4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
+    }
+    // left x right on top of `sum`
+    static __device__ f4 multiply(Frag left, Frag right, f4 sum)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(left[i], right[i], sum, 0, 0, 0);
+        return sum;
+    }
+    // value e of a fragment
+    static __device__ float value(Frag f, int e) { return f[e]; }
+    // the numbers x[0 .. 3] as PARTS fragments that add up to them
+    template <int PARTS>
+    static __device__ void split(const float *x, Frag *parts)
+    {
+        parts[0] = f4{x[0], x[1], x[2], x[3]};
+    }
+
+private:
+    static constexpr int kWaveLanes = 64;
+};
+
+template <>
+struct Matrix<bf16> {
+    using Frag = b8;
+    static constexpr int STEP = 32, SUB = 2;
+    static constexpr int PAD = 8;
+    static constexpr int EXACT = 3;      // 3 x 8 digits
+
+    static __device__ Frag along_rows(const bf16 *m, int pitch, int line, int at)
+    {
+        const int lane = threadIdx.x % kWaveLanes;
+        const bf16 *p = m + (line + lane % 16) * pitch + at + 4 * (lane / 16);
+        return __builtin_shufflevector(*(const b4 *)p, *(const b4 *)(p + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // The transposing LDS read: 16 lanes name 16 groups of four values, group i of row i / 4; lane i receives value i % 4 of the groups
+    // i / 4 of the four rows.  column(0), column(4), column(8), column(12) each begin four neighbouring columns.
+    template <typename F>
+    static __device__ Frag along_columns(const bf16 *m, int pitch, int at, F column)
+    {
+        const int lane = threadIdx.x % kWaveLanes, i = lane % 16;
+        const bf16 *p = m + (at + 4 * (lane / 16) + i / 4) * pitch + column(4 * (i % 4));
+        using Read = __attribute__((address_space(3))) s4;
+        const s4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)p);
+        const s4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + 16 * pitch));
+        return __builtin_shufflevector(__builtin_bit_cast(b4, low), __builtin_bit_cast(b4, high), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static __device__ f4 multiply(Frag left, Frag right, f4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(left, right, sum, 0, 0, 0); }
+    static __device__ float value(Frag f, int e) { return (float)f[e]; }
+    // x[0 .. 7]; each part holds the next eight digits of what the parts before it leave
+    template <int PARTS>
+    static __device__ void split(const float *x, Frag *parts)
+    {
+        float rest[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = x[e];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                parts[p][e] = (bf16)rest[e];
+                if (p + 1 < PARTS) rest[e] -= (float)parts[p][e];
+            }
+    }
+
+private:
+    static constexpr int kWaveLanes = 64;
+};
+
+}  // namespace sig
+#endif
