@@ -6,11 +6,10 @@
 //   S  <- l^n S + update_scale sum_j l^(n-1-j+e) y_j (x) z_j
 // All powers are of one head's decay and not above 1 where it decays, so nothing has to be scaled back.
 //
-// A workgroup of four wavefronts holds 64 NV columns of one head's state in registers, 16 NV a wavefront, as the tiles of a
-// matrix product: they are the left operand of x S as they lie.  x, y and z of a chunk are staged in LDS, the next chunk's loads
-// stay in flight in registers meanwhile.  Each wavefront works out the whole triangle x_i . y_j by itself: its tiles, too, are an
-// operand as they lie, and a second barrier a chunk would cost more than the products.  Output tiles are taken as their
-// transpose, in which a lane holds neighbouring columns of one token.
+// A workgroup holds VT columns of one head's state in registers, 16 a wavefront, as the tiles of a matrix product: they are the left
+// operand of x S as they lie.  x, y and z of a chunk are staged in LDS, the next chunk's loads stay in flight in registers
+// meanwhile.  The tiles of the triangle are shared out over the wavefronts and passed on through LDS, as the fragments that
+// everyone reads.  Output tiles are taken as their transpose, in which a lane holds neighbouring columns of one token.
 //
 // A product of matrices multiplies every pair: 0 x infinity where the triangle is empty, and the parts of an infinite number.  A chunk
 // whose output is not finite is therefore worked out again token by token, so that what is not a number reaches what it
@@ -25,8 +24,6 @@
 
 namespace sig {
 
-constexpr int kChunkThreads = 256;
-
 // The pieces along time that different workgroups take (A.T tokens from place `segment * segment_tokens` on)
 struct ChunkArgs {
     AttentionArgs a;
@@ -35,122 +32,139 @@ struct ChunkArgs {
     float *states;              // [segments][B][heads][rows][columns]: state-only launches write a segment's own, others read what lies before it
 };
 
-// A tile of C tokens x W values: global memory -> registers -> LDS (E), zeros where there is nothing.  The loads are
-// unconditional (what is not there is read from the first token instead, and dropped on the way to LDS), so that all are in flight at once.
-template <typename T, typename E, int C, int W>
+// Tiles of C tokens x W values, one after the other: global memory -> registers -> LDS (E), zeros where there is nothing.  A thread
+// takes the same group of values of every ROWS-th token.  Its loads are unconditional (what is not there is read from a value
+// that is, and dropped on the way to LDS), so that all are in flight at once.
+template <typename T, typename E, int C, int W, int THREADS>
 struct TileLoader {
     static constexpr int GROUP = 16 / (sizeof(T) > sizeof(E) ? sizeof(T) : sizeof(E));      // values of a load
-    static constexpr int ROW = W / GROUP, COUNT = C * ROW / kChunkThreads;
-    static_assert(C * ROW % kChunkThreads == 0);
+    static constexpr int WIDE = W <= 64 ? 64 : W <= 128 ? 128 : 256;                        // (threads beyond W load and drop)
+    static constexpr int ROWS = THREADS / (WIDE / GROUP), COUNT = C / ROWS;
+    static_assert(THREADS % (WIDE / GROUP) == 0 && C % ROWS == 0);
+    const T *p;          // of the next tile
+    int64_t stride;      // between tokens
+    int width;           // values of a token
+    bool there;
     Pack<T, GROUP> held[COUNT];
 
-    static __device__ bool there(int i, int n, int width, int *r, int *c)
+    static __device__ int row() { return threadIdx.x / (WIDE / GROUP); }
+    static __device__ int place() { return threadIdx.x % (WIDE / GROUP) * GROUP; }
+
+    // token 0 of the first tile is at `tokens`
+    __device__ TileLoader(const T *tokens, int64_t stride_, int width_) : stride(stride_), width(width_)
     {
-        const int at = threadIdx.x + i * kChunkThreads;
-        *r = at / ROW;
-        *c = at % ROW * GROUP;
-        return *r < n && *c + GROUP <= width;
+        there = place() + GROUP <= width;
+        p = tokens + row() * stride + (there ? place() : 0);
     }
-    // token r of the tile is at p + r * stride; 1 <= n of them are there, `width` values each
-    __device__ void load(const T *p, int64_t stride, int n, int width)
+    // the next tile, of which 1 <= n <= C tokens are there
+    __device__ void load(int n)
     {
-        if (width < GROUP) return;
+        if (width >= GROUP) {
+            if (n == C) {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            int r, c;
-            const bool ok = there(i, n, width, &r, &c);
-            held[i] = *(const Pack<T, GROUP> *)(p + (ok ? r * stride + c : 0));
-        }
-    }
-    __device__ void store(E *tile, int pitch, const T *p, int64_t stride, int n, int width) const
-    {
+                for (int i = 0; i < COUNT; ++i) held[i] = *(const Pack<T, GROUP> *)(p + i * ROWS * stride);
+            } else {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            int r, c;
-            const bool ok = there(i, n, width, &r, &c);
-            struct alignas(GROUP * sizeof(E)) { E v[GROUP]; } row;
-#pragma unroll
-            for (int j = 0; j < GROUP; ++j) row.v[j] = ok ? (E)held[i].v[j] : (E)0.0f;
-            *(decltype(row) *)(tile + r * pitch + c) = row;
-        }
-        // the last values of rows that are no whole number of groups (after the zeros of the same thread)
-        if (width < W && width % GROUP)
-#pragma unroll 1
-            for (int i = 0; i < COUNT; ++i) {
-                const int at = threadIdx.x + i * kChunkThreads, r = at / ROW, c = at % ROW * GROUP;
-                if (r < n && c < width && c + GROUP > width)
-#pragma unroll 1
-                    for (int j = c; j < width; ++j) tile[r * pitch + j] = (E)p[r * stride + j];
+                for (int i = 0; i < COUNT; ++i) {
+                    const int r = row() + i * ROWS;
+                    held[i] = *(const Pack<T, GROUP> *)(p + ((r < n ? r : n - 1) - row()) * stride);
+                }
             }
+        }
+        p += C * stride;
+    }
+    // the tile of the last load(n)
+    __device__ void store(E *tile, int pitch, int n) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int r = row() + i * ROWS;
+            const bool ok = there && r < n;
+            struct alignas(GROUP * sizeof(E)) { E v[GROUP]; } values;
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) values.v[j] = ok ? (E)held[i].v[j] : (E)0.0f;
+            if (W == WIDE || place() < W) *(decltype(values) *)(tile + r * pitch + place()) = values;
+        }
+        // the last values of tokens that are no whole number of groups (after the zeros of the same thread, which then reads from place 0)
+        const int rest = width % GROUP, c = place();
+        if (width < W && rest && c < width && c + GROUP > width) {
+            const T *from = p - C * stride + c;
+#pragma unroll 1
+            for (int r = row(); r < n; r += ROWS, from += ROWS * stride)
+#pragma unroll 1
+                for (int j = 0; j < rest; ++j) tile[r * pitch + c + j] = (E)from[j];
+        }
     }
 };
 
-// Column of the state that line r of tile `tile` of a wavefront's NV tiles stands for: two tiles of 16-bit outputs alternate in groups of
-// four, so that a lane's values of both are eight neighbours (a 16-byte store)
-template <typename O, int NV>
-__device__ inline int chunk_column(int tile, int r)
-{
-    return sizeof(O) == 2 && NV == 2 ? r / 4 * 8 + tile * 4 + r % 4 : tile * 16 + r;
-}
-
-// One token after the other, for the chunk in LDS (see above).  store(r, nv, o_r at the column of line `line`)
-template <bool OUTPUT, int KT, int NV, typename E, typename Column, typename Store>
+// One token after the other, for the chunk in LDS (see above).  store(r, o_r at the lane's column)
+template <bool OUTPUT, int KT, typename E, typename Store>
 __device__ inline void chunk_by_token(const AttentionArgs &A, float g, int n, const E *xs, const E *ys, int kpitch, const E *zs, int vpitch,
-                                            f4 (&s)[KT][NV], Column column, Store store)
+                                      f4 (&s)[KT], int column, Store store)
 {
     const int quad = threadIdx.x % 64 / 16;
     const float shrink = expm1f(g);
+#pragma unroll 1
     for (int r = 0; r < n; ++r) {
+        int rows = A.rows;
+        asm volatile("" : "+v"(rows));      // (compared anew: the masks of all rows would not fit the scalar registers)
+        const float z = A.update_scale * (float)zs[r * vpitch + column];
+        float part = 0.0f;
 #pragma unroll
-        for (int nv = 0; nv < NV; ++nv) {
-            const float z = A.update_scale * (float)zs[r * vpitch + column(nv)];
-            float part = 0.0f;
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 16 * kt + 4 * quad + i;
-                    if (row >= A.rows) continue;
-                    float c = s[kt][nv][i];
-                    if (!A.reversed) c = fmaf(c, shrink, c);
-                    c = fmaf((float)ys[r * kpitch + row], z, c);
-                    if (OUTPUT) part = fmaf((float)xs[r * kpitch + row], c, part);
-                    if (A.reversed) c = fmaf(c, shrink, c);
-                    s[kt][nv][i] = c;
-                }
-            if (OUTPUT) {
-                part += __shfl_xor(part, 16);
-                part += __shfl_xor(part, 32);
-                store(r, nv, A.out_scale * part);
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * kt + 4 * quad + i;
+                if (row >= rows) continue;
+                float c = s[kt][i];
+                if (!A.reversed) c = fmaf(c, shrink, c);
+                c = fmaf((float)ys[r * kpitch + row], z, c);
+                if (OUTPUT) part = fmaf((float)xs[r * kpitch + row], c, part);
+                if (A.reversed) c = fmaf(c, shrink, c);
+                s[kt][i] = c;
             }
+        if (OUTPUT) {
+            part += __shfl_xor(part, 16);
+            part += __shfl_xor(part, 32);
+            store(r, A.out_scale * part);
         }
     }
 }
 
-// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; PARTS: fragments that the state's update takes
-// each weighted z in (Matrix<E>::EXACT: all its digits); OUTPUT: 0 for launches that only work out the segments' own states
-template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT, int WAVES>
-__global__ __launch_bounds__(kChunkThreads, WAVES) void sig_attention_chunk_kernel(ChunkArgs G)
+// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; VT: columns of a workgroup; PARTS: fragments that
+// the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits); OUTPUT: 0 for launches that only work out the
+// segments' own states
+template <typename T, typename O, typename E, int C, int K, int VT, int PARTS, bool OUTPUT>
+__global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
 {
     using M = Matrix<E>;
     using Frag = typename M::Frag;
-    constexpr int VT = 64 * NV, KPITCH = K + M::PAD, VPITCH = VT + M::PAD;
+    constexpr int THREADS = 4 * VT, WAVES = VT / 16, KPITCH = K + M::PAD, VPITCH = VT + M::PAD;
     constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, SUB = M::SUB;
     constexpr int SPLIT = SUB == 2 ? 2 : 1;       // bfloat16 fragments of the state and of the triangle: 16 digits
     const AttentionArgs &A = G.a;
     __shared__ __attribute__((aligned(16))) E xs[OUTPUT ? C * KPITCH : 8], ys[C * KPITCH], zs[C * VPITCH];
-    __shared__ float power[C + 1];                // l^0 .. l^C
+    __shared__ Frag triangle[OUTPUT ? MT * STEPS * SPLIT * 64 : 1];
+    __shared__ float after[C + 2];                // out_scale l^(i+1)
+    __shared__ float gap_weight[C + 16];          // out_scale update_scale l^(i-15), zeros up to i = 14
+    __shared__ float left_weight[2 * C];          // update_scale l^(C-1-i+e), zeros from i = C on
 
     const int64_t head = blockIdx.x % A.heads, b = blockIdx.x / A.heads;
-    const int lane = threadIdx.x % 64, line = lane % 16, quad = lane / 16, wave = threadIdx.x / 64;
-    const int c0 = blockIdx.y * VT;               // first column of the workgroup, and of the wavefront in it
-    const int wave_column = wave * 16 * NV;
+    const int lane = threadIdx.x % 64, line = lane % 16, quad = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int c0 = blockIdx.y * VT, width = A.columns - c0, column = wave * 16 + line;     // of the workgroup, and of the lane in it
     const int64_t length = attention_length(A, b), first = (int64_t)blockIdx.z * G.segment_tokens;
     const int64_t last = first + G.segment_tokens < length && (int)blockIdx.z + 1 < G.segments ? first + G.segment_tokens : length;
     const float g = A.log_decay[head];
-    for (int i = threadIdx.x; i <= C; i += kChunkThreads) power[i] = i == 0 ? 1.0f : expf((float)i * g);
+    const auto power = [&](int i) { return i == 0 ? 1.0f : expf((float)i * g); };
+    if (OUTPUT) {
+        for (int i = threadIdx.x; i < C + 2; i += THREADS) after[i] = A.out_scale * power(i);
+        for (int i = threadIdx.x; i < C + 16; i += THREADS) gap_weight[i] = i < 15 ? 0.0f : A.out_scale * A.update_scale * power(i - 15);
+        for (int i = threadIdx.x; i < MT * STEPS * SPLIT * 64; i += THREADS) triangle[i] = Frag{};
+    }
+    for (int i = threadIdx.x; i < 2 * C; i += THREADS) left_weight[i] = i < C ? A.update_scale * power(C - 1 - i + A.reversed) : 0.0f;
 
-    // token number i of the pass is at x + i * stride
+    // token number i of the pass is at x + i * xstep
     const int64_t start = A.reversed ? length - 1 : 0;
     const int64_t xstep = A.reversed ? -A.xs[1] : A.xs[1], ystep = A.reversed ? -A.ys[1] : A.ys[1];
     const int64_t zstep = A.reversed ? -A.zs[1] : A.zs[1], ostep = A.reversed ? -A.os[1] : A.os[1];
@@ -159,162 +173,126 @@ __global__ __launch_bounds__(kChunkThreads, WAVES) void sig_attention_chunk_kern
     const T *z = (const T *)A.z + b * A.zs[0] + head / A.z_group * A.zs[2] + start * A.zs[1] + c0;
     O *o = (O *)A.o + b * A.os[0] + head * A.os[2] + start * A.os[1] + c0;
 
-    const int width = A.columns - c0;
-    auto column = [&](int nv) { return wave_column + chunk_column<O, NV>(nv, line); };
-    // the state: tile (kt, nv) holds, in a lane, column `line` of the tile at rows 16 kt + 4 quad + 0..3
-    f4 s[K / 16][NV];
+    // the state: tile kt holds, in a lane, its column at rows 16 kt + 4 quad + 0..3
+    f4 s[K / 16];
     const int64_t head_state = (int64_t)A.rows * A.columns, at_head = (int64_t)b * A.heads + head;
     const bool own = !OUTPUT || G.segments > 1;   // states in scratch
     const int64_t row_stride = own ? A.columns : A.row_stride, column_stride = own ? 1 : A.column_stride;
     float *at_segment = G.states + ((int64_t)blockIdx.z * A.B * A.heads + at_head) * head_state;
-    const float *from = !OUTPUT ? nullptr : own ? at_segment : A.state ? A.state + at_head * head_state : nullptr;
+    if constexpr (!OUTPUT) {
 #pragma unroll
-    for (int kt = 0; kt < K / 16; ++kt)
+        for (int kt = 0; kt < K / 16; ++kt) s[kt] = f4{};
+    } else {
+        const float *at = (own ? at_segment : A.state + at_head * head_state) + 4 * quad * row_stride + (c0 + column) * column_stride;
+        int rows = (own || A.state) && column < width ? A.rows - 4 * quad : 0;
+        asm volatile("" : "+v"(rows));
 #pragma unroll
-        for (int nv = 0; nv < NV; ++nv)
+        for (int kt = 0; kt < K / 16; ++kt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * kt + 4 * quad + i;
-                s[kt][nv][i] = from && row < A.rows && column(nv) < width ? from[row * row_stride + (c0 + column(nv)) * column_stride] : 0.0f;
-            }
+            for (int i = 0; i < 4; ++i) s[kt][i] = 16 * kt + i < rows ? at[(16 * kt + i) * row_stride] : 0.0f;
+    }
 
-    TileLoader<T, E, C, K> xl, yl;
-    TileLoader<T, E, C, VT> zl;
+    TileLoader<T, E, C, K, THREADS> xl(x + first * xstep, xstep, A.rows), yl(y + first * ystep, ystep, A.rows);
+    TileLoader<T, E, C, VT, THREADS> zl(z + first * zstep, zstep, width);
     auto load = [&](int64_t t) {
         const int n = last - t < C ? (int)(last - t) : C;
-        if (OUTPUT) xl.load(x + t * xstep, xstep, n, A.rows);
-        yl.load(y + t * ystep, ystep, n, A.rows);
-        zl.load(z + t * zstep, zstep, n, width);
+        if (OUTPUT) xl.load(n);
+        yl.load(n);
+        zl.load(n);
     };
     if (first < last) load(first);
     __syncthreads();
-    // weights of the triangle: l^(16 d + line - 4 quad - i) for tiles d apart, nothing above the diagonal
-    f4 inside[OUTPUT ? MT : 1];
-    if (OUTPUT)
-#pragma unroll
-        for (int d = 0; d < MT; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int gap = 16 * d + line - 4 * quad - i;
-                inside[d][i] = gap >= 0 ? A.out_scale * A.update_scale * power[gap] : 0.0f;
-            }
 
     bool by_token = false;
     for (int64_t t0 = first; t0 < last; t0 += C) {
         const int n = last - t0 < C ? (int)(last - t0) : C;
-        if (OUTPUT) xl.store(xs, KPITCH, x + t0 * xstep, xstep, n, A.rows);
-        yl.store(ys, KPITCH, y + t0 * ystep, ystep, n, A.rows);
-        zl.store(zs, VPITCH, z + t0 * zstep, zstep, n, width);
+        if (OUTPUT) xl.store(xs, KPITCH, n);
+        yl.store(ys, KPITCH, n);
+        zl.store(zs, VPITCH, n);
         __syncthreads();
         if (t0 + C < last) load(t0 + C);
 
-        if constexpr (!OUTPUT) {
-            if (by_token) {
-                chunk_by_token<false>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [](int, int, float) {});
-                __syncthreads();
-                continue;
-            }
-        }
-        Frag zf[STEPS][NV];
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-            for (int nv = 0; nv < NV; ++nv)
-                zf[st][nv] = M::along_columns(zs + wave_column, VPITCH, st * M::STEP, [&](int r) { return chunk_column<O, NV>(nv, r); });
-
+        f4 out[OUTPUT ? MT : 1] = {};
         if constexpr (OUTPUT) {
-            f4 out[MT][NV] = {};
+            // this wavefront's tiles of the triangle: tokens 16 m + line against 16 j + 4 quad + 0..3
+            for (int tile = wave; tile < MT * (MT + 1) / 2; tile += WAVES) {
+                int m = 0;
+#pragma unroll
+                for (int i = 1; i < MT; ++i) m += tile >= i * (i + 1) / 2;
+                const int j = tile - m * (m + 1) / 2;
+                f4 dots = {};
+#pragma unroll
+                for (int kk = 0; kk < KSTEPS; ++kk)
+                    dots = M::multiply(M::along_rows(ys, KPITCH, 16 * j, kk * M::STEP), M::along_rows(xs, KPITCH, 16 * m, kk * M::STEP), dots);
+                float values[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = gap_weight[15 + 16 * (m - j) + line - 4 * quad - i];
+                    values[i] = j < m || 4 * quad + i <= line ? w * dots[i] : 0.0f;      // (a later token may be infinite)
+                }
+                M::template put<SPLIT>(values, triangle + (m * STEPS + j / SUB) * SPLIT * 64 + lane, j % SUB);
+            }
             // what lies before the chunk
 #pragma unroll
             for (int kk = 0; kk < KSTEPS; ++kk) {
-                Frag sf[NV][SPLIT];
+                float values[4 * SUB];
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    float values[4 * SUB];
-#pragma unroll
-                    for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][nv][e % 4];
-                    M::template split<SPLIT>(values, sf[nv]);
-                }
+                for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][e % 4];
+                Frag sf[SPLIT];
+                M::template split<SPLIT>(values, sf);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const Frag xf = M::along_rows(xs, KPITCH, 16 * m, kk * M::STEP);
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int p = 0; p < SPLIT; ++p) out[m][nv] = M::multiply(sf[nv][p], xf, out[m][nv]);
+                    for (int p = 0; p < SPLIT; ++p) out[m] = M::multiply(sf[p], xf, out[m]);
                 }
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const float w = A.out_scale * power[16 * m + line + 1 - A.reversed];
+            for (int m = 0; m < MT; ++m) out[m] *= after[16 * m + line + 1 - A.reversed];
+            __syncthreads();
+        } else if (by_token) {
+            chunk_by_token<false>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [](int, float) {});
+            __syncthreads();
+            continue;
+        }
+
+        Frag zf[STEPS];
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) out[m][nv] *= w;
-            }
-            // the triangle
+        for (int st = 0; st < STEPS; ++st) zf[st] = M::along_columns(zs, VPITCH, st * M::STEP, wave * 16);
+        if constexpr (OUTPUT) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                Frag xf[KSTEPS];
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int kk = 0; kk < KSTEPS; ++kk) xf[kk] = M::along_rows(xs, KPITCH, 16 * m, kk * M::STEP);
+                for (int st = 0; st * SUB <= m; ++st)
 #pragma unroll
-                for (int st = 0; st * SUB <= m; ++st) {
-                    float values[4 * SUB];
-#pragma unroll
-                    for (int sub = 0; sub < SUB; ++sub) {
-                        const int j = st * SUB + sub;
-                        f4 dots = {};
-                        if (j <= m) {
-#pragma unroll
-                            for (int kk = 0; kk < KSTEPS; ++kk) dots = M::multiply(M::along_rows(ys, KPITCH, 16 * j, kk * M::STEP), xf[kk], dots);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            // (a token that is not there, or comes later, must not spoil the sum with 0 * infinity)
-                            const float w = j <= m ? inside[j <= m ? m - j : 0][i] : 0.0f;
-                            values[4 * sub + i] = j < m || (j == m && 4 * quad + i <= line) ? w * dots[i] : 0.0f;
-                        }
-                    }
-                    Frag pf[SPLIT];
-                    M::template split<SPLIT>(values, pf);
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int p = 0; p < SPLIT; ++p) out[m][nv] = M::multiply(zf[st][nv], pf[p], out[m][nv]);
-                }
-            }
+                    for (int p = 0; p < SPLIT; ++p) out[m] = M::multiply(zf[st], triangle[((m * STEPS + st) * SPLIT + p) * 64 + lane], out[m]);
             float worst = 0.0f;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) worst = fmaf(out[m][nv][i], 0.0f, worst);     // a NaN from anything that is not finite
+                for (int i = 0; i < 4; ++i) worst = fmaf(out[m][i], 0.0f, worst);     // a NaN from anything that is not finite
             if (__any(!(worst == 0.0f))) {
-                chunk_by_token<true>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [&](int r, int nv, float value) {
-                    if (quad == 0 && column(nv) < width) o[(t0 + r) * ostep + column(nv)] = from_float<O>(value);
+                chunk_by_token<true>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [&](int r, float value) {
+                    if (quad == 0 && column < width) o[(t0 + r) * ostep + column] = from_float<O>(value);
                 });
                 __syncthreads();
                 continue;
             }
+            const int at = wave * 16 + 4 * quad;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const int r = 16 * m + line;
                 if (r >= n) continue;
-                O *to = o + (t0 + r) * ostep;
-                constexpr int RUN = sizeof(O) == 2 && NV == 2 ? 8 : 4;
+                O *to = o + (t0 + r) * ostep + at;
+                Pack<O, 4> values;
 #pragma unroll
-                for (int q = 0; q < 4 * NV / RUN; ++q) {
-                    const int at = wave_column + (RUN == 8 ? 8 * quad : 16 * q + 4 * quad);
-                    Pack<O, RUN> values;
+                for (int j = 0; j < 4; ++j) values.v[j] = from_float<O>(out[m][j]);
+                if (at + 4 <= width) {
+                    *(Pack<O, 4> *)to = values;
+                } else {
 #pragma unroll
-                    for (int j = 0; j < RUN; ++j) values.v[j] = from_float<O>(out[m][RUN == 8 ? j / 4 : q][j % 4]);
-                    if (at + RUN <= width) {
-                        *(Pack<O, RUN> *)(to + at) = values;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < RUN; ++j)
-                            if (at + j < width) to[at + j] = values.v[j];
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        if (at + j < width) to[j] = values.v[j];
                 }
             }
         }
@@ -324,29 +302,20 @@ __global__ __launch_bounds__(kChunkThreads, WAVES) void sig_attention_chunk_kern
 #pragma unroll
         for (int kt = 0; kt < K / 16; ++kt)
 #pragma unroll
-            for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[kt][nv][i] = fmaf(s[kt][nv][i], shrink, s[kt][nv][i]);
+            for (int i = 0; i < 4; ++i) s[kt][i] = fmaf(s[kt][i], shrink, s[kt][i]);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-            Frag wf[NV][PARTS];
+            float values[4 * SUB];
 #pragma unroll
-            for (int nv = 0; nv < NV; ++nv) {
-                float values[4 * SUB];
-#pragma unroll
-                for (int e = 0; e < 4 * SUB; ++e) {
-                    const int j = st * M::STEP + e / 4 * 16 + 4 * quad + e % 4, ahead = n - 1 - j + A.reversed;
-                    values[e] = ahead >= 0 ? M::value(zf[st][nv], e) * (A.update_scale * power[ahead]) : 0.0f;
-                }
-                M::template split<PARTS>(values, wf[nv]);
-            }
+            for (int e = 0; e < 4 * SUB; ++e)
+                values[e] = M::value(zf[st], e) * left_weight[C - n + st * M::STEP + e / 4 * 16 + 4 * quad + e % 4];
+            Frag wf[PARTS];
+            M::template split<PARTS>(values, wf);
 #pragma unroll
             for (int kt = 0; kt < K / 16; ++kt) {
-                const Frag yf = M::along_columns(ys, KPITCH, st * M::STEP, [&](int r) { return 16 * kt + r; });
+                const Frag yf = M::along_columns(ys, KPITCH, st * M::STEP, 16 * kt);
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p) s[kt][nv] = M::multiply(yf, wf[nv][p], s[kt][nv]);
+                for (int p = 0; p < PARTS; ++p) s[kt] = M::multiply(yf, wf[p], s[kt]);
             }
         }
         if constexpr (OUTPUT) {
@@ -357,15 +326,13 @@ __global__ __launch_bounds__(kChunkThreads, WAVES) void sig_attention_chunk_kern
 #pragma unroll
                 for (int kt = 0; kt < K / 16; ++kt)
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) worst = fmaf(s[kt][nv][i], 0.0f, worst);
+                    for (int i = 0; i < 4; ++i) worst = fmaf(s[kt][i], 0.0f, worst);
             if (__syncthreads_or(!(worst == 0.0f))) {
                 by_token = true;
 #pragma unroll
-                for (int kt = 0; kt < K / 16; ++kt)
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv) s[kt][nv] = f4{};
+                for (int kt = 0; kt < K / 16; ++kt) s[kt] = f4{};
+                yl = TileLoader<T, E, C, K, THREADS>(y + first * ystep, ystep, A.rows);
+                zl = TileLoader<T, E, C, VT, THREADS>(z + first * zstep, zstep, width);
                 t0 = first - C;
                 load(first);
             }
@@ -377,54 +344,51 @@ __global__ __launch_bounds__(kChunkThreads, WAVES) void sig_attention_chunk_kern
             // behind the length
             O *rest = (O *)A.o + b * A.os[0] + head * A.os[2] + c0;
             const int left = width < VT ? width : VT;
-            for (int64_t i = threadIdx.x; i < (A.T - length) * left; i += kChunkThreads) rest[(length + i / left) * A.os[1] + i % left] = from_float<O>(0.0f);
+            for (int64_t i = threadIdx.x; i < (A.T - length) * left; i += THREADS) rest[(length + i / left) * A.os[1] + i % left] = from_float<O>(0.0f);
         }
         if (own || !A.state_out) return;
     }
-    float *to = own ? at_segment : A.state_out + at_head * head_state;
+    float *to = (own ? at_segment : A.state_out + at_head * head_state) + 4 * quad * row_stride + (c0 + column) * column_stride;
+    int rows = column < width ? A.rows - 4 * quad : 0;
+    asm volatile("" : "+v"(rows));
 #pragma unroll
     for (int kt = 0; kt < K / 16; ++kt)
 #pragma unroll
-        for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * kt + 4 * quad + i;
-                if (row < A.rows && column(nv) < width) to[row * row_stride + (c0 + column(nv)) * column_stride] = s[kt][nv][i];
-            }
+        for (int i = 0; i < 4; ++i)
+            if (16 * kt + i < rows) to[(16 * kt + i) * row_stride] = s[kt][i];
 }
 
-// The instance for `G`: columns of a workgroup 64 nv; rows up to 256
+// The instance for `G`: vt columns a workgroup
 template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
-void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
+void launch_chunk_instance(const ChunkArgs &G, int vt, hipStream_t st)
 {
     const AttentionArgs &A = G.a;
-    const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((A.columns + 64 * nv - 1) / (64 * nv)), (unsigned)G.segments);
+    const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((A.columns + vt - 1) / vt), (unsigned)G.segments);
     auto go = [&](auto k) {
         constexpr int K = decltype(k)::value;
-        constexpr int TOKENS = K > 192 && C > 32 ? 32 : C, WIDE = K <= 128 ? 2 : 1;      // (registers)
-        if (WIDE == 2 && nv == 2) sig_attention_chunk_kernel<T, O, E, TOKENS, K, WIDE, PARTS, OUTPUT, K * WIDE <= 64 ? 2 : 1><<<grid, kChunkThreads, 0, st>>>(G);
-        else sig_attention_chunk_kernel<T, O, E, TOKENS, K, 1, PARTS, OUTPUT, K <= 64 ? 2 : 1><<<grid, kChunkThreads, 0, st>>>(G);
+        constexpr int WIDE = K <= 128 ? 128 : 64;       // (registers)
+        if (vt == WIDE) sig_attention_chunk_kernel<T, O, E, C, K, WIDE, PARTS, OUTPUT><<<grid, 4 * WIDE, 0, st>>>(G);
+        else sig_attention_chunk_kernel<T, O, E, C, K, 64, PARTS, OUTPUT><<<grid, 256, 0, st>>>(G);
     };
-    if (A.rows <= 32) go(std::integral_constant<int, 32>());
-    else if (A.rows <= 64) go(std::integral_constant<int, 64>());
+    if (A.rows <= 64) go(std::integral_constant<int, 64>());
     else if (A.rows <= 128) go(std::integral_constant<int, 128>());
     else if (A.rows <= 192) go(std::integral_constant<int, 192>());
     else go(std::integral_constant<int, 256>());
 }
 
 template <typename T, typename E, int C>
-void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st)
+void launch_chunk(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st)
 {
     constexpr int PARTS = Matrix<E>::EXACT;
-    if (!output) launch_chunk_instance<T, T, E, C, PARTS, false>(G, nv, st);
-    else if (partial) launch_chunk_instance<T, float, E, C, PARTS, true>(G, nv, st);
-    else launch_chunk_instance<T, T, E, C, PARTS, true>(G, nv, st);
+    if (!output) launch_chunk_instance<T, T, E, C, PARTS, false>(G, vt, st);
+    else if (partial) launch_chunk_instance<T, float, E, C, PARTS, true>(G, vt, st);
+    else launch_chunk_instance<T, T, E, C, PARTS, true>(G, vt, st);
 }
 
 // one for each type of the operands, in a file of its own; partial: float32 output
-void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
-void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
-void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_f32(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
+void launch_chunk_bf16(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
+void launch_chunk_f16(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
 
 }  // namespace sig
 #endif

@@ -33,12 +33,11 @@ struct Matrix<float> {
         const int lane = threadIdx.x % kWaveLanes;
         return *(const f4 *)(m + (line + lane % 16) * pitch + at + 4 * (lane / 16));
     }
-    // lines = columns column(0 .. 15) of `m`, summed axis = its rows from `at` on
-    template <typename F>
-    static __device__ Frag along_columns(const float *m, int pitch, int at, F column)
+    // lines = columns of `m` from `line` on, summed axis = its rows from `at` on
+    static __device__ Frag along_columns(const float *m, int pitch, int at, int line)
     {
         const int lane = threadIdx.x % kWaveLanes;
-        const float *p = m + (at + 4 * (lane / 16)) * pitch + column(lane % 16);
+        const float *p = m + (at + 4 * (lane / 16)) * pitch + line + lane % 16;
         return f4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
     }
     // left x right on top of `sum`
@@ -55,6 +54,12 @@ struct Matrix<float> {
     static __device__ void split(const float *x, Frag *parts)
     {
         parts[0] = f4{x[0], x[1], x[2], x[3]};
+    }
+    // the lane's four places of a result tile into the fragments at `to` (PARTS of them, 64 apart), group `sub`
+    template <int PARTS>
+    static __device__ void put(const float *x, Frag *to, int)
+    {
+        *to = f4{x[0], x[1], x[2], x[3]};
     }
 
 private:
@@ -74,13 +79,11 @@ struct Matrix<bf16> {
         const bf16 *p = m + (line + lane % 16) * pitch + at + 4 * (lane / 16);
         return __builtin_shufflevector(*(const b4 *)p, *(const b4 *)(p + 16), 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    // The transposing LDS read: 16 lanes name 16 groups of four values, group i of row i / 4; lane i receives value i % 4 of the groups
-    // i / 4 of the four rows.  column(0), column(4), column(8), column(12) each begin four neighbouring columns.
-    template <typename F>
-    static __device__ Frag along_columns(const bf16 *m, int pitch, int at, F column)
+    // The transposing LDS read: 16 lanes name the quarters of four rows of 16 values, and lane i receives value i of each row.
+    static __device__ Frag along_columns(const bf16 *m, int pitch, int at, int line)
     {
         const int lane = threadIdx.x % kWaveLanes, i = lane % 16;
-        const bf16 *p = m + (at + 4 * (lane / 16) + i / 4) * pitch + column(4 * (i % 4));
+        const bf16 *p = m + (at + 4 * (lane / 16) + i / 4) * pitch + line + 4 * (i % 4);
         using Read = __attribute__((address_space(3))) s4;
         const s4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)p);
         const s4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + 16 * pitch));
@@ -92,20 +95,34 @@ struct Matrix<bf16> {
     template <int PARTS>
     static __device__ void split(const float *x, Frag *parts)
     {
-        float rest[8];
+        digits<PARTS, 8>(x, parts);
+    }
+    template <int PARTS>
+    static __device__ void put(const float *x, Frag *to, int sub)
+    {
+        b4 parts[PARTS];
+        digits<PARTS, 4>(x, parts);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rest[e] = x[e];
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                parts[p][e] = (bf16)rest[e];
-                if (p + 1 < PARTS) rest[e] -= (float)parts[p][e];
-            }
+        for (int p = 0; p < PARTS; ++p) *((b4 *)(to + 64 * p) + sub) = parts[p];
     }
 
 private:
     static constexpr int kWaveLanes = 64;
+
+    template <int PARTS, int N, typename V>
+    static __device__ void digits(const float *x, V *parts)
+    {
+        float rest[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) rest[e] = x[e];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                parts[p][e] = (bf16)rest[e];
+                if (p + 1 < PARTS) rest[e] -= (float)parts[p][e];
+            }
+    }
 };
 
 }  // namespace sig
