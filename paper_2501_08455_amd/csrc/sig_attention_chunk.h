@@ -6,8 +6,8 @@
 //   S  <- l^n S + update_scale sum_j l^(n-1-j+e) y_j (x) z_j
 // All powers are of one head's decay and not above 1 where it decays, so nothing has to be scaled back.
 //
-// A workgroup holds VT columns of one head's state in registers, 16 a wavefront, as the tiles of a matrix product: they are the left
-// operand of x S as they lie.  x, y and z of a chunk are staged in LDS, the next chunk's loads stay in flight in registers
+// A workgroup of four wavefronts holds 64 NV columns of one head's state in registers, 16 NV a wavefront, as the tiles of a matrix
+// product: they are the left operand of x S as they lie.  x, y and z of a chunk are staged in LDS, the next chunk's loads stay in flight in registers
 // meanwhile.  The tiles of the triangle are shared out over the wavefronts and passed on through LDS, as the fragments that
 // everyone reads.  Output tiles are taken as their transpose, in which a lane holds neighbouring columns of one token.
 //
@@ -23,6 +23,11 @@
 #include "sig_matrix.h"
 
 namespace sig {
+
+constexpr int kChunkThreads = 256;
+
+template <int N>
+using Number = std::integral_constant<int, N>;
 
 // The pieces along time that different workgroups take (A.T tokens from place `segment * segment_tokens` on)
 struct ChunkArgs {
@@ -73,6 +78,8 @@ struct TileLoader {
         }
         p += C * stride;
     }
+    // the last tile again
+    __device__ void back() { p -= C * stride; }
     // the tile of the last load(n)
     __device__ void store(E *tile, int pitch, int n) const
     {
@@ -80,10 +87,13 @@ struct TileLoader {
         for (int i = 0; i < COUNT; ++i) {
             const int r = row() + i * ROWS;
             const bool ok = there && r < n;
-            struct alignas(GROUP * sizeof(E)) { E v[GROUP]; } values;
+            struct { E v[GROUP]; } values;
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) values.v[j] = ok ? (E)held[i].v[j] : (E)0.0f;
-            if (W == WIDE || place() < W) *(decltype(values) *)(tile + r * pitch + place()) = values;
+            for (int j = 0; j < GROUP; ++j) values.v[j] = (E)held[i].v[j];
+            using u4 = __attribute__((ext_vector_type(4))) unsigned;
+            u4 bits = __builtin_bit_cast(u4, values);
+            bits = ok ? bits : u4{};
+            if (W == WIDE || place() < W) *(u4 *)(tile + r * pitch + place()) = bits;
         }
         // the last values of tokens that are no whole number of groups (after the zeros of the same thread, which then reads from place 0)
         const int rest = width % GROUP, c = place();
@@ -97,54 +107,72 @@ struct TileLoader {
     }
 };
 
-// One token after the other, for the chunk in LDS (see above).  store(r, o_r at the lane's column)
-template <bool OUTPUT, int KT, typename E, typename Store>
-__device__ inline void chunk_by_token(const AttentionArgs &A, float g, int n, const E *xs, const E *ys, int kpitch, const E *zs, int vpitch,
-                                      f4 (&s)[KT], int column, Store store)
+// One token after the other, for the chunk in LDS (see above).  store(r, nv, o_r at the lane's column of tile nv)
+template <bool OUTPUT, int KT, int NV, typename E, typename Row, typename Store>
+__device__ inline void chunk_by_token(const AttentionArgs &A, float g, int n, const E *xs, int xpitch, const E *ys, int ypitch, const E *zs, int zpitch,
+                                      f4 (&s)[KT][NV], int first_row, Row row_of, int column, Store store)
 {
-    const int quad = threadIdx.x % 64 / 16;
     const float shrink = expm1f(g);
 #pragma unroll 1
     for (int r = 0; r < n; ++r) {
         int rows = A.rows;
         asm volatile("" : "+v"(rows));      // (compared anew: the masks of all rows would not fit the scalar registers)
-        const float z = A.update_scale * (float)zs[r * vpitch + column];
-        float part = 0.0f;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
+        for (int nv = 0; nv < NV; ++nv) {
+            const float z = A.update_scale * (float)zs[r * zpitch + column + 16 * nv];
+            float part = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * kt + 4 * quad + i;
-                if (row >= rows) continue;
-                float c = s[kt][i];
-                if (!A.reversed) c = fmaf(c, shrink, c);
-                c = fmaf((float)ys[r * kpitch + row], z, c);
-                if (OUTPUT) part = fmaf((float)xs[r * kpitch + row], c, part);
-                if (A.reversed) c = fmaf(c, shrink, c);
-                s[kt][i] = c;
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = first_row + row_of(kt) + i;
+                    if (row >= rows) continue;
+                    float c = s[kt][nv][i];
+                    if (!A.reversed) c = fmaf(c, shrink, c);
+                    c = fmaf((float)ys[r * ypitch + row], z, c);
+                    if (OUTPUT) part = fmaf((float)xs[r * xpitch + row], c, part);
+                    if (A.reversed) c = fmaf(c, shrink, c);
+                    s[kt][nv][i] = c;
+                }
+            if (OUTPUT) {
+                part += __shfl_xor(part, 16);
+                part += __shfl_xor(part, 32);
+                store(r, nv, A.out_scale * part);
             }
-        if (OUTPUT) {
-            part += __shfl_xor(part, 16);
-            part += __shfl_xor(part, 32);
-            store(r, A.out_scale * part);
         }
     }
 }
 
-// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; VT: columns of a workgroup; PARTS: fragments that
+// The order of what has been written since the last call: LOADS reads of LDS, then PRODUCTS products with vector instructions between them
+template <int LOADS, int PRODUCTS>
+__device__ inline void interleave()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, LOADS, 0);
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; NV: tiles of 16 columns a wavefront; PARTS: fragments that
 // the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits); OUTPUT: 0 for launches that only work out the
 // segments' own states
-template <typename T, typename O, typename E, int C, int K, int VT, int PARTS, bool OUTPUT>
-__global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
+template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT>
+__global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
 {
     using M = Matrix<E>;
     using Frag = typename M::Frag;
-    constexpr int THREADS = 4 * VT, WAVES = VT / 16, KPITCH = K + M::PAD, VPITCH = VT + M::PAD;
-    constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, SUB = M::SUB;
+    constexpr int THREADS = kChunkThreads, WAVES = THREADS / 64, VT = 64 * NV;
+    constexpr int XPITCH = K + M::PAD, YPITCH = K + M::COLUMN_PAD, ZPITCH = VT + M::COLUMN_PAD;
+    constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, KT = K / 16, SUB = M::SUB;
     constexpr int SPLIT = SUB == 2 ? 2 : 1;       // bfloat16 fragments of the state and of the triangle: 16 digits
+    constexpr int YB = 4;                       // tiles of the state whose operands are loaded at once
     const AttentionArgs &A = G.a;
-    __shared__ __attribute__((aligned(16))) E xs[OUTPUT ? C * KPITCH : 8], ys[C * KPITCH], zs[C * VPITCH];
+    __shared__ __attribute__((aligned(16))) E xs[OUTPUT ? C * XPITCH : 8], ys[C * YPITCH], zs[C * ZPITCH];
     __shared__ Frag triangle[OUTPUT ? MT * STEPS * SPLIT * 64 : 1];
+    __shared__ int spoilt;                        // whether a wavefront has met what is not finite
     __shared__ float after[C + 2];                // out_scale l^(i+1)
     __shared__ float gap_weight[C + 16];          // out_scale update_scale l^(i-15), zeros up to i = 14
     __shared__ float left_weight[2 * C];          // update_scale l^(C-1-i+e), zeros from i = C on
@@ -152,10 +180,11 @@ __global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_
     const int64_t head = blockIdx.x % A.heads, b = blockIdx.x / A.heads;
     const int lane = threadIdx.x % 64, line = lane % 16, quad = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int c0 = blockIdx.y * VT, width = A.columns - c0, column = wave * 16 + line;     // of the workgroup, and of the lane in it
+    const int c0 = blockIdx.y * VT, width = A.columns - c0, column = wave * 16 * NV + line;     // of the workgroup, and of the lane in it
     const int64_t length = attention_length(A, b), first = (int64_t)blockIdx.z * G.segment_tokens;
     const int64_t last = first + G.segment_tokens < length && (int)blockIdx.z + 1 < G.segments ? first + G.segment_tokens : length;
     const float g = A.log_decay[head];
+    if (threadIdx.x == 0) spoilt = 0;
     const auto power = [&](int i) { return i == 0 ? 1.0f : expf((float)i * g); };
     if (OUTPUT) {
         for (int i = threadIdx.x; i < C + 2; i += THREADS) after[i] = A.out_scale * power(i);
@@ -173,23 +202,28 @@ __global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_
     const T *z = (const T *)A.z + b * A.zs[0] + head / A.z_group * A.zs[2] + start * A.zs[1] + c0;
     O *o = (O *)A.o + b * A.os[0] + head * A.os[2] + start * A.os[1] + c0;
 
-    // the state: tile kt holds, in a lane, its column at rows 16 kt + 4 quad + 0..3
-    f4 s[K / 16];
+    // the state: tile (kt, nv) holds, in a lane, its column at rows first_row + row_of(kt) + 0..3
+    const int first_row = 4 * SUB * quad;
+    const auto row_of = [](int kt) { return kt / SUB * M::STEP + 4 * (kt % SUB); };
+    f4 s[KT][NV];
     const int64_t head_state = (int64_t)A.rows * A.columns, at_head = (int64_t)b * A.heads + head;
     const bool own = !OUTPUT || G.segments > 1;   // states in scratch
     const int64_t row_stride = own ? A.columns : A.row_stride, column_stride = own ? 1 : A.column_stride;
     float *at_segment = G.states + ((int64_t)blockIdx.z * A.B * A.heads + at_head) * head_state;
-    if constexpr (!OUTPUT) {
 #pragma unroll
-        for (int kt = 0; kt < K / 16; ++kt) s[kt] = f4{};
-    } else {
-        const float *at = (own ? at_segment : A.state + at_head * head_state) + 4 * quad * row_stride + (c0 + column) * column_stride;
-        int rows = (own || A.state) && column < width ? A.rows - 4 * quad : 0;
-        asm volatile("" : "+v"(rows));
+    for (int nv = 0; nv < NV; ++nv) {
+        if constexpr (!OUTPUT) {
 #pragma unroll
-        for (int kt = 0; kt < K / 16; ++kt)
+            for (int kt = 0; kt < KT; ++kt) s[kt][nv] = f4{};
+        } else {
+            const float *at = (own ? at_segment : A.state + at_head * head_state) + first_row * row_stride + (c0 + column + 16 * nv) * column_stride;
+            int rows = (own || A.state) && column + 16 * nv < width ? A.rows - first_row : 0;
+            asm volatile("" : "+v"(rows));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[kt][i] = 16 * kt + i < rows ? at[(16 * kt + i) * row_stride] : 0.0f;
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[kt][nv][i] = row_of(kt) + i < rows ? at[(row_of(kt) + i) * row_stride] : 0.0f;
+        }
     }
 
     TileLoader<T, E, C, K, THREADS> xl(x + first * xstep, xstep, A.rows), yl(y + first * ystep, ystep, A.rows);
@@ -203,16 +237,23 @@ __global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_
     if (first < last) load(first);
     __syncthreads();
 
-    bool by_token = false;
-    for (int64_t t0 = first; t0 < last; t0 += C) {
+    O *to = o + (first + line) * ostep + wave * 16 * NV + 4 * quad;      // the lane's outputs of the next chunk
+    // Loads from LDS are issued a block of products ahead (left alone, the compiler waits for each in turn), and the splitting of the
+    // next operand goes between the products: a product keeps its unit busy for four vector instructions.
+    int64_t t0 = first;
+    bool again = false;          // OUTPUT: whether this wavefront still owes the chunk in LDS
+    for (; t0 < last; t0 += C) {
         const int n = last - t0 < C ? (int)(last - t0) : C;
-        if (OUTPUT) xl.store(xs, KPITCH, n);
-        yl.store(ys, KPITCH, n);
-        zl.store(zs, VPITCH, n);
+        if (OUTPUT) xl.store(xs, XPITCH, n);
+        yl.store(ys, YPITCH, n);
+        zl.store(zs, ZPITCH, n);
         __syncthreads();
         if (t0 + C < last) load(t0 + C);
 
-        f4 out[OUTPUT ? MT : 1] = {};
+        O *to_chunk = to;
+        to += C * ostep;
+        f4 out[OUTPUT ? MT : 1][NV] = {};
+        Frag zf[STEPS][NV];
         if constexpr (OUTPUT) {
             // this wavefront's tiles of the triangle: tokens 16 m + line against 16 j + 4 quad + 0..3
             for (int tile = wave; tile < MT * (MT + 1) / 2; tile += WAVES) {
@@ -221,122 +262,217 @@ __global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_
                 for (int i = 1; i < MT; ++i) m += tile >= i * (i + 1) / 2;
                 const int j = tile - m * (m + 1) / 2;
                 f4 dots = {};
+                float weight[4];
 #pragma unroll
-                for (int kk = 0; kk < KSTEPS; ++kk)
-                    dots = M::multiply(M::along_rows(ys, KPITCH, 16 * j, kk * M::STEP), M::along_rows(xs, KPITCH, 16 * m, kk * M::STEP), dots);
+                for (int i = 0; i < 4; ++i) weight[i] = gap_weight[15 + 16 * (m - j) + line - 4 * quad - i];
+                constexpr int TB = KSTEPS < 4 ? KSTEPS : 4;
+#pragma unroll
+                for (int k0 = 0; k0 < KSTEPS; k0 += TB) {
+                    Frag left[TB], right[TB];
+#pragma unroll
+                    for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) {
+                        left[kk] = M::along_rows(ys, YPITCH, 16 * j, (k0 + kk) * M::STEP);
+                        right[kk] = M::along_rows(xs, XPITCH, 16 * m, (k0 + kk) * M::STEP);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) dots = M::multiply(left[kk], right[kk], dots);
+                }
                 float values[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float w = gap_weight[15 + 16 * (m - j) + line - 4 * quad - i];
-                    values[i] = j < m || 4 * quad + i <= line ? w * dots[i] : 0.0f;      // (a later token may be infinite)
-                }
+                for (int i = 0; i < 4; ++i) values[i] = j < m || 4 * quad + i <= line ? weight[i] * dots[i] : 0.0f;      // (a later token may be infinite)
                 M::template put<SPLIT>(values, triangle + (m * STEPS + j / SUB) * SPLIT * 64 + lane, j % SUB);
             }
             // what lies before the chunk
-#pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk) {
+            Frag xf[2][MT], sf[2][SPLIT];
+            auto state_step = [&](int kk, int nv, Frag (&to)[SPLIT]) {
                 float values[4 * SUB];
 #pragma unroll
-                for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][e % 4];
-                Frag sf[SPLIT];
-                M::template split<SPLIT>(values, sf);
+                for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][nv][e % 4];
+                M::template split<SPLIT>(values, to);
+            };
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const Frag xf = M::along_rows(xs, KPITCH, 16 * m, kk * M::STEP);
+            for (int m = 0; m < MT; ++m) xf[0][m] = M::along_rows(xs, XPITCH, 16 * m, 0);
+            state_step(0, 0, sf[0]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int p = 0; p < SPLIT; ++p) out[m] = M::multiply(sf[p], xf, out[m]);
+            for (int kk = 0; kk < KSTEPS; ++kk)
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) {
+                    const int now = (kk * NV + nv) % 2;
+                    if (nv == 0 && kk + 1 < KSTEPS) {
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) xf[(kk + 1) % 2][m] = M::along_rows(xs, XPITCH, 16 * m, (kk + 1) * M::STEP);
+                    } else if (nv == NV - 1 && kk + 1 == KSTEPS) {
+#pragma unroll
+                        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                            for (int i = 0; i < NV; ++i) zf[st][i] = M::template along_columns<false>(zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * i);
+                    }
+                    if (nv + 1 < NV) state_step(kk, nv + 1, sf[1 - now]);
+                    else if (kk + 1 < KSTEPS) state_step(kk + 1, 0, sf[1 - now]);
+#pragma unroll
+                    for (int p = 0; p < SPLIT; ++p)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) out[m][nv] = M::multiply(sf[now][p], xf[kk % 2][m], out[m][nv]);
+                    interleave<MT, SPLIT * MT * M::PRODUCTS>();
                 }
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m) out[m] *= after[16 * m + line + 1 - A.reversed];
-            __syncthreads();
-        } else if (by_token) {
-            chunk_by_token<false>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [](int, float) {});
-            __syncthreads();
-            continue;
-        }
-
-        Frag zf[STEPS];
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) zf[st] = M::along_columns(zs, VPITCH, st * M::STEP, wave * 16);
-        if constexpr (OUTPUT) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int st = 0; st * SUB <= m; ++st)
-#pragma unroll
-                    for (int p = 0; p < SPLIT; ++p) out[m] = M::multiply(zf[st], triangle[((m * STEPS + st) * SPLIT + p) * 64 + lane], out[m]);
-            float worst = 0.0f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) worst = fmaf(out[m][i], 0.0f, worst);     // a NaN from anything that is not finite
-            if (__any(!(worst == 0.0f))) {
-                chunk_by_token<true>(A, g, n, xs, ys, KPITCH, zs, VPITCH, s, column, [&](int r, float value) {
-                    if (quad == 0 && column < width) o[(t0 + r) * ostep + column] = from_float<O>(value);
-                });
-                __syncthreads();
-                continue;
-            }
-            const int at = wave * 16 + 4 * quad;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const int r = 16 * m + line;
-                if (r >= n) continue;
-                O *to = o + (t0 + r) * ostep + at;
-                Pack<O, 4> values;
+                const float w = after[16 * m + line + 1 - A.reversed];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) values.v[j] = from_float<O>(out[m][j]);
-                if (at + 4 <= width) {
-                    *(Pack<O, 4> *)to = values;
-                } else {
+                for (int nv = 0; nv < NV; ++nv) out[m][nv] *= w;
+            }
+            __syncthreads();
+            // the triangle
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (at + j < width) to[j] = values.v[j];
+            for (int st = 0; st < STEPS; ++st) {
+                Frag pairs[MT][SPLIT];
+#pragma unroll
+                for (int m = st * SUB; m < MT; ++m)
+#pragma unroll
+                    for (int p = 0; p < SPLIT; ++p) pairs[m][p] = triangle[((m * STEPS + st) * SPLIT + p) * 64 + lane];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int p = 0; p < SPLIT; ++p)
+#pragma unroll
+                    for (int m = st * SUB; m < MT; ++m)
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv) out[m][nv] = M::multiply(zf[st][nv], pairs[m][p], out[m][nv]);
+            }
+            float worst = 0.0f;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) worst = fmaf(out[m][nv][i], 0.0f, worst);     // a NaN from anything that is not finite
+            again = __any(!(worst == 0.0f));
+            if (again) {
+                spoilt = 1;
+            } else {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    if (16 * m + line >= n) continue;
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) {
+                        O *at = to_chunk + 16 * m * ostep + 16 * nv;
+                        Pack<O, 4> values;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) values.v[j] = from_float<O>(out[m][nv][j]);
+                        const int left = width - (wave * 16 * NV + 16 * nv + 4 * quad);
+                        if (left >= 4) {
+                            store_pack(at, values);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 3; ++j)
+                                if (j < left) at[j] = values.v[j];
+                        }
+                    }
                 }
             }
-        }
-
-        // the state behind the chunk.  l^n = 1 + (l^n - 1): the power itself, rounded, would drift over many chunks where little decays
-        const float shrink = expm1f((float)n * g);
-#pragma unroll
-        for (int kt = 0; kt < K / 16; ++kt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[kt][i] = fmaf(s[kt][i], shrink, s[kt][i]);
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-            float values[4 * SUB];
-#pragma unroll
-            for (int e = 0; e < 4 * SUB; ++e)
-                values[e] = M::value(zf[st], e) * left_weight[C - n + st * M::STEP + e / 4 * 16 + 4 * quad + e % 4];
-            Frag wf[PARTS];
-            M::template split<PARTS>(values, wf);
-#pragma unroll
-            for (int kt = 0; kt < K / 16; ++kt) {
-                const Frag yf = M::along_columns(ys, KPITCH, st * M::STEP, 16 * kt);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) s[kt] = M::multiply(yf, wf[p], s[kt]);
-            }
-        }
-        if constexpr (OUTPUT) {
-            __syncthreads();
         } else {
-            float worst = 0.0f;
-            if (t0 + C >= last)
 #pragma unroll
-                for (int kt = 0; kt < K / 16; ++kt)
+            for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) worst = fmaf(s[kt][i], 0.0f, worst);
-            if (__syncthreads_or(!(worst == 0.0f))) {
-                by_token = true;
+                for (int nv = 0; nv < NV; ++nv) zf[st][nv] = M::template along_columns<false>(zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * nv);
+        }
+        if (!again) {
+            // the state behind the chunk.  l^n = 1 + (l^n - 1): the power itself, rounded, would drift over many chunks where little decays
+            const float shrink = expm1f((float)n * g);
+            constexpr int BLOCKS = KT / YB, ALL = STEPS * BLOCKS;
+            Frag yf[2][YB], wf[2][NV][PARTS];
+            auto y_block = [&](int block, Frag (&to)[YB]) {
 #pragma unroll
-                for (int kt = 0; kt < K / 16; ++kt) s[kt] = f4{};
-                yl = TileLoader<T, E, C, K, THREADS>(y + first * ystep, ystep, A.rows);
-                zl = TileLoader<T, E, C, VT, THREADS>(z + first * zstep, zstep, width);
-                t0 = first - C;
-                load(first);
+                for (int i = 0; i < YB; ++i) {
+                    const int kt = block % BLOCKS * YB + i;
+                    to[i] = M::template along_columns<true>(ys, YPITCH, block / BLOCKS * M::STEP, kt / SUB * M::STEP, kt % SUB);
+                }
+            };
+            auto z_step = [&](int st, Frag (&to)[NV][PARTS]) {
+                float weight[4 * SUB];
+#pragma unroll
+                for (int e = 0; e < 4 * SUB; ++e) weight[e] = left_weight[C - n + st * M::STEP + e / 4 * 16 + 4 * quad + e % 4];
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) {
+                    float values[4 * SUB];
+#pragma unroll
+                    for (int e = 0; e < 4 * SUB; ++e) values[e] = weight[e] * M::value(zf[st][nv], e);
+                    M::template split<PARTS>(values, to[nv]);
+                }
+            };
+            auto shrink_block = [&](int block) {
+#pragma unroll
+                for (int kt = block * YB; kt < (block + 1) * YB; ++kt)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[kt][nv][i] = fmaf(s[kt][nv][i], shrink, s[kt][nv][i]);
+            };
+            y_block(0, yf[0]);
+            shrink_block(0);
+            z_step(0, wf[0]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int block = 0; block < ALL; ++block) {
+                const int st = block / BLOCKS, k0 = block % BLOCKS * YB;
+                if (block + 1 < ALL) y_block(block + 1, yf[(block + 1) % 2]);
+                if (block + 1 < BLOCKS) shrink_block(block + 1);
+                if (block % BLOCKS == BLOCKS - 1 && st + 1 < STEPS) z_step(st + 1, wf[(st + 1) % 2]);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                        for (int i = 0; i < YB; ++i) s[k0 + i][nv] = M::multiply(yf[block % 2][i], wf[st % 2][nv][p], s[k0 + i][nv]);
+                interleave<YB * M::COLUMN_READS, PARTS * NV * YB * M::PRODUCTS>();
             }
         }
+        __syncthreads();
+        if (OUTPUT && spoilt) break;
+    }
+    if constexpr (!OUTPUT) {
+        float worst = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) worst = fmaf(s[kt][nv][i], 0.0f, worst);
+        if (__syncthreads_or(!(worst == 0.0f))) {
+            // the whole segment again, token by token
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) s[kt][nv] = f4{};
+            yl = TileLoader<T, E, C, K, THREADS>(y + first * ystep, ystep, A.rows);
+            zl = TileLoader<T, E, C, VT, THREADS>(z + first * zstep, zstep, width);
+            t0 = first - C;
+        }
+    } else if (t0 + C < last) {
+        // (loaded anew behind the chunk in LDS: its registers are wanted)
+        xl.back();
+        yl.back();
+        zl.back();
+    }
+    // token by token from here on: first, with output, the chunk in LDS for those who could not take it
+    int c = column;
+    asm volatile("" : "+v"(c));      // (nothing of this loop is worked out ahead of the other, which has no registers to keep it)
+    for (; t0 < last; t0 += C) {
+        const int n = last - t0 < C ? (int)(last - t0) : C;
+        if (t0 >= first && (!OUTPUT || again))
+            chunk_by_token<OUTPUT>(A, g, n, xs, XPITCH, ys, YPITCH, zs, ZPITCH, s, first_row, row_of, c, [&](int r, int nv, float value) {
+                if (quad == 0 && c + 16 * nv < width) o[(t0 + r) * ostep + c + 16 * nv] = from_float<O>(value);
+            });
+        again = true;
+        __syncthreads();
+        if (t0 + C >= last) break;
+        const int more = last - t0 - C < C ? (int)(last - t0 - C) : C;
+        load(t0 + C);
+        if (OUTPUT) xl.store(xs, XPITCH, more);
+        yl.store(ys, YPITCH, more);
+        zl.store(zs, ZPITCH, more);
+        __syncthreads();
     }
 
     if constexpr (OUTPUT) {
@@ -348,47 +484,49 @@ __global__ __launch_bounds__(4 * VT, K <= 128 ? 2 : 1) void sig_attention_chunk_
         }
         if (own || !A.state_out) return;
     }
-    float *to = (own ? at_segment : A.state_out + at_head * head_state) + 4 * quad * row_stride + (c0 + column) * column_stride;
-    int rows = column < width ? A.rows - 4 * quad : 0;
-    asm volatile("" : "+v"(rows));
 #pragma unroll
-    for (int kt = 0; kt < K / 16; ++kt)
+    for (int nv = 0; nv < NV; ++nv) {
+        float *to = (own ? at_segment : A.state_out + at_head * head_state) + first_row * row_stride + (c0 + c + 16 * nv) * column_stride;
+        int rows = c + 16 * nv < width ? A.rows - first_row : 0;
+        asm volatile("" : "+v"(rows));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (16 * kt + i < rows) to[(16 * kt + i) * row_stride] = s[kt][i];
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (row_of(kt) + i < rows) to[(row_of(kt) + i) * row_stride] = s[kt][nv][i];
+    }
 }
 
-// The instance for `G`: vt columns a workgroup
+// The instance for `G`: up to 64 nv columns a workgroup
 template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
-void launch_chunk_instance(const ChunkArgs &G, int vt, hipStream_t st)
+void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
 {
     const AttentionArgs &A = G.a;
-    const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((A.columns + vt - 1) / vt), (unsigned)G.segments);
-    auto go = [&](auto k) {
-        constexpr int K = decltype(k)::value;
-        constexpr int WIDE = K <= 128 ? 128 : 64;       // (registers)
-        if (vt == WIDE) sig_attention_chunk_kernel<T, O, E, C, K, WIDE, PARTS, OUTPUT><<<grid, 4 * WIDE, 0, st>>>(G);
-        else sig_attention_chunk_kernel<T, O, E, C, K, 64, PARTS, OUTPUT><<<grid, 256, 0, st>>>(G);
+    auto go = [&](auto k, auto n) {
+        constexpr int NV = decltype(n)::value;
+        const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((A.columns + 64 * NV - 1) / (64 * NV)), (unsigned)G.segments);
+        sig_attention_chunk_kernel<T, O, E, C, decltype(k)::value, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
-    if (A.rows <= 64) go(std::integral_constant<int, 64>());
-    else if (A.rows <= 128) go(std::integral_constant<int, 128>());
-    else if (A.rows <= 192) go(std::integral_constant<int, 192>());
-    else go(std::integral_constant<int, 256>());
+    constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
+    if (A.rows <= 64) nv == 2 ? go(Number<64>(), Number<2>()) : go(Number<64>(), Number<1>());
+    else if (A.rows <= 128) nv == 2 ? go(Number<128>(), Number<WIDE>()) : go(Number<128>(), Number<1>());
+    else if (A.rows <= 192) go(Number<192>(), Number<1>());
+    else go(Number<256>(), Number<1>());
 }
 
 template <typename T, typename E, int C>
-void launch_chunk(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st)
+void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st)
 {
     constexpr int PARTS = Matrix<E>::EXACT;
-    if (!output) launch_chunk_instance<T, T, E, C, PARTS, false>(G, vt, st);
-    else if (partial) launch_chunk_instance<T, float, E, C, PARTS, true>(G, vt, st);
-    else launch_chunk_instance<T, T, E, C, PARTS, true>(G, vt, st);
+    if (!output) launch_chunk_instance<T, T, E, C, PARTS, false>(G, nv, st);
+    else if (partial) launch_chunk_instance<T, float, E, C, PARTS, true>(G, nv, st);
+    else launch_chunk_instance<T, T, E, C, PARTS, true>(G, nv, st);
 }
 
 // one for each type of the operands, in a file of its own; partial: float32 output
-void launch_chunk_f32(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
-void launch_chunk_bf16(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
-void launch_chunk_f16(const ChunkArgs &G, int vt, bool output, bool partial, hipStream_t st);
+void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
 
 }  // namespace sig
 #endif

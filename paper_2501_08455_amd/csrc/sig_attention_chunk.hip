@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kThreads) void sig_attention_join_kernel(ChunkArgs 
 }
 
 struct Cut {
-    int columns, segments;      // columns of the state a workgroup, workgroups along time
+    int nv, segments;      // 64 nv columns of the state a workgroup, workgroups along time
     int64_t segment_tokens;
 };
 
@@ -38,8 +38,8 @@ Cut cut_of(const AttentionArgs &A, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
     Cut cut;
-    cut.columns = A.columns > 64 && A.rows <= 128 ? 128 : 64;
-    const int64_t workgroups = A.B * A.heads * ((A.columns + cut.columns - 1) / cut.columns), chunks = (A.T + chunk - 1) / chunk;
+    cut.nv = A.columns > 64 && A.rows <= 128 ? 2 : 1;
+    const int64_t workgroups = A.B * A.heads * ((A.columns + 64 * cut.nv - 1) / (64 * cut.nv)), chunks = (A.T + chunk - 1) / chunk;
     int64_t segments = workgroups >= cus ? 1 : 2 * cus / workgroups;
     if (segments > chunks / 4) segments = chunks / 4 > 1 ? chunks / 4 : 1;
     const int64_t each = (chunks + segments - 1) / segments;
@@ -65,11 +65,11 @@ hipError_t launch_attention_chunk(const AttentionArgs &A, int type, int out_type
     const auto launch = type == SIG_BF16 ? launch_chunk_bf16 : type == SIG_F16 ? launch_chunk_f16 : launch_chunk_f32;
     const bool partial = out_type != type;
     if (cut.segments > 1) {
-        launch(G, cut.columns, false, partial, st);
+        launch(G, cut.nv, false, partial, st);
         const int64_t values = A.B * A.heads * A.rows * A.columns;
         sig_attention_join_kernel<<<(unsigned)((values + kThreads - 1) / kThreads), kThreads, 0, st>>>(G);
     }
-    launch(G, cut.columns, true, partial, st);
+    launch(G, cut.nv, true, partial, st);
     return hipGetLastError();
 }
 

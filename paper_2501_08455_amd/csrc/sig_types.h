@@ -43,5 +43,14 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[N];
 };
 
+// *to = values, as one store (member by member the compiler may take several)
+template <typename T, int N>
+__device__ inline void store_pack(T *to, const Pack<T, N> &values)
+{
+    using Words = __attribute__((ext_vector_type(N * sizeof(T) / 4))) unsigned;
+    struct __attribute__((packed, aligned(sizeof(T)))) Whole { Words words; };
+    ((Whole *)to)->words = __builtin_bit_cast(Words, values);
+}
+
 }  // namespace sig
 #endif
