@@ -24,18 +24,6 @@ constexpr int64_t kPiece = 8192;        // values of a piece of a longer row
 constexpr int kWidest = 1024;           // workgroups that keep sums of the weights' gradients
 
 template <typename T, int N>
-__device__ inline Pack<T, N> load_pack(const T *p)
-{
-    if constexpr (N == 1) {
-        return Pack<T, 1>{{*p}};
-    } else {
-        using Words = __attribute__((ext_vector_type(N * sizeof(T) / 4))) unsigned;
-        struct __attribute__((packed, aligned(sizeof(T)))) Whole { Words words; };
-        return __builtin_bit_cast(Pack<T, N>, ((const Whole *)p)->words);
-    }
-}
-
-template <typename T, int N>
 __device__ inline void widen(const Pack<T, N> &pack, float (&v)[N])
 {
 #pragma unroll
@@ -54,8 +42,7 @@ __device__ inline void store_values(T *p, const float (&v)[N])
     Pack<T, N> pack;
 #pragma unroll
     for (int i = 0; i < N; ++i) pack.v[i] = from_float<T>(v[i]);
-    if constexpr (N == 1) *p = pack.v[0];
-    else store_pack(p, pack);
+    store_pack(p, pack);
 }
 
 // weights, or `otherwise` where there are none

@@ -43,13 +43,25 @@ struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[N];
 };
 
-// *to = values, as one store (member by member the compiler may take several)
+// a pack as the words that it is moved in
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) PackWords {
+    __attribute__((ext_vector_type(N * sizeof(T) / 4))) unsigned words;
+};
+
+// as one load or store (member by member the compiler may take several)
+template <typename T, int N>
+__device__ inline Pack<T, N> load_pack(const T *from)
+{
+    if constexpr (N * sizeof(T) < 4) return *(const Pack<T, N> *)from;
+    else return __builtin_bit_cast(Pack<T, N>, ((const PackWords<T, N> *)from)->words);
+}
+
 template <typename T, int N>
 __device__ inline void store_pack(T *to, const Pack<T, N> &values)
 {
-    using Words = __attribute__((ext_vector_type(N * sizeof(T) / 4))) unsigned;
-    struct __attribute__((packed, aligned(sizeof(T)))) Whole { Words words; };
-    ((Whole *)to)->words = __builtin_bit_cast(Words, values);
+    if constexpr (N * sizeof(T) < 4) *(Pack<T, N> *)to = values;
+    else ((PackWords<T, N> *)to)->words = __builtin_bit_cast(decltype(PackWords<T, N>::words), values);
 }
 
 }  // namespace sig
