@@ -157,7 +157,8 @@ __device__ inline void interleave()
 }
 
 // T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; NV: tiles of 16 columns a wavefront; PARTS: fragments that
-// the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits); OUTPUT: 0 for launches that only work out the
+// the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits; two of bfloat16, sixteen digits, where nothing but outputs in
+// bfloat16 depends on the state: a hundred times finer than they are); OUTPUT: 0 for launches that only work out the
 // segments' own states
 template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT>
 __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
@@ -257,10 +258,7 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
         if constexpr (OUTPUT) {
             // this wavefront's tiles of the triangle: tokens 16 m + line against 16 j + 4 quad + 0..3
             for (int tile = wave; tile < MT * (MT + 1) / 2; tile += WAVES) {
-                int m = 0;
-#pragma unroll
-                for (int i = 1; i < MT; ++i) m += tile >= i * (i + 1) / 2;
-                const int j = tile - m * (m + 1) / 2;
+                const int m = (int)(0x3333222110ull >> 4 * tile & 15), j = tile - m * (m + 1) / 2;
                 f4 dots = {};
                 float weight[4];
 #pragma unroll
@@ -514,19 +512,20 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
     else go(Number<256>(), Number<1>());
 }
 
+// exact: all digits of the state (where it is a result), else sixteen (where only outputs of the operands' type depend on it)
 template <typename T, typename E, int C>
-void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st)
+void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st)
 {
-    constexpr int PARTS = Matrix<E>::EXACT;
-    if (!output) launch_chunk_instance<T, T, E, C, PARTS, false>(G, nv, st);
-    else if (partial) launch_chunk_instance<T, float, E, C, PARTS, true>(G, nv, st);
-    else launch_chunk_instance<T, T, E, C, PARTS, true>(G, nv, st);
+    constexpr int EXACT = Matrix<E>::EXACT, SHORT = EXACT < 2 ? EXACT : 2;
+    if (!output) exact ? launch_chunk_instance<T, T, E, C, EXACT, false>(G, nv, st) : launch_chunk_instance<T, T, E, C, SHORT, false>(G, nv, st);
+    else if (partial) exact ? launch_chunk_instance<T, float, E, C, EXACT, true>(G, nv, st) : launch_chunk_instance<T, float, E, C, SHORT, true>(G, nv, st);
+    else exact ? launch_chunk_instance<T, T, E, C, EXACT, true>(G, nv, st) : launch_chunk_instance<T, T, E, C, SHORT, true>(G, nv, st);
 }
 
 // one for each type of the operands, in a file of its own; partial: float32 output
-void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
-void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
-void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
+void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
+void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
 
 }  // namespace sig
 #endif

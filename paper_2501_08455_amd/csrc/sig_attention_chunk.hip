@@ -63,13 +63,13 @@ hipError_t launch_attention_chunk(const AttentionArgs &A, int type, int out_type
     const Cut cut = cut_of(A, type, cus);
     const ChunkArgs G = {A, cut.segment_tokens, cut.segments, scratch};
     const auto launch = type == SIG_BF16 ? launch_chunk_bf16 : type == SIG_F16 ? launch_chunk_f16 : launch_chunk_f32;
-    const bool partial = out_type != type;
+    const bool partial = out_type != type, exact = A.exact;
     if (cut.segments > 1) {
-        launch(G, cut.nv, false, partial, st);
+        launch(G, cut.nv, false, partial, exact, st);
         const int64_t values = A.B * A.heads * A.rows * A.columns;
         sig_attention_join_kernel<<<(unsigned)((values + kThreads - 1) / kThreads), kThreads, 0, st>>>(G);
     }
-    launch(G, cut.nv, true, partial, st);
+    launch(G, cut.nv, true, partial, exact, st);
     return hipGetLastError();
 }
 
