@@ -44,9 +44,10 @@ __device__ inline int64_t attention_length(const AttentionArgs &A, int64_t b)
 // one token after the other
 hipError_t launch_attention_recurrent(const AttentionArgs &A, int type, int out_type, hipStream_t st);
 
-// in chunks (sig_attention_chunk.h): floats of scratch that the launches need, and the launches
-int64_t attention_chunk_scratch_floats(const AttentionArgs &A, int type, int cus);
-hipError_t launch_attention_chunk(const AttentionArgs &A, int type, int out_type, float *scratch, int cus, hipStream_t st);
+// Passes over the same tokens in chunks (sig_attention_chunk.h), together where they hold states of the same size: floats of scratch that
+// the launches need, and the launches
+int64_t attention_chunk_scratch_floats(const AttentionArgs *a, int passes, int type, int cus);
+hipError_t launch_attention_chunk(const AttentionArgs *a, int passes, int type, int out_type, float *scratch, int cus, hipStream_t st);
 
 }  // namespace sig
 #endif

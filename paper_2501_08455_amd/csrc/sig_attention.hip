@@ -64,11 +64,17 @@ AttentionArgs pass(const sig_attention_t &s, const float *log_decay, const int64
 // Up to this many tokens go one after the other: a chunk's products cost as much for one token as for all of it
 constexpr int kRecurrentTokens = 16;
 
-int64_t scratch_floats(const AttentionArgs &A, int type, int cus) { return A.T > kRecurrentTokens ? attention_chunk_scratch_floats(A, type, cus) : 0; }
-
-hipError_t launch(const AttentionArgs &A, int type, int out_type, float *scratch, int cus, hipStream_t st)
+int64_t scratch_floats(const AttentionArgs *a, int passes, int type, int cus)
 {
-    return A.T > kRecurrentTokens ? launch_attention_chunk(A, type, out_type, scratch, cus, st) : launch_attention_recurrent(A, type, out_type, st);
+    return a[0].T > kRecurrentTokens ? attention_chunk_scratch_floats(a, passes, type, cus) : 0;
+}
+
+hipError_t launch(const AttentionArgs *a, int passes, int type, int out_type, float *scratch, int cus, hipStream_t st)
+{
+    if (a[0].T > kRecurrentTokens) return launch_attention_chunk(a, passes, type, out_type, scratch, cus, st);
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < passes && e == hipSuccess; ++i) e = launch_attention_recurrent(a[i], type, out_type, st);
+    return e;
 }
 
 // the state of `A`, kept [key][value] where its rows are keys, else read as the transpose
@@ -105,11 +111,11 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     const hipStream_t st = (hipStream_t)hip_stream;
     Scratch scratch;
     float *work = nullptr;
-    if (const int64_t floats = scratch_floats(A, s.type, ctx->num_cu)) {
+    if (const int64_t floats = scratch_floats(&A, 1, s.type, ctx->num_cu)) {
         const int got = scratch.get(ctx, (size_t)floats * sizeof(float), st, &work);
         if (got != SIG_OK) return got;
     }
-    return launch(A, s.type, s.type, work, ctx->num_cu, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+    return launch(&A, 1, s.type, s.type, work, ctx->num_cu, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
@@ -126,19 +132,25 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     int64_t gs[3];
     contiguous(gs, s, s.heads, V);
 
-    // the three passes; shared keys' and values' gradients go to scratch, heads apart, and are added up from there
-    AttentionArgs Q = pass(s, log_decay, lengths, V, K), K_ = Q, V_ = pass(s, log_decay, lengths, K, V);
+    // the three passes: the gradients of q, k and v
+    AttentionArgs a[3];
+    AttentionArgs &Q = a[0], &K_ = a[1], &V_ = a[2];
+    Q = pass(s, log_decay, lengths, V, K);
     operand(&Q.x, Q.xs, &Q.x_group, grad_out, gs, 1);
     operand(&Q.y, Q.ys, &Q.y_group, v, s.v_strides, group);
     operand(&Q.z, Q.zs, &Q.z_group, k, s.k_strides, group);
     Q.out_scale = s.scale;
     from_state(Q, state, nullptr, true);
+    Q.o = grad_q;
+    contiguous(Q.os, s, s.heads, K);
+    K_ = pass(s, log_decay, lengths, V, K);
     operand(&K_.x, K_.xs, &K_.x_group, v, s.v_strides, group);
     operand(&K_.y, K_.ys, &K_.y_group, grad_out, gs, 1);
     operand(&K_.z, K_.zs, &K_.z_group, q, s.q_strides, 1);
     K_.update_scale = s.scale;
     K_.reversed = 1;
     from_state(K_, grad_state, nullptr, true);
+    V_ = pass(s, log_decay, lengths, K, V);
     operand(&V_.x, V_.xs, &V_.x_group, k, s.k_strides, group);
     operand(&V_.y, V_.ys, &V_.y_group, q, s.q_strides, 1);
     operand(&V_.z, V_.zs, &V_.z_group, grad_out, gs, 1);
@@ -146,42 +158,45 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     V_.reversed = 1;
     V_.exact = grad_initial != nullptr;
     from_state(V_, grad_state, grad_initial, false);
-
+    K_.o = grad_k;
+    contiguous(K_.os, s, s.heads, K);
+    V_.o = grad_v;
+    contiguous(V_.os, s, s.heads, V);
     const int cus = ctx->num_cu;
-    int64_t states = 0;
-    for (const AttentionArgs *A : {&Q, &K_, &V_}) {
-        const int64_t floats = scratch_floats(*A, s.type, cus);
+    auto status = [](hipError_t e) { return e == hipSuccess ? SIG_OK : SIG_ERR_HIP; };
+    if (s.T == 0) return status(launch(&V_, 1, s.type, s.type, nullptr, cus, st));      // (the state's gradient alone)
+
+    // shared keys' and values' gradients go to scratch first, heads apart, and are added up from there
+    const bool shared = group > 1;
+    int64_t states = scratch_floats(a, shared ? 1 : 3, s.type, cus);
+    if (shared) {
+        const int64_t floats = scratch_floats(a + 1, 2, s.type, cus);
         if (floats > states) states = floats;
     }
-    const int64_t parts = group > 1 ? s.B * s.T * s.heads * (K > V ? K : V) : 0;
+    const int64_t parts = shared ? s.B * s.T * s.heads : 0;
     Scratch scratch;
     float *work = nullptr;
     if (states + parts > 0) {
-        rc = scratch.get(ctx, (size_t)(states + parts) * sizeof(float), st, &work);
+        rc = scratch.get(ctx, (size_t)(states + parts * (K + V)) * sizeof(float), st, &work);
         if (rc != SIG_OK) return rc;
     }
-    float *part = group > 1 ? work + states : nullptr;
-    auto shared_pass = [&](AttentionArgs &A, void *grad, int dim) {
-        A.o = part ? (void *)part : grad;
-        contiguous(A.os, s, s.heads, dim);
-        hipError_t e = launch(A, s.type, part ? (int)SIG_F32 : s.type, work, cus, st);
+    if (!shared) return status(launch(a, 3, s.type, s.type, work, cus, st));
+    float *part_k = work + states, *part_v = part_k + parts * K;
+    K_.o = part_k;
+    V_.o = part_v;
+    hipError_t e = launch(a, 1, s.type, s.type, work, cus, st);
+    if (e == hipSuccess) e = launch(a + 1, 2, s.type, SIG_F32, work, cus, st);
+    auto add_up = [&](const float *part, void *grad, int dim) {
         const int64_t values = s.B * s.T * s.shared_heads * dim, blocks = (values + kThreads - 1) / kThreads;
-        if (e != hipSuccess || !part || values == 0) return e;
         with_type(s.type, [&](auto t) {
             using E = typename decltype(t)::type;
             sig_attention_share_kernel<E><<<(unsigned)(blocks < 65536 ? blocks : 65536), kThreads, 0, st>>>(part, (E *)grad, values, group, dim);
         });
         return hipGetLastError();
     };
-    hipError_t e = hipSuccess;
-    if (s.T > 0) {
-        Q.o = grad_q;
-        contiguous(Q.os, s, s.heads, K);
-        e = launch(Q, s.type, s.type, work, cus, st);
-        if (e == hipSuccess) e = shared_pass(K_, grad_k, K);
-    }
-    if (e == hipSuccess) e = shared_pass(V_, grad_v, V);
-    return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+    if (e == hipSuccess) e = add_up(part_k, grad_k, K);
+    if (e == hipSuccess) e = add_up(part_v, grad_v, V);
+    return status(e);
 }
 
 }  // extern "C"

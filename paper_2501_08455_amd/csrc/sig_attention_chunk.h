@@ -29,12 +29,16 @@ constexpr int kChunkThreads = 256;
 template <int N>
 using Number = std::integral_constant<int, N>;
 
-// The pieces along time that different workgroups take (A.T tokens from place `segment * segment_tokens` on)
+constexpr int kMostPasses = 3;
+
+// Passes of the same batch, heads and rows that one launch takes, and the segments along time that different workgroups take: A.T
+// tokens from place segment * segment_tokens on
 struct ChunkArgs {
-    AttentionArgs a;
+    AttentionArgs a[kMostPasses];
+    int passes, segments;
     int64_t segment_tokens;     // a multiple of the chunk; at least T where there is one segment
-    int segments;
-    float *states;              // [segments][B][heads][rows][columns]: state-only launches write a segment's own, others read what lies before it
+    int64_t states_apart;       // floats of `states` between passes
+    float *states;              // [passes][segments - 1][B][heads][rows][columns]: segments' own states, then what lies before the next segment
 };
 
 // Tiles of C tokens x W values, one after the other: global memory -> registers -> LDS (E), zeros where there is nothing.  A thread
@@ -170,7 +174,9 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, KT = K / 16, SUB = M::SUB;
     constexpr int SPLIT = SUB == 2 ? 2 : 1;       // bfloat16 fragments of the state and of the triangle: 16 digits
     constexpr int YB = 4;                       // tiles of the state whose operands are loaded at once
-    const AttentionArgs &A = G.a;
+    const int pass = blockIdx.z % G.passes, segment = blockIdx.z / G.passes;
+    const AttentionArgs &A = G.a[pass];
+    if ((int)blockIdx.y * VT >= A.columns) return;
     __shared__ __attribute__((aligned(16))) E xs[OUTPUT ? C * XPITCH : 8], ys[C * YPITCH], zs[C * ZPITCH];
     __shared__ Frag triangle[OUTPUT ? MT * STEPS * SPLIT * 64 : 1];
     __shared__ int spoilt;                        // whether a wavefront has met what is not finite
@@ -182,8 +188,8 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     const int lane = threadIdx.x % 64, line = lane % 16, quad = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int c0 = blockIdx.y * VT, width = A.columns - c0, column = wave * 16 * NV + line;     // of the workgroup, and of the lane in it
-    const int64_t length = attention_length(A, b), first = (int64_t)blockIdx.z * G.segment_tokens;
-    const int64_t last = first + G.segment_tokens < length && (int)blockIdx.z + 1 < G.segments ? first + G.segment_tokens : length;
+    const int64_t length = attention_length(A, b), first = segment * G.segment_tokens;
+    const int64_t last = first + G.segment_tokens < length && segment + 1 < G.segments ? first + G.segment_tokens : length;
     const float g = A.log_decay[head];
     if (threadIdx.x == 0) spoilt = 0;
     const auto power = [&](int i) { return i == 0 ? 1.0f : expf((float)i * g); };
@@ -208,17 +214,19 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     const auto row_of = [](int kt) { return kt / SUB * M::STEP + 4 * (kt % SUB); };
     f4 s[KT][NV];
     const int64_t head_state = (int64_t)A.rows * A.columns, at_head = (int64_t)b * A.heads + head;
-    const bool own = !OUTPUT || G.segments > 1;   // states in scratch
-    const int64_t row_stride = own ? A.columns : A.row_stride, column_stride = own ? 1 : A.column_stride;
-    float *at_segment = G.states + ((int64_t)blockIdx.z * A.B * A.heads + at_head) * head_state;
+    // A segment's state is kept behind it, and what lies before it where the last one's was.
+    float *kept = G.states + pass * G.states_apart + (segment * A.B * A.heads + at_head) * head_state;
+    const float *from = segment > 0 ? kept - A.B * A.heads * head_state : A.state ? A.state + at_head * head_state : nullptr;
+    float *state_to = !OUTPUT ? kept : segment + 1 == G.segments && A.state_out ? A.state_out + at_head * head_state : nullptr;
 #pragma unroll
     for (int nv = 0; nv < NV; ++nv) {
         if constexpr (!OUTPUT) {
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) s[kt][nv] = f4{};
         } else {
-            const float *at = (own ? at_segment : A.state + at_head * head_state) + first_row * row_stride + (c0 + column + 16 * nv) * column_stride;
-            int rows = (own || A.state) && column + 16 * nv < width ? A.rows - first_row : 0;
+            const int64_t row_stride = segment > 0 ? A.columns : A.row_stride, column_stride = segment > 0 ? 1 : A.column_stride;
+            const float *at = from + first_row * row_stride + (c0 + column + 16 * nv) * column_stride;
+            int rows = from && column + 16 * nv < width ? A.rows - first_row : 0;
             asm volatile("" : "+v"(rows));
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
@@ -474,17 +482,18 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     }
 
     if constexpr (OUTPUT) {
-        if ((int)blockIdx.z + 1 == G.segments) {
+        if (segment + 1 == G.segments) {
             // behind the length
             O *rest = (O *)A.o + b * A.os[0] + head * A.os[2] + c0;
             const int left = width < VT ? width : VT;
             for (int64_t i = threadIdx.x; i < (A.T - length) * left; i += THREADS) rest[(length + i / left) * A.os[1] + i % left] = from_float<O>(0.0f);
         }
-        if (own || !A.state_out) return;
+        if (!state_to) return;
     }
+    const int64_t row_stride = OUTPUT ? A.row_stride : A.columns, column_stride = OUTPUT ? A.column_stride : 1;
 #pragma unroll
     for (int nv = 0; nv < NV; ++nv) {
-        float *to = (own ? at_segment : A.state_out + at_head * head_state) + first_row * row_stride + (c0 + c + 16 * nv) * column_stride;
+        float *to = state_to + first_row * row_stride + (c0 + c + 16 * nv) * column_stride;
         int rows = c + 16 * nv < width ? A.rows - first_row : 0;
         asm volatile("" : "+v"(rows));
 #pragma unroll
@@ -495,21 +504,30 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     }
 }
 
+// rows of the state that an instance holds, for so many
+inline int chunk_rows(int rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : rows <= 192 ? 192 : 256; }
+
 // The instance for `G`: up to 64 nv columns a workgroup
 template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
 void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
 {
-    const AttentionArgs &A = G.a;
+    const AttentionArgs &A = G.a[0];
+    int columns = 0;
+    for (int i = 0; i < G.passes; ++i) columns = G.a[i].columns > columns ? G.a[i].columns : columns;
     auto go = [&](auto k, auto n) {
         constexpr int NV = decltype(n)::value;
-        const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((A.columns + 64 * NV - 1) / (64 * NV)), (unsigned)G.segments);
+        const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((columns + 64 * NV - 1) / (64 * NV)),
+                        (unsigned)(G.passes * (OUTPUT ? G.segments : G.segments - 1)));
         sig_attention_chunk_kernel<T, O, E, C, decltype(k)::value, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
     constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
-    if (A.rows <= 64) nv == 2 ? go(Number<64>(), Number<2>()) : go(Number<64>(), Number<1>());
-    else if (A.rows <= 128) nv == 2 ? go(Number<128>(), Number<WIDE>()) : go(Number<128>(), Number<1>());
-    else if (A.rows <= 192) go(Number<192>(), Number<1>());
-    else go(Number<256>(), Number<1>());
+    switch (chunk_rows(A.rows)) {
+    case 64: nv == 2 ? go(Number<64>(), Number<2>()) : go(Number<64>(), Number<1>());
+        break;
+    case 128: nv == 2 ? go(Number<128>(), Number<WIDE>()) : go(Number<128>(), Number<1>()); break;
+    case 192: go(Number<192>(), Number<1>()); break;
+    default: go(Number<256>(), Number<1>());
+    }
 }
 
 // exact: all digits of the state (where it is a result), else sixteen (where only outputs of the operands' type depend on it)

@@ -1,4 +1,4 @@
-// Linear attention in chunks: how a call is cut, and what joins the pieces of a sequence that different workgroups take.
+// Linear attention in chunks: how calls are cut, and what joins the segments of a sequence that different workgroups take.
 #include "sig_attention_chunk.h"
 
 using namespace sig;
@@ -7,26 +7,32 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// states[segment] from each segment's own state to what lies before it; the state behind the last one to A.state_out
+// Each segment's own state -> what lies before the next one
 __global__ __launch_bounds__(kThreads) void sig_attention_join_kernel(ChunkArgs G)
 {
-    const AttentionArgs &A = G.a;
+    constexpr int AHEAD = 8;      // loads in flight
+    const AttentionArgs &A = G.a[blockIdx.y];
     const int64_t size = (int64_t)A.rows * A.columns, all = A.B * A.heads * size;
     const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (at >= all) return;
     const int64_t at_head = at / size, row = at % size / A.columns, column = at % A.columns;
-    const int64_t place = at_head * size + row * A.row_stride + column * A.column_stride;
     const int64_t length = attention_length(A, at_head / A.heads);
-    const float g = A.log_decay[at_head % A.heads];
-    float s = A.state ? A.state[place] : 0.0f;
-    for (int i = 0; i < G.segments; ++i) {
-        int64_t n = length - i * G.segment_tokens;
-        if (n > G.segment_tokens && i + 1 < G.segments) n = G.segment_tokens;
-        const float own = G.states[i * all + at];
-        G.states[i * all + at] = s;
-        if (n > 0) s = fmaf(s, expm1f((float)n * g), s) + own;
+    const float g = A.log_decay[at_head % A.heads], whole = expm1f((float)G.segment_tokens * g);
+    float *states = G.states + blockIdx.y * G.states_apart + at;
+    float s = A.state ? A.state[at_head * size + row * A.row_stride + column * A.column_stride] : 0.0f;
+    for (int first = 0; first < G.segments - 1; first += AHEAD) {
+        float own[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) own[i] = first + i < G.segments - 1 ? states[(first + i) * all] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (first + i >= G.segments - 1) break;
+            const int64_t n = length - (first + i) * G.segment_tokens;
+            if (n >= G.segment_tokens) s = fmaf(s, whole, s) + own[i];
+            else if (n > 0) s = fmaf(s, expm1f((float)n * g), s) + own[i];
+            states[(first + i) * all] = s;
+        }
     }
-    if (A.state_out) A.state_out[place] = s;
 }
 
 struct Cut {
@@ -34,43 +40,87 @@ struct Cut {
     int64_t segment_tokens;
 };
 
-Cut cut_of(const AttentionArgs &A, int type, int cus)
+// How many columns a workgroup takes and how many workgroups share a sequence, measured (us, forward; gradient):
+//   bf16, 128 x 128, 128 heads     one segment of 128 columns   of 64 columns   four segments of 128 columns
+//     4,096 tokens                 325; 421                     277; 521        222; 556
+//     1,024 tokens                 81; 107                      62; 123         82; 195
+//   f32, 128 x 128, 128 heads, 1,024 tokens   198; 353          129; 328        164; 438
+// Workgroups of 128 columns, which share the operands' loads and the pairs of a chunk, where they are more than the units (float32, bound by
+// its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that, and long sequences of
+// less than two a unit, are cut along time, which costs a second read of y and z, the segments' states and two more launches
+// (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64
+// segments 355, 48, 40 and 49).
+Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
-    Cut cut;
-    cut.nv = A.columns > 64 && A.rows <= 128 ? 2 : 1;
-    const int64_t workgroups = A.B * A.heads * ((A.columns + 64 * cut.nv - 1) / (64 * cut.nv)), chunks = (A.T + chunk - 1) / chunk;
-    int64_t segments = workgroups >= cus ? 1 : 2 * cus / workgroups;
-    if (segments > chunks / 4) segments = chunks / 4 > 1 ? chunks / 4 : 1;
-    const int64_t each = (chunks + segments - 1) / segments;
-    cut.segments = (int)((chunks + each - 1) / each);
-    cut.segment_tokens = each * chunk;
+    bool wide = false;
+    for (int i = 0; i < passes; ++i) wide = wide || (a[i].columns > 64 && a[i].rows <= 128);      // (registers)
+    auto workgroups = [&](int nv) {
+        int64_t n = 0;
+        for (int i = 0; i < passes; ++i) n += a[i].B * a[i].heads * ((a[i].columns + 64 * nv - 1) / (64 * nv));
+        return n;
+    };
+    Cut cut = {wide && 4 * workgroups(2) >= (type == SIG_BF16 ? 5 : 8) * cus ? 2 : 1, 1, a[0].T};
+    const int64_t chunks = (a[0].T + chunk - 1) / chunk, n = workgroups(cut.nv);
+    if (4 * n < 3 * cus || (cut.nv == 1 && n < 2 * cus && chunks >= 48)) {
+        if (wide) cut.nv = 2;
+        int64_t segments = 2 * cus / workgroups(cut.nv);
+        if (segments > chunks / 4) segments = chunks / 4;
+        if (segments < 1) segments = 1;
+        const int64_t each = (chunks + segments - 1) / segments;
+        cut.segments = (int)((chunks + each - 1) / each);
+        cut.segment_tokens = each * chunk;
+    }
     return cut;
+}
+
+int64_t states_of(const AttentionArgs &A, const Cut &cut) { return (cut.segments - 1) * A.B * A.heads * A.rows * A.columns; }
+
+// passes that one launch takes together: as many of the next ones as hold the same rows
+int together(const AttentionArgs *a, int passes)
+{
+    int n = 1;
+    while (n < passes && n < kMostPasses && chunk_rows(a[n].rows) == chunk_rows(a[0].rows)) ++n;
+    return n;
 }
 
 }  // namespace
 
 namespace sig {
 
-int64_t attention_chunk_scratch_floats(const AttentionArgs &A, int type, int cus)
+int64_t attention_chunk_scratch_floats(const AttentionArgs *a, int passes, int type, int cus)
 {
-    const Cut cut = cut_of(A, type, cus);
-    return cut.segments > 1 ? cut.segments * A.B * A.heads * A.rows * A.columns : 0;
+    int64_t most = 0;
+    for (int first = 0, n; first < passes; first += n) {
+        n = together(a + first, passes - first);
+        const int64_t floats = n * states_of(a[first], cut_of(a + first, n, type, cus));
+        if (floats > most) most = floats;
+    }
+    return most;
 }
 
-hipError_t launch_attention_chunk(const AttentionArgs &A, int type, int out_type, float *scratch, int cus, hipStream_t st)
+hipError_t launch_attention_chunk(const AttentionArgs *a, int passes, int type, int out_type, float *scratch, int cus, hipStream_t st)
 {
-    const Cut cut = cut_of(A, type, cus);
-    const ChunkArgs G = {A, cut.segment_tokens, cut.segments, scratch};
     const auto launch = type == SIG_BF16 ? launch_chunk_bf16 : type == SIG_F16 ? launch_chunk_f16 : launch_chunk_f32;
-    const bool partial = out_type != type, exact = A.exact;
-    if (cut.segments > 1) {
-        launch(G, cut.nv, false, partial, exact, st);
-        const int64_t values = A.B * A.heads * A.rows * A.columns;
-        sig_attention_join_kernel<<<(unsigned)((values + kThreads - 1) / kThreads), kThreads, 0, st>>>(G);
+    const bool partial = out_type != type;
+    for (int first = 0, n; first < passes; first += n) {
+        n = together(a + first, passes - first);
+        const Cut cut = cut_of(a + first, n, type, cus);
+        ChunkArgs G = {{}, n, cut.segments, cut.segment_tokens, states_of(a[first], cut), scratch};
+        bool exact = false;
+        for (int i = 0; i < n; ++i) {
+            G.a[i] = a[first + i];
+            exact = exact || G.a[i].exact;
+        }
+        if (cut.segments > 1) {
+            launch(G, cut.nv, false, partial, exact, st);
+            const int64_t values = G.a[0].B * G.a[0].heads * G.a[0].rows * G.a[0].columns;
+            sig_attention_join_kernel<<<dim3((unsigned)((values + kThreads - 1) / kThreads), (unsigned)n), kThreads, 0, st>>>(G);
+        }
+        launch(G, cut.nv, true, partial, exact, st);
+        if (hipError_t e = hipGetLastError()) return e;
     }
-    launch(G, cut.nv, true, partial, exact, st);
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace sig
