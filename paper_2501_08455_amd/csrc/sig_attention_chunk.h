@@ -47,7 +47,7 @@ struct ChunkArgs {
 template <typename T, typename E, int C, int W, int THREADS>
 struct TileLoader {
     static constexpr int GROUP = 16 / (sizeof(T) > sizeof(E) ? sizeof(T) : sizeof(E));      // values of a load
-    static constexpr int WIDE = W <= 64 ? 64 : W <= 128 ? 128 : 256;                        // (threads beyond W load and drop)
+    static constexpr int WIDE = W <= 32 ? 32 : W <= 64 ? 64 : W <= 128 ? 128 : 256;         // (threads beyond W load and drop)
     static constexpr int ROWS = THREADS / (WIDE / GROUP), COUNT = C / ROWS;
     static_assert(THREADS % (WIDE / GROUP) == 0 && C % ROWS == 0);
     const T *p;          // of the next tile
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     constexpr int XPITCH = K + M::PAD, YPITCH = K + M::COLUMN_PAD, ZPITCH = VT + M::COLUMN_PAD;
     constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, KT = K / 16, SUB = M::SUB;
     constexpr int SPLIT = SUB == 2 ? 2 : 1;       // bfloat16 fragments of the state and of the triangle: 16 digits
-    constexpr int YB = 4;                       // tiles of the state whose operands are loaded at once
+    constexpr int YB = KT % 4 == 0 ? 4 : KT % 3 == 0 ? 3 : KT;      // tiles of the state whose operands are loaded at once
     const int pass = blockIdx.z % G.passes, segment = blockIdx.z / G.passes;
     const AttentionArgs &A = G.a[pass];
     if ((int)blockIdx.y * VT >= A.columns) return;
@@ -387,6 +387,7 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
             // the state behind the chunk.  l^n = 1 + (l^n - 1): the power itself, rounded, would drift over many chunks where little decays
             const float shrink = expm1f((float)n * g);
             constexpr int BLOCKS = KT / YB, ALL = STEPS * BLOCKS;
+            static_assert(KT % YB == 0);
             Frag yf[2][YB], wf[2][NV][PARTS];
             auto y_block = [&](int block, Frag (&to)[YB]) {
 #pragma unroll
@@ -504,8 +505,14 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     }
 }
 
-// rows of the state that an instance holds, for so many
-inline int chunk_rows(int rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : rows <= 192 ? 192 : 256; }
+// Rows of the state that an instance holds, for so many: whole steps of the products (32 rows, 16 of float32), since every
+// padded row costs its products.  Float32, 16 sequences of ragged length, 12 heads of 40 rows by 72 columns and the gradient:
+// 503 us with 48 and 80 rows, 692 us with 64 and 128.
+inline int chunk_rows(int rows, int type)
+{
+    const bool halves = type != SIG_BF16;
+    return rows <= 32 ? 32 : halves && rows <= 48 ? 48 : rows <= 64 ? 64 : halves && rows <= 80 ? 80 : rows <= 96 ? 96 : rows <= 128 ? 128 : rows <= 192 ? 192 : 256;
+}
 
 // The instance for `G`: up to 64 nv columns a workgroup
 template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
@@ -521,9 +528,13 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
         sig_attention_chunk_kernel<T, O, E, C, decltype(k)::value, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
     constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
-    switch (chunk_rows(A.rows)) {
-    case 64: nv == 2 ? go(Number<64>(), Number<2>()) : go(Number<64>(), Number<1>());
-        break;
+    auto either = [&](auto k) { nv == 2 ? go(k, Number<2>()) : go(k, Number<1>()); };
+    switch (chunk_rows(A.rows, sizeof(E) == 2 ? SIG_BF16 : SIG_F32)) {
+    case 32: either(Number<32>()); break;
+    case 48: if constexpr (sizeof(E) == 4) either(Number<48>()); break;
+    case 64: either(Number<64>()); break;
+    case 80: if constexpr (sizeof(E) == 4) either(Number<80>()); break;
+    case 96: nv == 2 ? go(Number<96>(), Number<WIDE>()) : go(Number<96>(), Number<1>()); break;
     case 128: nv == 2 ? go(Number<128>(), Number<WIDE>()) : go(Number<128>(), Number<1>()); break;
     case 192: go(Number<192>(), Number<1>()); break;
     default: go(Number<256>(), Number<1>());

@@ -77,10 +77,10 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 int64_t states_of(const AttentionArgs &A, const Cut &cut) { return (cut.segments - 1) * A.B * A.heads * A.rows * A.columns; }
 
 // passes that one launch takes together: as many of the next ones as hold the same rows
-int together(const AttentionArgs *a, int passes)
+int together(const AttentionArgs *a, int passes, int type)
 {
     int n = 1;
-    while (n < passes && n < kMostPasses && chunk_rows(a[n].rows) == chunk_rows(a[0].rows)) ++n;
+    while (n < passes && n < kMostPasses && chunk_rows(a[n].rows, type) == chunk_rows(a[0].rows, type)) ++n;
     return n;
 }
 
@@ -92,7 +92,7 @@ int64_t attention_chunk_scratch_floats(const AttentionArgs *a, int passes, int t
 {
     int64_t most = 0;
     for (int first = 0, n; first < passes; first += n) {
-        n = together(a + first, passes - first);
+        n = together(a + first, passes - first, type);
         const int64_t floats = n * states_of(a[first], cut_of(a + first, n, type, cus));
         if (floats > most) most = floats;
     }
@@ -104,7 +104,7 @@ hipError_t launch_attention_chunk(const AttentionArgs *a, int passes, int type, 
     const auto launch = type == SIG_BF16 ? launch_chunk_bf16 : type == SIG_F16 ? launch_chunk_f16 : launch_chunk_f32;
     const bool partial = out_type != type;
     for (int first = 0, n; first < passes; first += n) {
-        n = together(a + first, passes - first);
+        n = together(a + first, passes - first, type);
         const Cut cut = cut_of(a + first, n, type, cus);
         ChunkArgs G = {{}, n, cut.segments, cut.segment_tokens, states_of(a[first], cut), scratch};
         bool exact = false;
