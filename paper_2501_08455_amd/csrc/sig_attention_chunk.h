@@ -483,11 +483,17 @@ __global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention
     }
 
     if constexpr (OUTPUT) {
-        if (segment + 1 == G.segments) {
-            // behind the length
-            O *rest = (O *)A.o + b * A.os[0] + head * A.os[2] + c0;
-            const int left = width < VT ? width : VT;
-            for (int64_t i = threadIdx.x; i < (A.T - length) * left; i += THREADS) rest[(length + i / left) * A.os[1] + i % left] = from_float<O>(0.0f);
+        // behind the length: zeros, a segment's own (four columns a thread)
+        const int64_t end = segment + 1 < G.segments ? first + G.segment_tokens : A.T;
+        constexpr int LANES = VT / 4;
+        const int c4 = threadIdx.x % LANES * 4, left = width - c4;
+        for (int64_t t = (first > length ? first : length) + threadIdx.x / LANES; t < end; t += THREADS / LANES) {
+            O *rest = (O *)A.o + b * A.os[0] + head * A.os[2] + t * A.os[1] + c0 + c4;
+            if (left >= 4) {
+                store_pack(rest, Pack<O, 4>{});
+            } else {
+                for (int j = 0; j < left; ++j) rest[j] = from_float<O>(0.0f);
+            }
         }
         if (!state_to) return;
     }
