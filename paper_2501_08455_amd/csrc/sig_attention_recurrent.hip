@@ -119,7 +119,7 @@ namespace sig {
 
 hipError_t launch_attention_recurrent(const AttentionArgs &A, int type, int out_type, hipStream_t st)
 {
-    const bool packed = A.columns % 4 == 0 && A.column_stride == 1;
+    const bool packed = A.columns % 4 == 0 && (A.column_stride == 1 || (!A.state && !A.state_out));
     with_type(type, [&](auto tag) {
         using T = typename decltype(tag)::type;
         if (out_type == type) packed ? launch<T, T, 4>(A, st) : launch<T, T, 1>(A, st);
