@@ -11,15 +11,26 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostDim = 256;
 
-// out[token][shared head][.] = sum over the heads of a shared head of part[token][head][.], in their order
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sig_attention_share_kernel(const float *part, T *out, int64_t values, int group, int dim)
+// out[token][shared head][.] = sum over the heads of a shared head of part[token][head][.], in their order.  `lanes` threads (a power
+// of two) take a shared head's values, N each, up to four heads' loads at once.
+template <typename T, int N>
+__global__ __launch_bounds__(kThreads) void sig_attention_share_kernel(const float *part, T *out, int64_t rows, int group, int dim, int lanes)
 {
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < values; i += (int64_t)gridDim.x * kThreads) {
-        const float *p = part + i / dim * group * dim + i % dim;
-        float sum = 0.0f;
-        for (int h = 0; h < group; ++h) sum += p[(int64_t)h * dim];
-        out[i] = from_float<T>(sum);
+    const int at = threadIdx.x % lanes * N, apart = kThreads / lanes;
+    if (at >= dim) return;
+    for (int64_t row = (int64_t)blockIdx.x * apart + threadIdx.x / lanes; row < rows; row += (int64_t)gridDim.x * apart) {
+        const float *p = part + row * group * dim + at;
+        float sum[N] = {};
+#pragma unroll 4
+        for (int h = 0; h < group; ++h) {
+            const Pack<float, N> values = load_pack<float, N>(p + (int64_t)h * dim);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] += values.v[j];
+        }
+        Pack<T, N> result;
+#pragma unroll
+        for (int j = 0; j < N; ++j) result.v[j] = from_float<T>(sum[j]);
+        store_pack(out + row * dim + at, result);
     }
 }
 
@@ -187,10 +198,16 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     hipError_t e = launch(a, 1, s.type, s.type, work, cus, st);
     if (e == hipSuccess) e = launch(a + 1, 2, s.type, SIG_F32, work, cus, st);
     auto add_up = [&](const float *part, void *grad, int dim) {
-        const int64_t values = s.B * s.T * s.shared_heads * dim, blocks = (values + kThreads - 1) / kThreads;
+        const int64_t rows = s.B * s.T * s.shared_heads;
+        const int each = dim % 4 == 0 ? 4 : 1;
+        int lanes = 1;
+        while (lanes * each < dim) lanes *= 2;
+        const int64_t blocks = (rows + kThreads / lanes - 1) / (kThreads / lanes);
+        const unsigned grid = (unsigned)(blocks < 65536 ? blocks : 65536);
         with_type(s.type, [&](auto t) {
             using E = typename decltype(t)::type;
-            sig_attention_share_kernel<E><<<(unsigned)(blocks < 65536 ? blocks : 65536), kThreads, 0, st>>>(part, (E *)grad, values, group, dim);
+            if (each == 4) sig_attention_share_kernel<E, 4><<<grid, kThreads, 0, st>>>(part, (E *)grad, rows, group, dim, lanes);
+            else sig_attention_share_kernel<E, 1><<<grid, kThreads, 0, st>>>(part, (E *)grad, rows, group, dim, lanes);
         });
         return hipGetLastError();
     };
