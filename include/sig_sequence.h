@@ -28,7 +28,7 @@ enum sig_type { SIG_F32 = 0, SIG_BF16 = 1, SIG_F16 = 2 };
  *   y            DEVICE, [rows][width] of `type`, contiguous; must not overlap the inputs
  *   stats        DEVICE, float32 [rows][2], what sig_layer_norm_backward needs (mean, 1 / sqrt(...)); may be NULL
  * rows == 0 returns SIG_OK and launches nothing; width < 1, rows < 0 or a NaN or negative eps are SIG_ERR_INVALID.
- * NaN and Inf spoil their own row only.  Any width: rows of up to 8,192 values stay on chip between their
+ * NaN and Inf spoil their own row only.  Any width: rows of up to 16,384 values stay on chip between their
  * statistics and their output, longer ones are read twice and cut across workgroups (context scratch of about 2 floats for
  * every 8,192 values).
  */
