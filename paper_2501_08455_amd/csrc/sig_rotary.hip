@@ -15,6 +15,9 @@ constexpr int kThreads = 256;
 constexpr int kMostTokens = 16;      // of a workgroup
 constexpr int kTable = 2048;         // pairs of a workgroup's tokens
 
+template <typename T>
+constexpr int kGroup = 16 / sizeof(T);     // values of the widest load
+
 struct RotaryArgs {
     int64_t B, T, heads, dim, turned;
     int64_t xs[3], ys[3], ps[2];     // strides: batch, token, head
@@ -46,12 +49,15 @@ __device__ void turn(double position, double frequency, float *c, float *s)
     sincospif(2.0f * (float)(turns - rint(turns)), s, c);
 }
 
-// N neighbouring values, or N pairs of the half layout, are a unit; a line is a token's head, its turned units first, then those that are
-// copied (the last of them may be cut short).  `places` threads take a line.
+// N neighbouring values, or N pairs of the half layout, are a turned unit, M neighbouring values a copied one; a line is a token's head, its
+// turned units first.  The last copied unit ends with the line, if that means that it overlaps the one before, or, where there are fewer
+// than M values to copy, is those.  `places` threads take a line.  (Copied values in the turned units' width: 10 and 20 of 40 and 20 of 80 bfloat16
+// turned 416, 118 and 202 us, so 125, 92 and 100.)
 template <typename T, int N, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, RotaryArgs A)
 {
     constexpr int AT_ONCE = 4;       // lines a thread has in flight
+    constexpr int M = kGroup<T>;
     __shared__ float2 table[kTable];
     __shared__ int64_t from[kMostTokens], to[kMostTokens];
     const int half = (int)A.turned / 2, dim = (int)A.dim, turned = (int)A.turned, heads = (int)A.heads;
@@ -71,15 +77,17 @@ __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, 
         }
     }
     __syncthreads();
-    const int turned_units = INTERLEAVED ? turned / N : half / N, units = turned_units + (A.copy ? (dim - turned + N - 1) / N : 0);
+    const int turned_units = INTERLEAVED ? turned / N : half / N, units = turned_units + (A.copy ? (dim - turned + M - 1) / M : 0);
     const int line_step = kThreads / A.places, token_step = line_step / heads, head_step = line_step % heads;
     const int first_line = threadIdx.x / A.places;
     for (int unit = threadIdx.x % A.places; unit < units; unit += A.places) {
         const bool copied = unit >= turned_units;
-        const int at = copied ? turned + (unit - turned_units) * N : unit * N, left = dim - at;
+        const bool few = copied && dim - turned < M;
+        const int at = !copied ? unit * N : few ? turned : min(turned + (unit - turned_units) * M, dim - M);
         int token = first_line / heads, head = first_line % heads;
         while (token < tokens) {
             Pack<T, N> low[AT_ONCE], high[AT_ONCE];
+            Pack<T, M> same[N < M ? AT_ONCE : 1];      // (else `low`)
             const T *source[AT_ONCE];
             int tokens_of[AT_ONCE], heads_of[AT_ONCE];
 #pragma unroll
@@ -94,7 +102,9 @@ __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, 
                 }
                 if (tokens_of[k] >= tokens) continue;
                 source[k] = x + from[tokens_of[k]] + heads_of[k] * A.xs[2] + at;
-                if (left >= N) {
+                if (N < M && copied) {
+                    if (!few) same[N < M ? k : 0] = load_pack<T, M>(source[k]);
+                } else if (!few) {
                     low[k] = load_pack<T, N>(source[k]);
                     if (!INTERLEAVED && !copied) high[k] = load_pack<T, N>(source[k] + half);
                 }
@@ -103,10 +113,11 @@ __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, 
             for (int k = 0; k < AT_ONCE; ++k) {
                 if (tokens_of[k] >= tokens) continue;
                 T *p = y + to[tokens_of[k]] + heads_of[k] * A.ys[2] + at;
-                if (left < N) {
-                    for (int j = 0; j < left; ++j) p[j] = source[k][j];
+                if (few) {
+                    for (int j = 0; j < dim - turned; ++j) p[j] = source[k][j];
                 } else if (copied) {
-                    store_pack(p, low[k]);
+                    if constexpr (N < M) store_pack(p, same[k]);
+                    else store_pack(p, low[k]);
                 } else if constexpr (INTERLEAVED) {
                     const float2 *angle = table + tokens_of[k] * half + at / 2;
 #pragma unroll
@@ -160,14 +171,14 @@ extern "C" int sig_rotary(sig_ctx *ctx, const void *x, const int64_t *x_strides,
     with_type(type, [&](auto t) {
         using E = typename decltype(t)::type;
         auto go = [&](auto n) {
-            constexpr int N = decltype(n)::value;
-            const int64_t units = (interleaved ? turned / N : turned / 2 / N) + (A.copy ? (dim - turned + N - 1) / N : 0);
+            constexpr int N = decltype(n)::value, M = kGroup<E>;
+            const int64_t units = (interleaved ? turned / N : turned / 2 / N) + (A.copy ? (dim - turned + M - 1) / M : 0);
             while (A.places < units && A.places < kThreads) A.places *= 2;
             if (interleaved) sig_rotary_kernel<E, N, true><<<grid, kThreads, 0, (hipStream_t)hip_stream>>>((const E *)x, (E *)y, A);
             else sig_rotary_kernel<E, N, false><<<grid, kThreads, 0, (hipStream_t)hip_stream>>>((const E *)x, (E *)y, A);
         };
         // the widest loads that the turned components are a whole number of
-        constexpr int MOST = 16 / sizeof(E);
+        constexpr int MOST = kGroup<E>;
         const int64_t whole = interleaved ? turned : turned / 2;
         if (whole % MOST == 0) go(std::integral_constant<int, MOST>());
         else if (whole % (MOST / 2) == 0) go(std::integral_constant<int, MOST / 2>());
