@@ -164,8 +164,10 @@ __device__ inline void interleave()
 // the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits; two of bfloat16, sixteen digits, where nothing but outputs in
 // bfloat16 depends on the state: a hundred times finer than they are); OUTPUT: 0 for launches that only work out the
 // segments' own states
+// Two workgroups a unit, where LDS has room for them (with one, whose registers the compiler then spreads out: 192 rows of bfloat16 1.15 to 1.6
+// times as long, 192 and 256 rows of float32 1.1 to 1.3).
 template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT>
-__global__ __launch_bounds__(kChunkThreads, K <= 128 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
+__global__ __launch_bounds__(kChunkThreads, sizeof(E) == 4 || K <= 192 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
 {
     using M = Matrix<E>;
     using Frag = typename M::Frag;
