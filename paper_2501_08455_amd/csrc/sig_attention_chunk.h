@@ -167,7 +167,7 @@ __device__ inline void interleave()
 // Two workgroups a unit, where LDS has room for them (with one, whose registers the compiler then spreads out: 192 rows of bfloat16 1.15 to 1.6
 // times as long, 192 and 256 rows of float32 1.1 to 1.3).
 template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT>
-__global__ __launch_bounds__(kChunkThreads, sizeof(E) == 4 || K <= 192 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
+__global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
 {
     using M = Matrix<E>;
     using Frag = typename M::Frag;
@@ -533,7 +533,8 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
         constexpr int NV = decltype(n)::value;
         const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((columns + 64 * NV - 1) / (64 * NV)),
                         (unsigned)(G.passes * (OUTPUT ? G.segments : G.segments - 1)));
-        sig_attention_chunk_kernel<T, O, E, C, decltype(k)::value, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
+        constexpr int K = decltype(k)::value;
+        sig_attention_chunk_kernel<T, O, E, K == 256 ? 32 : C, K, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
     constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
     auto either = [&](auto k) { nv == 2 ? go(k, Number<2>()) : go(k, Number<1>()); };
