@@ -49,12 +49,16 @@ struct Cut {
 // its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that, and long sequences of
 // less than two a unit, are cut along time, which costs a second read of y and z, the segments' states and two more launches
 // (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64
-// segments 355, 48, 40 and 49).
+// segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of such workgroups at once: two, or three of small
+// states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two, 98 for three).
 Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
-    bool wide = false;
-    for (int i = 0; i < passes; ++i) wide = wide || (a[i].columns > 64 && a[i].rows <= 128);      // (registers)
+    bool wide = false, small = true;
+    for (int i = 0; i < passes; ++i) {
+        wide = wide || (a[i].columns > 64 && a[i].rows <= 128);      // (registers)
+        small = small && a[i].rows <= (type == SIG_BF16 ? 64 : 96);
+    }
     auto workgroups = [&](int nv) {
         int64_t n = 0;
         for (int i = 0; i < passes; ++i) n += a[i].B * a[i].heads * ((a[i].columns + 64 * nv - 1) / (64 * nv));
@@ -64,7 +68,7 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     const int64_t chunks = (a[0].T + chunk - 1) / chunk, n = workgroups(cut.nv);
     if (4 * n < 3 * cus || (cut.nv == 1 && n < 2 * cus && chunks >= 48)) {
         if (wide) cut.nv = 2;
-        int64_t segments = 2 * cus / workgroups(cut.nv);
+        int64_t segments = (small && cut.nv == 1 ? 3 : 2) * cus / workgroups(cut.nv);      // (that many workgroups a unit)
         if (segments > chunks / 4) segments = chunks / 4;
         if (segments < 1) segments = 1;
         const int64_t each = (chunks + segments - 1) / segments;
