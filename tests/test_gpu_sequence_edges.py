@@ -1,0 +1,120 @@
+"""The sequence-model operators at the sizes where their kernels change form, against the same 64-bit references and with the same tolerances as
+tests/test_gpu_sequence_ops.py."""
+import pytest
+import torch
+
+from paper_2501_08455_amd import autograd, binding
+from test_gpu_sequence_ops import (TYPES, assert_near, attention_inputs, attention_reference, check_attention, noise, norm_reference, rotary_reference, wide)
+
+gpu = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- layer norm: groups of lanes, one workgroup a row, pieces
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("width", [31, 32, 33, 127, 129, 256, 257, 511, 513, 1023, 2048, 2051, 8191, 8192, 8193, 8200, 12007, 16383, 16384, 16392, 24576])
+def test_layer_norm_where_its_form_changes(width, kind):
+    rows = 37 if width < 4096 else 5
+    x = (noise(rows, width, seed=50) + 0.25).to(kind).cuda().requires_grad_(True)
+    weight, bias = (1.0 + 0.3 * noise(width, seed=51)).float().cuda().requires_grad_(True), noise(width, seed=52).float().cuda().requires_grad_(True)
+    g = noise(rows, width, seed=53, kind=kind).cuda()
+    y = autograd.layer_norm(x, weight, bias)
+    grads = torch.autograd.grad(y, (x, weight, bias), g)
+    want = norm_reference(x, weight, bias, 1e-5, g)
+    assert_near(y, want[0], what="y")
+    assert_near(grads[0], want[1], size=want[4], what="grad x")
+    size = float(torch.sqrt((wide(g) ** 2).sum(0) * rows).norm())
+    assert_near(grads[1], want[2], size=size, what="grad weight")
+    assert_near(grads[2], want[3], size=size, what="grad bias")
+
+
+@gpu
+@pytest.mark.parametrize("width", [9001, 16384])
+def test_layer_norm_of_wide_rows_in_many_workgroups_turns(width):
+    """More rows than workgroups: the sums of the weights' gradients over several rows of one workgroup, and views with rows apart."""
+    rows = 2 * 256 * 4 + 3
+    base = noise(rows, width + 5, seed=54).float().cuda()
+    x, g = base[:, 2:2 + width], noise(1, width, seed=55).float().cuda().expand(rows, width)
+    weight = (1.0 + 0.3 * noise(width, seed=56)).float().cuda().requires_grad_(True)
+    x = x.detach().requires_grad_(True)
+    gx, gw = torch.autograd.grad(autograd.layer_norm(x, weight), (x, weight), g)
+    want = norm_reference(x, weight, None, 1e-5, g)
+    assert_near(gx, want[1], size=want[4])
+    assert_near(gw, want[2], size=float(torch.sqrt((wide(g) ** 2).sum(0) * rows).norm()))
+
+
+# ---------------------------------------------------------------- rotary: copied components in their own units
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,turned", [(40, 10), (40, 20), (80, 20), (64, 4), (16, 14), (13, 8), (9, 8), (8, 2), (17, 2), (23, 6), (24, 16), (3, 2), (100, 96)])
+def test_rotary_of_some_components(dim, turned, interleaved, kind):
+    x = noise(2, 19, 3, dim + 1, seed=57, kind=kind).cuda()[..., 1:]
+    f = (10000.0 ** (-torch.arange(turned // 2, dtype=torch.float64) / (turned // 2))).cuda()
+    p = torch.arange(19, device="cuda") * 31
+    y = binding.rotary(x, p, f, interleaved=interleaved)
+    assert_near(y, rotary_reference(x, p, f, interleaved, 1.0))
+    assert torch.equal(y[..., turned:], x[..., turned:])
+    room = torch.full((2, 19, 3, dim + 3), 7.0, dtype=kind, device="cuda")
+    binding.rotary(x, p, f, interleaved=interleaved, out=room[..., 1:1 + dim])
+    assert torch.equal(room[..., 1:1 + dim], y) and (room[..., 0] == 7.0).all() and (room[..., 1 + dim:] == 7.0).all()
+
+
+# ---------------------------------------------------------------- linear attention: rows and columns of its instances, chunks, segments
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows", [31, 32, 47, 48, 49, 63, 65, 79, 80, 81, 95, 96, 97, 129, 191, 193, 255])
+def test_linear_attention_of_every_number_of_rows(rows, kind):
+    check_attention(*attention_inputs(2, 70, 2, 2, rows, 24, kind, ragged=True, seed=60))
+    check_attention(*attention_inputs(1, 45, 2, 1, 24, rows, kind, seed=64))
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("T", [15, 16, 17, 31, 32, 33, 64, 95, 96, 97, 128, 129])
+@pytest.mark.parametrize("K,V", [(48, 96), (256, 20)])
+def test_linear_attention_around_chunks(K, V, T, kind):
+    check_attention(*attention_inputs(1, T, 2, 2, K, V, kind, seed=68))
+
+
+@gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K,V,G", [(16, 33, 2), (96, 72, 1), (130, 64, 2), (256, 16, 2)])
+def test_linear_attention_of_long_ragged_sequences(K, V, G, kind):
+    """Sequences that are cut along time, whose lengths end within a segment, before it and at its start: outputs, zeros behind the lengths
+    and states by cutting the sequence by hand."""
+    T = 3000
+    q, k, v, log_decay, state, _ = attention_inputs(4, T, 2, G, K, V, kind, seed=72)
+    lengths = torch.tensor([0, 1, 1537, T], device="cuda")
+    o, s = binding.linear_attention(q, k, v, log_decay, state=state, lengths=lengths, return_state=True)
+    for b, n in enumerate(lengths.tolist()):
+        assert not o[b, n:].any()
+        if n == 0:
+            assert torch.equal(s[b], state[b])
+            continue
+        cut = attention_reference(q[b:b + 1, :n], k[b:b + 1, :n], v[b:b + 1, :n], log_decay, state[b:b + 1], None, K ** -0.5,
+                                  torch.zeros(1, n, 2, V), None)
+        assert_near(o[b:b + 1, :n], cut[0], kind)
+        assert_near(s[b:b + 1], cut[1])
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("K,V", [(72, 192), (36, 8), (37, 9)])
+def test_linear_attention_gradient_of_single_tokens(K, V, kind):
+    """Shared heads, no initial state, no gradient of the final one: the transposed passes have no state to read or write."""
+    q, k, v, log_decay, _, _ = attention_inputs(5, 1, 4, 2, K, V, kind, state=False, seed=76)
+    g = noise(5, 1, 4, V, seed=77, kind=kind).cuda()
+    ins = [t.requires_grad_(True) for t in (q, k, v)]
+    grads = torch.autograd.grad(autograd.linear_attention(*ins, log_decay), ins, g)
+    want = attention_reference(q, k, v, log_decay, None, None, K ** -0.5, g, None)
+    for got, ref in zip(grads, want[2:5]):
+        assert_near(got, ref)
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("dim", [1, 3, 4, 31, 36, 130, 256])
+@pytest.mark.parametrize("group", [2, 5, 9])
+def test_linear_attention_gradients_of_shared_heads(group, dim, kind):
+    check_attention(*attention_inputs(2, 20, 2 * group, 2, dim, dim, kind, seed=80))
