@@ -80,6 +80,8 @@ int sig_rotary(sig_ctx *ctx, const void *x, const int64_t *x_strides, void *y, c
  *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous
  *   state_out    DEVICE, as `state` (and may be the same array): the state behind the last token; may be NULL
  * T == 1 is the form for single tokens.  Dimensions 1 ... 256; T == 0 copies the state; B == 0 does nothing.
+ * Context scratch where few heads' long sequences are cut along time: a state for each segment, of at most three workgroups for each
+ * compute unit; else none.
  */
 typedef struct sig_attention_t {
     int64_t B, T;
@@ -98,7 +100,9 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
  *   grad_state   DEVICE, float32, gradient with respect to state_out; NULL: zeros
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
- *   grad_initial DEVICE, float32, gradient with respect to `state`; may be NULL
+ *   grad_initial DEVICE, float32, gradient with respect to `state`; may be NULL; overlaps no other argument
+ * Context scratch as above, for up to three passes at once; and where heads share keys and values, B * T * heads * (key_dim + value_dim)
+ * floats for what is added up.
  */
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
                                   const float *log_decay, const float *state, const int64_t *lengths, const void *grad_out,

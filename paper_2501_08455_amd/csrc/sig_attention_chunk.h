@@ -11,6 +11,12 @@
 // meanwhile.  The tiles of the triangle are shared out over the wavefronts and passed on through LDS, as the fragments that
 // everyone reads.  Output tiles are taken as their transpose, in which a lane holds neighbouring columns of one token.
 //
+// Bound by neither memory nor the matrix units, but by what a chunk's steps wait for one after the other (operands from LDS, barriers) on the
+// two workgroups that a unit holds.  Measured: 65,536 tokens, 8 heads of 128 x 128 bfloat16, 242 us (2.2 TB/s of what goes in and out; matrix
+// units busy for 29% of the main launch, vector instructions 40%); 8 x 4,096 tokens, 16 heads, training, 660 us; 64 x 255 tokens, 4
+// heads of 64 x 64 float32, 26 us (2.6 TB/s).  Chunks of 64 tokens of bfloat16, since each also rounds the state anew for its
+// products (32 tokens: training 698 us), but 32 where the state has 256 rows (LDS then holds two workgroups); 32 of float32.
+//
 // A product of matrices multiplies every pair: 0 x infinity where the triangle is empty, and the parts of an infinite number.  A chunk
 // whose output is not finite is therefore worked out again token by token, so that what is not a number reaches what it
 // reaches in the recurrence (launches without output: the whole segment, if its state is not finite).
@@ -38,7 +44,9 @@ struct ChunkArgs {
     int passes, segments;
     int64_t segment_tokens;     // a multiple of the chunk; at least T where there is one segment
     int64_t states_apart;       // floats of `states` between passes
-    float *states;              // [passes][segments - 1][B][heads][rows][columns]: segments' own states, then what lies before the next segment
+    // [passes][segments][B][heads][rows][columns]: segments' own states, then what lies before the next segment; in the last place, where
+    // the last segment's workgroups write over the initial state, a copy of it for the first one's
+    float *states;
 };
 
 // Tiles of C tokens x W values, one after the other: global memory -> registers -> LDS (E), zeros where there is nothing.  A thread
@@ -218,7 +226,8 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     const int64_t head_state = (int64_t)A.rows * A.columns, at_head = (int64_t)b * A.heads + head;
     // A segment's state is kept behind it, and what lies before it where the last one's was.
     float *kept = G.states + pass * G.states_apart + (segment * A.B * A.heads + at_head) * head_state;
-    const float *from = segment > 0 ? kept - A.B * A.heads * head_state : A.state ? A.state + at_head * head_state : nullptr;
+    const bool copied = segment == 0 && G.segments > 1 && A.state && A.state == A.state_out, own = segment > 0 || copied;
+    const float *from = own ? kept + (copied ? G.segments - 1 : -1) * A.B * A.heads * head_state : A.state ? A.state + at_head * head_state : nullptr;
     float *state_to = !OUTPUT ? kept : segment + 1 == G.segments && A.state_out ? A.state_out + at_head * head_state : nullptr;
 #pragma unroll
     for (int nv = 0; nv < NV; ++nv) {
@@ -226,7 +235,7 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) s[kt][nv] = f4{};
         } else {
-            const int64_t row_stride = segment > 0 ? A.columns : A.row_stride, column_stride = segment > 0 ? 1 : A.column_stride;
+            const int64_t row_stride = own ? A.columns : A.row_stride, column_stride = own ? 1 : A.column_stride;
             const float *at = from + first_row * row_stride + (c0 + column + 16 * nv) * column_stride;
             int rows = from && column + 16 * nv < width ? A.rows - first_row : 0;
             asm volatile("" : "+v"(rows));

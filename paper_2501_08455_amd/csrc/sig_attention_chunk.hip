@@ -20,6 +20,7 @@ __global__ __launch_bounds__(kThreads) void sig_attention_join_kernel(ChunkArgs 
     const float g = A.log_decay[at_head % A.heads], whole = expm1f((float)G.segment_tokens * g);
     float *states = G.states + blockIdx.y * G.states_apart + at;
     float s = A.state ? A.state[at_head * size + row * A.row_stride + column * A.column_stride] : 0.0f;
+    if (A.state && A.state == A.state_out) states[(G.segments - 1) * all] = s;
     for (int first = 0; first < G.segments - 1; first += AHEAD) {
         float own[AHEAD];
 #pragma unroll
@@ -78,7 +79,7 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     return cut;
 }
 
-int64_t states_of(const AttentionArgs &A, const Cut &cut) { return (cut.segments - 1) * A.B * A.heads * A.rows * A.columns; }
+int64_t states_of(const AttentionArgs &A, const Cut &cut) { return cut.segments > 1 ? cut.segments * A.B * A.heads * A.rows * A.columns : 0; }
 
 // passes that one launch takes together: as many of the next ones as hold the same rows
 int together(const AttentionArgs *a, int passes, int type)

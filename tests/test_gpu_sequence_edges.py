@@ -1,5 +1,7 @@
 """The sequence-model operators at the sizes where their kernels change form, against the same 64-bit references and with the same tolerances as
 tests/test_gpu_sequence_ops.py."""
+import ctypes
+
 import pytest
 import torch
 
@@ -118,3 +120,23 @@ def test_linear_attention_gradient_of_single_tokens(K, V, kind):
 @pytest.mark.parametrize("group", [2, 5, 9])
 def test_linear_attention_gradients_of_shared_heads(group, dim, kind):
     check_attention(*attention_inputs(2, 20, 2 * group, 2, dim, dim, kind, seed=80))
+
+
+@gpu
+@pytest.mark.parametrize("kind,number", [(torch.float32, binding.SIG_F32), (torch.bfloat16, binding.SIG_BF16)])
+@pytest.mark.parametrize("T", [1, 20, 3000])
+def test_linear_attention_over_its_own_state(T, kind, number):
+    """The C entry point may write the new state over the initial one, also where a sequence's segments are different workgroups'."""
+    K, V = 64, 48
+    q, k, v, log_decay, state, _ = attention_inputs(2, T, 2, 2, K, V, kind, seed=90)
+    want_o, want_s = binding.linear_attention(q, k, v, log_decay, state=state, return_state=True)
+    shape = binding.sig_attention_t(2, T, 2, 2, K, V, number, K ** -0.5)
+    for name, t in (("q_strides", q), ("k_strides", k), ("v_strides", v)):
+        for i in range(3):
+            getattr(shape, name)[i] = t.stride(i)
+    o = torch.empty_like(want_o)
+    lib = binding.load()
+    rc = lib.sig_linear_attention(binding.default_ctx(), ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), None,
+                                  o.data_ptr(), state.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    assert torch.equal(o, want_o) and torch.equal(state, want_s)
