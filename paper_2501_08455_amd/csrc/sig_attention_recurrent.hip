@@ -1,4 +1,8 @@
 // Linear attention one token after the other (sig_attention.h): the form for single tokens.
+//
+// Bound by memory: a token reads and writes the whole state, with two multiply-adds a value.  Each thread's part of the state is some
+// rows apart in four neighbouring columns, so that loads are wide and the sum over rows needs two steps across lanes and one through
+// LDS.  Measured, one token: 256 x 16 states of 128 x 128, 114 us (4.8 TB/s, a copy of that size 4.9); 128 x 4 of 64 x 64, 5.6 us.
 #include "sig_attention.h"
 #include "sig_types.h"
 

@@ -8,6 +8,10 @@
 // second read.  Workgroups walk over rows, and in the gradient each thread adds up its columns' share of the
 // weights' gradients on the way; a second launch adds up the workgroups' sums in their order.  Longer rows are cut into pieces that
 // different workgroups take: partial sums, the rows' own numbers from them, then the output from a second read.
+//
+// Measured (a large copy reaches 4.9 TB/s, one that the last cache level holds 7.2): 65,536 rows of 780 bfloat16, 37 us forward (5.5 TB/s) and
+// 72 + 5 us for the gradient and the weights' (4.3 TB/s); 16 rows of 1,111,110 float32, 12 + 3 + 26 us and 23 + 5 + 38 us (5.3 to 6.2 TB/s in
+// the launches that read rows); 128 rows of 780, 3.6 us, which is a launch.
 #include <type_traits>
 #include <utility>
 
