@@ -72,17 +72,25 @@ AttentionArgs pass(const sig_attention_t &s, const float *log_decay, const int64
     return A;
 }
 
-// Up to this many tokens go one after the other: a chunk's products cost as much for one token as for all of it
-constexpr int kRecurrentTokens = 16;
+// Up to this many tokens go one after the other: a chunk's products cost as much for one token as for all of it.  Measured (us, token by
+// token; as a chunk):
+//   forward, tokens                            2           4           8            16
+//   bf16, 128 sequences, 16 heads of 64 x 64   17; 31      22; 31      32; 30       53; 30
+//   bf16, 64 sequences, 16 heads of 128 x 128  31; 47      40; 47      61; 48       103; 47
+//   f32, 128 sequences, 4 heads of 64 x 64     7.6; 11.4   9.6; 11.4   14.5; 11.4   24.9; 11.7
+// The gradient's passes are a launch each token by token, and one in chunks: 64 x 64 as above 75; 77 with two tokens, 99; 75 with four.
+constexpr int kRecurrentTokens = 4, kRecurrentGradientTokens = 2;
 
-int64_t scratch_floats(const AttentionArgs *a, int passes, int type, int cus)
+bool by_token(const AttentionArgs *a, bool gradient) { return a[0].T <= (gradient ? kRecurrentGradientTokens : kRecurrentTokens); }
+
+int64_t scratch_floats(const AttentionArgs *a, int passes, int type, int cus, bool gradient)
 {
-    return a[0].T > kRecurrentTokens ? attention_chunk_scratch_floats(a, passes, type, cus) : 0;
+    return by_token(a, gradient) ? 0 : attention_chunk_scratch_floats(a, passes, type, cus);
 }
 
-hipError_t launch(const AttentionArgs *a, int passes, int type, int out_type, float *scratch, int cus, hipStream_t st)
+hipError_t launch(const AttentionArgs *a, int passes, int type, int out_type, float *scratch, int cus, bool gradient, hipStream_t st)
 {
-    if (a[0].T > kRecurrentTokens) return launch_attention_chunk(a, passes, type, out_type, scratch, cus, st);
+    if (!by_token(a, gradient)) return launch_attention_chunk(a, passes, type, out_type, scratch, cus, st);
     hipError_t e = hipSuccess;
     for (int i = 0; i < passes && e == hipSuccess; ++i) e = launch_attention_recurrent(a[i], type, out_type, st);
     return e;
@@ -122,11 +130,11 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     const hipStream_t st = (hipStream_t)hip_stream;
     Scratch scratch;
     float *work = nullptr;
-    if (const int64_t floats = scratch_floats(&A, 1, s.type, ctx->num_cu)) {
+    if (const int64_t floats = scratch_floats(&A, 1, s.type, ctx->num_cu, false)) {
         const int got = scratch.get(ctx, (size_t)floats * sizeof(float), st, &work);
         if (got != SIG_OK) return got;
     }
-    return launch(&A, 1, s.type, s.type, work, ctx->num_cu, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+    return launch(&A, 1, s.type, s.type, work, ctx->num_cu, false, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
@@ -175,13 +183,13 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     contiguous(V_.os, s, s.heads, V);
     const int cus = ctx->num_cu;
     auto status = [](hipError_t e) { return e == hipSuccess ? SIG_OK : SIG_ERR_HIP; };
-    if (s.T == 0) return status(launch(&V_, 1, s.type, s.type, nullptr, cus, st));      // (the state's gradient alone)
+    if (s.T == 0) return status(launch(&V_, 1, s.type, s.type, nullptr, cus, true, st));      // (the state's gradient alone)
 
     // shared keys' and values' gradients go to scratch first, heads apart, and are added up from there
     const bool shared = group > 1;
-    int64_t states = scratch_floats(a, shared ? 1 : 3, s.type, cus);
+    int64_t states = scratch_floats(a, shared ? 1 : 3, s.type, cus, true);
     if (shared) {
-        const int64_t floats = scratch_floats(a + 1, 2, s.type, cus);
+        const int64_t floats = scratch_floats(a + 1, 2, s.type, cus, true);
         if (floats > states) states = floats;
     }
     const int64_t parts = shared ? s.B * s.T * s.heads : 0;
@@ -191,12 +199,12 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
         rc = scratch.get(ctx, (size_t)(states + parts * (K + V)) * sizeof(float), st, &work);
         if (rc != SIG_OK) return rc;
     }
-    if (!shared) return status(launch(a, 3, s.type, s.type, work, cus, st));
+    if (!shared) return status(launch(a, 3, s.type, s.type, work, cus, true, st));
     float *part_k = work + states, *part_v = part_k + parts * K;
     K_.o = part_k;
     V_.o = part_v;
-    hipError_t e = launch(a, 1, s.type, s.type, work, cus, st);
-    if (e == hipSuccess) e = launch(a + 1, 2, s.type, SIG_F32, work, cus, st);
+    hipError_t e = launch(a, 1, s.type, s.type, work, cus, true, st);
+    if (e == hipSuccess) e = launch(a + 1, 2, s.type, SIG_F32, work, cus, true, st);
     auto add_up = [&](const float *part, void *grad, int dim) {
         const int64_t rows = s.B * s.T * s.shared_heads;
         const int each = dim % 4 == 0 ? 4 : 1;
