@@ -15,7 +15,7 @@
 // two workgroups that a unit holds.  Measured: 65,536 tokens, 8 heads of 128 x 128 bfloat16, 242 us (2.2 TB/s of what goes in and out; matrix
 // units busy for 29% of the main launch, vector instructions 40%); 8 x 4,096 tokens, 16 heads, training, 660 us; 64 x 255 tokens, 4
 // heads of 64 x 64 float32, 26 us (2.6 TB/s).  Chunks of 64 tokens of bfloat16, since each also rounds the state anew for its
-// products (32 tokens: training 698 us), but 32 where the state has 256 rows (LDS then holds two workgroups); 32 of float32.
+// products (32 tokens: training 698 us), but 32 where the state has 256 rows (LDS then holds two workgroups) or sequences are short; 32 of float32.
 //
 // A product of matrices multiplies every pair: 0 x infinity where the triangle is empty, and the parts of an infinite number.  A chunk
 // whose output is not finite is therefore worked out again token by token, so that what is not a number reaches what it
@@ -531,6 +531,13 @@ inline int chunk_rows(int rows, int type)
     return rows <= 32 ? 32 : halves && rows <= 48 ? 48 : rows <= 64 ? 64 : halves && rows <= 80 ? 80 : rows <= 96 ? 96 : rows <= 128 ? 128 : rows <= 192 ? 192 : 256;
 }
 
+// Up to so many tokens bfloat16 goes in chunks of 32 too (more workgroups a unit, fewer tokens to fill up).  Measured (us, chunks of 64; of 32):
+//   tokens                                        16         48         96         192        256        3,000
+//   128 sequences, 16 heads of 64 x 64            26; 18     27; 23     39; 28     53; 45     64; 59     748; 783
+//   64 sequences, 16 heads of 128 x 128, training 126; 89    137; 122   209; 164   314; 293   396; 379   4,091; 4,274
+//   4 sequences, 8 heads of 128 x 128             11; 9      11; 12     16; 15     20; 23     25; 28     82; 84
+constexpr int kShortTokens = 192;
+
 // The instance for `G`: up to 64 nv columns a workgroup
 template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
 void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
@@ -543,6 +550,12 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
         const dim3 grid((unsigned)(A.B * A.heads), (unsigned)((columns + 64 * NV - 1) / (64 * NV)),
                         (unsigned)(G.passes * (OUTPUT ? G.segments : G.segments - 1)));
         constexpr int K = decltype(k)::value;
+        if constexpr (OUTPUT && C == 64 && K >= 64 && K < 256) {
+            if (A.T <= kShortTokens) {
+                sig_attention_chunk_kernel<T, O, E, 32, K, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
+                return;
+            }
+        }
         sig_attention_chunk_kernel<T, O, E, K == 256 ? 32 : C, K, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
     constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
