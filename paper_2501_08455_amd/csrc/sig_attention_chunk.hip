@@ -47,8 +47,9 @@ struct Cut {
 //     1,024 tokens                 81; 107                      62; 123         82; 195
 //   f32, 128 x 128, 128 heads, 1,024 tokens   198; 353          129; 328        164; 438
 // Workgroups of 128 columns, which share the operands' loads and the pairs of a chunk, where they are more than the units (float32, bound by
-// its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that, and long sequences of
-// less than two a unit, are cut along time, which costs a second read of y and z, the segments' states and two more launches
+// its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that, and small states' long sequences of
+// less than two a unit (50 sequences of 2,048 tokens, 4 heads of 64 x 64 bfloat16: 94 whole, 79 cut; of 192 x 64 float32 386 whole, 415
+// cut, of 256 x 64 452 and 511), are cut along time, which costs a second read of y and z, the segments' states and two more launches
 // (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64
 // segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of such workgroups at once: two, or three of small
 // states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two, 98 for three).
@@ -67,7 +68,7 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     };
     Cut cut = {wide && 4 * workgroups(2) >= (type == SIG_BF16 ? 5 : 8) * cus ? 2 : 1, 1, a[0].T};
     const int64_t chunks = (a[0].T + chunk - 1) / chunk, n = workgroups(cut.nv);
-    if (4 * n < 3 * cus || (cut.nv == 1 && n < 2 * cus && chunks >= 48)) {
+    if (4 * n < 3 * cus || (small && cut.nv == 1 && n < 2 * cus && chunks >= (type == SIG_BF16 ? 32 : 48))) {
         if (wide) cut.nv = 2;
         int64_t segments = (small && cut.nv == 1 ? 3 : 2) * cus / workgroups(cut.nv);      // (that many workgroups a unit)
         if (segments > chunks / 4) segments = chunks / 4;
