@@ -5,8 +5,10 @@
  * synchronisation, a status code for every failure, context scratch as described there (each entry point says what it
  * keeps there), deterministic results (no atomics, fixed summation order).
  *
- * Values are float32, bfloat16 or float16 in memory (enum sig_type).  All arithmetic, sums, statistics and states
- * are in float32 or more; each output is rounded once.  Pointers are aligned to their type, no more is asked for.
+ * Values are float32, bfloat16 or float16 in memory (enum sig_type).  Sums, statistics and states are in float32 or more; each
+ * output is rounded once.  Arithmetic is float32's too, but for one thing: attention of bfloat16 over more than four tokens (more than two in
+ * the gradient) multiplies with the state, and with the products of queries and keys, rounded to 16 digits, for outputs that
+ * have 8.  The state itself, and so state_out and grad_initial, keeps float32's.  Pointers are aligned to their type, no more is asked for.
  */
 #ifndef SIG_SEQUENCE_H
 #define SIG_SEQUENCE_H

@@ -30,7 +30,6 @@ struct AttentionArgs {
     int heads, rows, columns;          // of the state: x and y have `rows` values, z and o `columns`
     float out_scale, update_scale;
     int reversed;
-    int exact;                         // whether the state keeps all its digits (not where only a gradient in 16 bits depends on it)
 };
 
 __device__ inline int64_t attention_length(const AttentionArgs &A, int64_t b)

@@ -125,7 +125,6 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     A.o = out;
     contiguous(A.os, s, s.heads, s.value_dim);
     A.out_scale = s.scale;
-    A.exact = 1;      // (also where the state is not asked for: the outputs do not depend on that)
     from_state(A, state, state_out, false);
     const hipStream_t st = (hipStream_t)hip_stream;
     Scratch scratch;
@@ -175,7 +174,6 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     operand(&V_.z, V_.zs, &V_.z_group, grad_out, gs, 1);
     V_.update_scale = s.scale;
     V_.reversed = 1;
-    V_.exact = grad_initial != nullptr;
     from_state(V_, grad_state, grad_initial, false);
     K_.o = grad_k;
     contiguous(K_.os, s, s.heads, K);

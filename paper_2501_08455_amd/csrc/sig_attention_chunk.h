@@ -168,13 +168,11 @@ __device__ inline void interleave()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; NV: tiles of 16 columns a wavefront; PARTS: fragments that
-// the state's update takes each weighted z in (Matrix<E>::EXACT: all its digits; two of bfloat16, sixteen digits, where nothing but outputs in
-// bfloat16 depends on the state: a hundred times finer than they are); OUTPUT: 0 for launches that only work out the
-// segments' own states
+// T, O: types of operands and output; E: type in LDS; K: rows of the state, rounded up; NV: tiles of 16 columns a wavefront; OUTPUT: 0 for launches that
+// only work out the segments' own states
 // Two workgroups a unit, where LDS has room for them (with one, whose registers the compiler then spreads out: 192 rows of bfloat16 1.15 to 1.6
 // times as long, 192 and 256 rows of float32 1.1 to 1.3).
-template <typename T, typename O, typename E, int C, int K, int NV, int PARTS, bool OUTPUT>
+template <typename T, typename O, typename E, int C, int K, int NV, bool OUTPUT>
 __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void sig_attention_chunk_kernel(ChunkArgs G)
 {
     using M = Matrix<E>;
@@ -182,7 +180,10 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     constexpr int THREADS = kChunkThreads, WAVES = THREADS / 64, VT = 64 * NV;
     constexpr int XPITCH = K + M::PAD, YPITCH = K + M::COLUMN_PAD, ZPITCH = VT + M::COLUMN_PAD;
     constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, KT = K / 16, SUB = M::SUB;
-    constexpr int SPLIT = SUB == 2 ? 2 : 1;       // bfloat16 fragments of the state and of the triangle: 16 digits
+    // The state itself keeps all digits of float32: each weighted z goes into its update as fragments that add up to it.  As operands of the
+    // outputs' products the state and the triangle of pairs are two bfloat16 fragments, 16 digits, where those outputs are rounded to 8 (24 digits
+    // leave the same errors: 65,536 tokens, 8 heads of 128 x 128, 258 us instead of 239; a training batch 792 instead of 714).
+    constexpr int PARTS = M::EXACT, SPLIT = SUB == 2 ? 2 : 1;
     constexpr int YB = KT % 4 == 0 ? 4 : KT % 3 == 0 ? 3 : KT;      // tiles of the state whose operands are loaded at once
     const int pass = blockIdx.z % G.passes, segment = blockIdx.z / G.passes;
     const AttentionArgs &A = G.a[pass];
@@ -539,7 +540,7 @@ inline int chunk_rows(int rows, int type)
 constexpr int kShortTokens = 192;
 
 // The instance for `G`: up to 64 nv columns a workgroup
-template <typename T, typename O, typename E, int C, int PARTS, bool OUTPUT>
+template <typename T, typename O, typename E, int C, bool OUTPUT>
 void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
 {
     const AttentionArgs &A = G.a[0];
@@ -552,11 +553,11 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
         constexpr int K = decltype(k)::value;
         if constexpr (OUTPUT && C == 64 && K >= 64 && K < 256) {
             if (A.T <= kShortTokens) {
-                sig_attention_chunk_kernel<T, O, E, 32, K, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
+                sig_attention_chunk_kernel<T, O, E, 32, K, NV, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
                 return;
             }
         }
-        sig_attention_chunk_kernel<T, O, E, K == 256 ? 32 : C, K, NV, PARTS, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
+        sig_attention_chunk_kernel<T, O, E, K == 256 ? 32 : C, K, NV, OUTPUT><<<grid, kChunkThreads, 0, st>>>(G);
     };
     constexpr int WIDE = sizeof(O) == sizeof(T) || sizeof(E) == 4 ? 2 : 1;       // (registers)
     auto either = [&](auto k) { nv == 2 ? go(k, Number<2>()) : go(k, Number<1>()); };
@@ -572,20 +573,18 @@ void launch_chunk_instance(const ChunkArgs &G, int nv, hipStream_t st)
     }
 }
 
-// exact: all digits of the state (where it is a result), else sixteen (where only outputs of the operands' type depend on it)
 template <typename T, typename E, int C>
-void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st)
+void launch_chunk(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st)
 {
-    constexpr int EXACT = Matrix<E>::EXACT, SHORT = EXACT < 2 ? EXACT : 2;
-    if (!output) exact ? launch_chunk_instance<T, T, E, C, EXACT, false>(G, nv, st) : launch_chunk_instance<T, T, E, C, SHORT, false>(G, nv, st);
-    else if (partial) exact ? launch_chunk_instance<T, float, E, C, EXACT, true>(G, nv, st) : launch_chunk_instance<T, float, E, C, SHORT, true>(G, nv, st);
-    else exact ? launch_chunk_instance<T, T, E, C, EXACT, true>(G, nv, st) : launch_chunk_instance<T, T, E, C, SHORT, true>(G, nv, st);
+    if (!output) launch_chunk_instance<T, T, E, C, false>(G, nv, st);
+    else if (partial) launch_chunk_instance<T, float, E, C, true>(G, nv, st);
+    else launch_chunk_instance<T, T, E, C, true>(G, nv, st);
 }
 
 // one for each type of the operands, in a file of its own; partial: float32 output
-void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
-void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
-void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, bool exact, hipStream_t st);
+void launch_chunk_f32(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_bf16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
+void launch_chunk_f16(const ChunkArgs &G, int nv, bool output, bool partial, hipStream_t st);
 
 }  // namespace sig
 #endif

@@ -113,17 +113,13 @@ hipError_t launch_attention_chunk(const AttentionArgs *a, int passes, int type, 
         n = together(a + first, passes - first, type);
         const Cut cut = cut_of(a + first, n, type, cus);
         ChunkArgs G = {{}, n, cut.segments, cut.segment_tokens, states_of(a[first], cut), scratch};
-        bool exact = false;
-        for (int i = 0; i < n; ++i) {
-            G.a[i] = a[first + i];
-            exact = exact || G.a[i].exact;
-        }
+        for (int i = 0; i < n; ++i) G.a[i] = a[first + i];
         if (cut.segments > 1) {
-            launch(G, cut.nv, false, partial, exact, st);
+            launch(G, cut.nv, false, partial, st);
             const int64_t values = G.a[0].B * G.a[0].heads * G.a[0].rows * G.a[0].columns;
             sig_attention_join_kernel<<<dim3((unsigned)((values + kThreads - 1) / kThreads), (unsigned)n), kThreads, 0, st>>>(G);
         }
-        launch(G, cut.nv, true, partial, exact, st);
+        launch(G, cut.nv, true, partial, st);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
