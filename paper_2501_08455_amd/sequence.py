@@ -82,7 +82,8 @@ class SequenceModel(torch.nn.Module):
         """The cache behind the first point, x0 [B, inputs]."""
         B = x0.shape[0]
         state = torch.zeros(B, self.heads, self.head_dim, self.head_dim, device=x0.device)
-        return {"point": torch.tanh(self.path(x0)), "row": None, "state": state, "position": torch.zeros(1, device=x0.device)}
+        # (counted in whole numbers, as forward() does: float32 stops at 2^24)
+        return {"point": torch.tanh(self.path(x0)), "row": None, "state": state, "position": torch.zeros(1, dtype=torch.int64, device=x0.device)}
 
     @torch.no_grad()
     def step(self, x, cache):
