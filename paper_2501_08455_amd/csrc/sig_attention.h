@@ -11,6 +11,8 @@
 #ifndef SIG_ATTENTION_H
 #define SIG_ATTENTION_H
 
+#include <cfloat>
+
 #include "sig_internal.h"
 #include "sig_sequence.h"
 
@@ -38,6 +40,16 @@ __device__ inline int64_t attention_length(const AttentionArgs &A, int64_t b)
     const int64_t n = A.lengths[b];
     return n < 0 ? 0 : n > A.T ? A.T : n;
 }
+
+// What a number is multiplied with over `tokens` tokens: l^tokens = 1 + shrink.  (The power itself, rounded, would drift over many tokens where
+// little decays.)  s l^tokens is s + s shrink, where an infinite s has to stay what it is, as long as l is not 0: the s that is shrunk is
+// taken into -most .. most.
+struct Decay {
+    float shrink, most;
+
+    __device__ Decay(float log_decay, float tokens) : shrink(expm1f(tokens * log_decay)), most(log_decay == -INFINITY ? INFINITY : FLT_MAX) {}
+    __device__ float operator()(float s) const { return fmaf(__builtin_amdgcn_fmed3f(s, -most, most), shrink, s); }
+};
 
 // types of the operands and of `o` (enum sig_type)
 // one token after the other

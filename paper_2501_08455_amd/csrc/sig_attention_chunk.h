@@ -124,7 +124,7 @@ template <bool OUTPUT, int KT, int NV, typename E, typename Row, typename Store>
 __device__ inline void chunk_by_token(const AttentionArgs &A, float g, int n, const E *xs, int xpitch, const E *ys, int ypitch, const E *zs, int zpitch,
                                       f4 (&s)[KT][NV], int first_row, Row row_of, int column, Store store)
 {
-    const float shrink = expm1f(g);
+    const Decay decay(g, 1.0f);
 #pragma unroll 1
     for (int r = 0; r < n; ++r) {
         int rows = A.rows;
@@ -140,10 +140,10 @@ __device__ inline void chunk_by_token(const AttentionArgs &A, float g, int n, co
                     const int row = first_row + row_of(kt) + i;
                     if (row >= rows) continue;
                     float c = s[kt][nv][i];
-                    if (!A.reversed) c = fmaf(c, shrink, c);
+                    if (!A.reversed) c = decay(c);
                     c = fmaf((float)ys[r * ypitch + row], z, c);
                     if (OUTPUT) part = fmaf((float)xs[r * xpitch + row], c, part);
-                    if (A.reversed) c = fmaf(c, shrink, c);
+                    if (A.reversed) c = decay(c);
                     s[kt][nv][i] = c;
                 }
             if (OUTPUT) {
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
                 for (int nv = 0; nv < NV; ++nv) zf[st][nv] = M::template along_columns<false>(zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * nv);
         }
         if (!again) {
-            // the state behind the chunk.  l^n = 1 + (l^n - 1): the power itself, rounded, would drift over many chunks where little decays
+            // the state behind the chunk (a finite one; see Decay)
             const float shrink = expm1f((float)n * g);
             constexpr int BLOCKS = KT / YB, ALL = STEPS * BLOCKS;
             static_assert(KT % YB == 0);

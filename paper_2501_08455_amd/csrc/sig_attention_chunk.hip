@@ -17,7 +17,8 @@ __global__ __launch_bounds__(kThreads) void sig_attention_join_kernel(ChunkArgs 
     if (at >= all) return;
     const int64_t at_head = at / size, row = at % size / A.columns, column = at % A.columns;
     const int64_t length = attention_length(A, at_head / A.heads);
-    const float g = A.log_decay[at_head % A.heads], whole = expm1f((float)G.segment_tokens * g);
+    const float g = A.log_decay[at_head % A.heads];
+    const Decay whole(g, (float)G.segment_tokens);
     float *states = G.states + blockIdx.y * G.states_apart + at;
     float s = A.state ? A.state[at_head * size + row * A.row_stride + column * A.column_stride] : 0.0f;
     if (A.state && A.state == A.state_out) states[(G.segments - 1) * all] = s;
@@ -29,8 +30,8 @@ __global__ __launch_bounds__(kThreads) void sig_attention_join_kernel(ChunkArgs 
         for (int i = 0; i < AHEAD; ++i) {
             if (first + i >= G.segments - 1) break;
             const int64_t n = length - (first + i) * G.segment_tokens;
-            if (n >= G.segment_tokens) s = fmaf(s, whole, s) + own[i];
-            else if (n > 0) s = fmaf(s, expm1f((float)n * g), s) + own[i];
+            if (n >= G.segment_tokens) s = whole(s) + own[i];
+            else if (n > 0) s = Decay(g, (float)n)(s) + own[i];
             states[(first + i) * all] = s;
         }
     }

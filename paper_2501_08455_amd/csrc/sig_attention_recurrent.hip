@@ -27,8 +27,7 @@ __global__ __launch_bounds__(kThreads) void sig_attention_recurrent_kernel(Atten
     const T *z = (const T *)A.z + b * A.zs[0] + head / A.z_group * A.zs[2];
     O *o = (O *)A.o + b * A.os[0] + head * A.os[2];
     const int64_t state_at = ((int64_t)b * A.heads + head) * A.rows * A.columns;
-    // l = 1 + shrink: the decay itself, rounded, would drift over many tokens where little decays
-    const float shrink = expm1f(A.log_decay[head]);
+    const Decay decay(A.log_decay[head], 1.0f);
     const int64_t length = attention_length(A, b);
     const bool in = c < A.columns;    // (with N > 1 the columns are a multiple of N)
 
@@ -65,10 +64,10 @@ __global__ __launch_bounds__(kThreads) void sig_attention_recurrent_kernel(Atten
             const float xr = to_float(x[t * A.xs[1] + row]), yr = to_float(y[t * A.ys[1] + row]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                if (!A.reversed) s[i][j] = fmaf(s[i][j], shrink, s[i][j]);
+                if (!A.reversed) s[i][j] = decay(s[i][j]);
                 s[i][j] = fmaf(yr, zs[j], s[i][j]);
                 part[j] = fmaf(xr, s[i][j], part[j]);
-                if (A.reversed) s[i][j] = fmaf(s[i][j], shrink, s[i][j]);
+                if (A.reversed) s[i][j] = decay(s[i][j]);
             }
         }
 #pragma unroll
