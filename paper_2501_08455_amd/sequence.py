@@ -49,7 +49,9 @@ class SequenceModel(torch.nn.Module):
     with a decay for each head -> layer norm of each head -> Dense(outputs).
 
     `model(x)` with x [B, L, inputs] gives [B, L - 1, outputs], one row for each prefix; `lengths` [B] counts the prefixes that are there.
-    `model.begin(x0)` and `model.step(x, cache)` give the same rows one point at a time."""
+    `model.begin(x0)` and `model.step(x, cache)` give the same rows one point at a time.
+
+    A model whose parameters are converted (`model.bfloat16()`, `.half()`) mixes and attends in that type; paths, signatures and states are float32."""
 
     def __init__(self, inputs, channels, depth, outputs, heads=4, head_dim=64, turned=None, decays=(0.125, 0.002), device="cuda", **positions):
         super().__init__()
@@ -67,10 +69,29 @@ class SequenceModel(torch.nn.Module):
         lost = decays[0] * (decays[1] / decays[0]) ** (torch.arange(heads, dtype=torch.float64) / max(heads - 1, 1))
         self.register_buffer("log_decay", torch.log1p(-lost).float().to(device))
 
+    def _apply(self, fn, *args, **kwargs):
+        # the operators take these two in their own types, whatever the parameters are converted to: they only move
+        own = {name: self._buffers[name] for name in ("frequencies", "log_decay")}
+        super()._apply(fn, *args, **kwargs)
+        for name, buffer in own.items():
+            if self._buffers[name].dtype != buffer.dtype:
+                self._buffers[name] = buffer.to(self._buffers[name].device)
+        return self
+
+    def _points(self, x):
+        """The path's points, float32 (differences of rounded points would lose the steps between them)."""
+        if self.path.weight.dtype == torch.float32:
+            return torch.tanh(self.path(x.float()))
+        return torch.tanh(torch.nn.functional.linear(x.float(), self.path.weight.float(), self.path.bias.float()))
+
+    def _normed(self, layer_norm, rows):
+        """Signature rows, float32, through the layer norm and into the parameters' type (their range may be beyond float16's before)."""
+        return layer_norm(rows, self.norm_weight.float(), self.norm_bias.float()).to(self.mix.weight.dtype)
+
     def forward(self, x, lengths=None):
-        rows = autograd.signature(torch.tanh(self.path(x)), self.depth, stream=True)
+        rows = autograd.signature(self._points(x), self.depth, stream=True)
         B, T, _ = rows.shape
-        mixed = self.mix(autograd.layer_norm(rows, self.norm_weight, self.norm_bias)).view(B, T, 3 * self.heads, self.head_dim)
+        mixed = self.mix(self._normed(autograd.layer_norm, rows)).view(B, T, 3 * self.heads, self.head_dim)
         positions = torch.arange(T, device=x.device)
         # queries and keys are turned together
         turned = autograd.rotary(mixed[:, :, :2 * self.heads], positions, self.frequencies, scale=self.scale)
@@ -81,14 +102,14 @@ class SequenceModel(torch.nn.Module):
     def begin(self, x0):
         """The cache behind the first point, x0 [B, inputs]."""
         B = x0.shape[0]
-        state = torch.zeros(B, self.heads, self.head_dim, self.head_dim, device=x0.device)
+        state = torch.zeros(B, self.heads, self.head_dim, self.head_dim, dtype=torch.float32, device=x0.device)
         # (counted in whole numbers, as forward() does: float32 stops at 2^24)
-        return {"point": torch.tanh(self.path(x0)), "row": None, "state": state, "position": torch.zeros(1, dtype=torch.int64, device=x0.device)}
+        return {"point": self._points(x0), "row": None, "state": state, "position": torch.zeros(1, dtype=torch.int64, device=x0.device)}
 
     @torch.no_grad()
     def step(self, x, cache):
         """The next point, x [B, inputs]: the outputs [B, outputs] of the prefix that ends there.  Updates `cache` in place."""
-        point = torch.tanh(self.path(x))
+        point = self._points(x)
         segment = binding.signature(torch.stack((cache["point"], point), 1), self.depth)
         if cache["row"] is None:
             cache["row"] = segment
@@ -99,7 +120,7 @@ class SequenceModel(torch.nn.Module):
                 raise binding.SigError(rc, "sig_combine")
             cache["row"] = row
         cache["point"] = point
-        mixed = self.mix(binding.layer_norm(cache["row"], self.norm_weight, self.norm_bias)).view(-1, 1, 3 * self.heads, self.head_dim)
+        mixed = self.mix(self._normed(binding.layer_norm, cache["row"])).view(-1, 1, 3 * self.heads, self.head_dim)
         turned = mixed[:, :, :2 * self.heads]
         binding.rotary(turned, cache["position"], self.frequencies, scale=self.scale, out=turned)
         cache["position"] += 1
