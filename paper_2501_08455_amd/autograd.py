@@ -39,23 +39,47 @@ def signature(path, depth, stream=False):
     return (binding._torch_lib or binding.torch_lib()).autograd_signature(path, depth, stream)
 
 
-class _TracedCall(torch.autograd.Function):
-    """A native differentiable call while torch.jit.trace is recording (see _Traced): `call` takes the tensors."""
+class _FirstOrderOnly(torch.autograd.Function):
+    """The first `count` of `tensors`, the gradients; a derivative of those with respect to any of them is an error, not a zero."""
 
     @staticmethod
-    def forward(ctx, call, *tensors):
-        ctx.inputs = [t.detach().requires_grad_(t.requires_grad) if torch.is_tensor(t) else t for t in tensors]
-        with torch.enable_grad():
-            ctx.outputs = call(*ctx.inputs)
-        one = torch.is_tensor(ctx.outputs)
-        return ctx.outputs.detach() if one else tuple(t.detach() for t in ctx.outputs)
+    def forward(ctx, count, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:count])
 
     @staticmethod
     def backward(ctx, *grads):
-        outputs = (ctx.outputs,) if torch.is_tensor(ctx.outputs) else ctx.outputs
-        wanted = [t for t in ctx.inputs if torch.is_tensor(t) and t.requires_grad]
-        got = iter(torch.autograd.grad(outputs, wanted, grads))
-        return (None,) + tuple(next(got) if torch.is_tensor(t) and t.requires_grad else None for t in ctx.inputs)
+        raise RuntimeError("libsig's operators have no second derivative")
+
+
+class _TracedCall(torch.autograd.Function):
+    """A native differentiable call while torch.jit.trace is recording (see _Traced): `call` takes the tensors.  The backward pass makes
+    it again from the saved inputs and goes through its own node, which is gone behind each call: what a graph may do with a saved
+    tensor (be walked twice, notice a change in place, be freed) stays with this Function's."""
+
+    @staticmethod
+    def _recorded(call, tensors, needed):
+        inputs = [t.detach().requires_grad_(n) if torch.is_tensor(t) else t for t, n in zip(tensors, needed)]
+        with torch.enable_grad():
+            out = call(*inputs)
+        return inputs, (out,) if torch.is_tensor(out) else out
+
+    @staticmethod
+    def forward(ctx, call, *tensors):
+        ctx.call = call
+        ctx.save_for_backward(*tensors)
+        # (recorded, so that it refuses here what it has no gradient for)
+        out = [t.detach() for t in _TracedCall._recorded(call, tensors, ctx.needs_input_grad[1:])[1]]
+        return out[0] if len(out) == 1 else tuple(out)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        needed = ctx.needs_input_grad[1:]
+        inputs, out = _TracedCall._recorded(ctx.call, ctx.saved_tensors, needed)
+        got = torch.autograd.grad(out, [t for t, n in zip(inputs, needed) if n], [g.detach() for g in grads])
+        if torch.is_grad_enabled():
+            got = _FirstOrderOnly.apply(len(got), *got, *(t for t in ctx.saved_tensors + grads if t is not None))
+        got = iter(got)
+        return (None,) + tuple(next(got) if n else None for n in needed)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
