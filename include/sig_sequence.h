@@ -29,7 +29,8 @@ enum sig_type { SIG_F32 = 0, SIG_BF16 = 1, SIG_F16 = 2 };
  *   weight, bias DEVICE, [width] of `weight_type` (SIG_F32 or `type`), each may be NULL (1 and 0)
  *   y            DEVICE, [rows][width] of `type`, contiguous; must not overlap the inputs
  *   stats        DEVICE, float32 [rows][2], what sig_layer_norm_backward needs (mean, 1 / sqrt(...)); may be NULL
- * rows == 0 returns SIG_OK and launches nothing; width < 1, rows < 0 or a NaN or negative eps are SIG_ERR_INVALID.
+ * rows == 0 returns SIG_OK and launches nothing; width < 1, rows < 0 or a NaN or negative eps are SIG_ERR_INVALID; rows of more than 16,384
+ * values that are 2^24 pieces of 8,192 or more are SIG_ERR_TOO_LARGE.
  * NaN and Inf spoil their own row only.  Any width: rows of up to 16,384 values stay on chip between their
  * statistics and their output, longer ones are read twice and cut across workgroups (context scratch of about 2 floats for
  * every 8,192 values).
@@ -62,7 +63,8 @@ enum sig_position { SIG_POSITION_I32 = 0, SIG_POSITION_I64 = 1, SIG_POSITION_F32
  *   positions    DEVICE, of `position_type`, position_strides[2] values apart between batches and tokens (0: shared);
  *                whole positions, or times (irregular series)
  *   frequencies  DEVICE, float64 [turned / 2], radians a position
- * The angle is reduced in 64 bits, so that far positions keep their digits.  turned is even, 0 <= turned <= dim.
+ * The angle is reduced in 64 bits, so that far positions keep their digits.  turned is even, 0 <= turned <= dim; more than 4,096 turned
+ * components are SIG_ERR_UNSUPPORTED, 2^31 tokens (B * T) or more, or so many values of a token, SIG_ERR_TOO_LARGE.
  */
 int sig_rotary(sig_ctx *ctx, const void *x, const int64_t *x_strides, void *y, const int64_t *y_strides, int type, int64_t B, int64_t T,
                int64_t heads, int64_t dim, int64_t turned, const void *positions, int position_type, const int64_t *position_strides,
@@ -81,7 +83,8 @@ int sig_rotary(sig_ctx *ctx, const void *x, const int64_t *x_strides, void *y, c
  *                not read, give zeros, and leave the state alone
  *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous
  *   state_out    DEVICE, as `state` (and may be the same array): the state behind the last token; may be NULL
- * T == 1 is the form for single tokens.  Dimensions 1 ... 256; T == 0 copies the state; B == 0 does nothing.
+ * T == 1 is the form for single tokens.  Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); T == 0 copies the state; B == 0 does
+ * nothing.  2^24 heads or more, or 2^31 states, are SIG_ERR_TOO_LARGE; what one launch cannot hold is taken in slices of the batch.
  * Context scratch where few heads' long sequences are cut along time: a state for each segment, of at most three workgroups for each
  * compute unit; else none.
  */

@@ -1,5 +1,7 @@
 // Entry points of linear attention (include/sig_sequence.h): argument checks, the passes of the gradient, and the sum
 // over heads that share keys and values.
+#include <type_traits>
+
 #include "sig_attention.h"
 #include "sig_context.h"
 #include "sig_types.h"
@@ -10,6 +12,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostDim = 256;
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 32) / kThreads - 1;      // along an axis: a launch holds fewer than 2^32 threads there
 
 // out[token][shared head][.] = sum over the heads of a shared head of part[token][head][.], in their order.  `lanes` threads (a power
 // of two) take a shared head's values, N each, up to four heads' loads at once.
@@ -40,7 +43,7 @@ int check(const sig_ctx *ctx, const sig_attention_t *s)
         s->value_dim < 1 || !valid_type(s->type))
         return SIG_ERR_INVALID;
     if (s->key_dim > kMostDim || s->value_dim > kMostDim) return SIG_ERR_UNSUPPORTED;
-    if (s->B > INT32_MAX / s->heads || (s->T > 0 && s->B * s->heads > INT64_MAX / (8 * kMostDim) / s->T)) return SIG_ERR_TOO_LARGE;
+    if (s->heads > kMostWorkgroups || s->B > INT32_MAX / s->heads || (s->T > 0 && s->B * s->heads > INT64_MAX / (8 * kMostDim) / s->T)) return SIG_ERR_TOO_LARGE;
     return SIG_OK;
 }
 
@@ -105,18 +108,10 @@ void from_state(AttentionArgs &A, const float *state, float *state_out, bool tra
     A.column_stride = transposed ? A.rows : 1;
 }
 
-}  // namespace
-
-extern "C" {
-
-int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v, const float *log_decay,
-                         const float *state, const int64_t *lengths, void *out, float *state_out, void *hip_stream)
+// the call for a batch that one launch holds
+int forward(sig_ctx *ctx, const sig_attention_t &s, const void *q, const void *k, const void *v, const float *log_decay, const float *state,
+            const int64_t *lengths, void *out, float *state_out, hipStream_t st)
 {
-    const int rc = check(ctx, shape);
-    if (rc != SIG_OK) return rc;
-    const sig_attention_t &s = *shape;
-    if (s.B == 0 || (s.T == 0 && !state_out)) return SIG_OK;
-    if (!log_decay || (s.T > 0 && (!q || !k || !v || !out))) return SIG_ERR_INVALID;
     const int group = s.heads / s.shared_heads;
     AttentionArgs A = pass(s, log_decay, lengths, s.key_dim, s.value_dim);
     operand(&A.x, A.xs, &A.x_group, q, s.q_strides, 1);
@@ -126,7 +121,6 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     contiguous(A.os, s, s.heads, s.value_dim);
     A.out_scale = s.scale;
     from_state(A, state, state_out, false);
-    const hipStream_t st = (hipStream_t)hip_stream;
     Scratch scratch;
     float *work = nullptr;
     if (const int64_t floats = scratch_floats(&A, 1, s.type, ctx->num_cu, false)) {
@@ -136,16 +130,10 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
     return launch(&A, 1, s.type, s.type, work, ctx->num_cu, false, st) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
-int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
-                                  const float *log_decay, const float *state, const int64_t *lengths, const void *grad_out,
-                                  const float *grad_state, void *grad_q, void *grad_k, void *grad_v, float *grad_initial, void *hip_stream)
+int backward(sig_ctx *ctx, const sig_attention_t &s, const void *q, const void *k, const void *v, const float *log_decay, const float *state,
+             const int64_t *lengths, const void *grad_out, const float *grad_state, void *grad_q, void *grad_k, void *grad_v, float *grad_initial,
+             hipStream_t st)
 {
-    int rc = check(ctx, shape);
-    if (rc != SIG_OK) return rc;
-    const sig_attention_t &s = *shape;
-    if (s.B == 0 || (s.T == 0 && !grad_initial)) return SIG_OK;
-    if (!log_decay || (s.T > 0 && (!q || !k || !v || !grad_out || !grad_q || !grad_k || !grad_v))) return SIG_ERR_INVALID;
-    const hipStream_t st = (hipStream_t)hip_stream;
     const int K = s.key_dim, V = s.value_dim, group = s.heads / s.shared_heads;
     int64_t gs[3];
     contiguous(gs, s, s.heads, V);
@@ -194,7 +182,7 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     Scratch scratch;
     float *work = nullptr;
     if (states + parts > 0) {
-        rc = scratch.get(ctx, (size_t)(states + parts * (K + V)) * sizeof(float), st, &work);
+        const int rc = scratch.get(ctx, (size_t)(states + parts * (K + V)) * sizeof(float), st, &work);
         if (rc != SIG_OK) return rc;
     }
     if (!shared) return status(launch(a, 3, s.type, s.type, work, cus, true, st));
@@ -220,6 +208,65 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     if (e == hipSuccess) e = add_up(part_k, grad_k, K);
     if (e == hipSuccess) e = add_up(part_v, grad_v, V);
     return status(e);
+}
+
+// p + count values of `bytes`; null stays null
+template <typename P>
+P *behind(P *p, int64_t count, int64_t bytes)
+{
+    using Byte = std::conditional_t<std::is_const_v<P>, const char, char>;
+    return p ? (P *)((Byte *)p + count * bytes) : p;
+}
+
+// f(slice of the shape, its first batch element) for slices of at most `most` of them, until one fails
+template <typename F>
+int in_slices(const sig_attention_t &s, int64_t most, F f)
+{
+    sig_attention_t part = s;
+    for (int64_t b = 0; b < s.B; b += most) {
+        part.B = s.B - b < most ? s.B - b : most;
+        if (const int rc = f(part, b)) return rc;
+    }
+    return SIG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v, const float *log_decay,
+                         const float *state, const int64_t *lengths, void *out, float *state_out, void *hip_stream)
+{
+    const int rc = check(ctx, shape);
+    if (rc != SIG_OK) return rc;
+    const sig_attention_t &s = *shape;
+    if (s.B == 0 || (s.T == 0 && !state_out)) return SIG_OK;
+    if (!log_decay || (s.T > 0 && (!q || !k || !v || !out))) return SIG_ERR_INVALID;
+    const int64_t bytes = type_bytes(s.type), state_size = (int64_t)s.heads * s.key_dim * s.value_dim;
+    return in_slices(s, kMostWorkgroups / s.heads, [&](const sig_attention_t &part, int64_t b) {
+        return forward(ctx, part, behind(q, b * s.q_strides[0], bytes), behind(k, b * s.k_strides[0], bytes), behind(v, b * s.v_strides[0], bytes), log_decay,
+                       behind(state, b * state_size, 4), behind(lengths, b, 8), behind(out, b * s.T * s.heads * s.value_dim, bytes),
+                       behind(state_out, b * state_size, 4), (hipStream_t)hip_stream);
+    });
+}
+
+int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
+                                  const float *log_decay, const float *state, const int64_t *lengths, const void *grad_out,
+                                  const float *grad_state, void *grad_q, void *grad_k, void *grad_v, float *grad_initial, void *hip_stream)
+{
+    const int rc = check(ctx, shape);
+    if (rc != SIG_OK) return rc;
+    const sig_attention_t &s = *shape;
+    if (s.B == 0 || (s.T == 0 && !grad_initial)) return SIG_OK;
+    if (!log_decay || (s.T > 0 && (!q || !k || !v || !grad_out || !grad_q || !grad_k || !grad_v))) return SIG_ERR_INVALID;
+    const int64_t bytes = type_bytes(s.type), state_size = (int64_t)s.heads * s.key_dim * s.value_dim;
+    return in_slices(s, kMostWorkgroups / s.heads, [&](const sig_attention_t &part, int64_t b) {
+        return backward(ctx, part, behind(q, b * s.q_strides[0], bytes), behind(k, b * s.k_strides[0], bytes), behind(v, b * s.v_strides[0], bytes), log_decay,
+                        behind(state, b * state_size, 4), behind(lengths, b, 8), behind(grad_out, b * s.T * s.heads * s.value_dim, bytes),
+                        behind(grad_state, b * state_size, 4), behind(grad_q, b * s.T * s.heads * s.key_dim, bytes),
+                        behind(grad_k, b * s.T * s.shared_heads * s.key_dim, bytes), behind(grad_v, b * s.T * s.shared_heads * s.value_dim, bytes),
+                        behind(grad_initial, b * state_size, 4), (hipStream_t)hip_stream);
+    });
 }
 
 }  // extern "C"

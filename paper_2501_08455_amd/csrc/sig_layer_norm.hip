@@ -539,9 +539,13 @@ void with_lanes(int64_t width, F f)
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int launched() { return hipGetLastError() == hipSuccess ? SIG_OK : SIG_ERR_HIP; }
 
+// A launch holds fewer than 2^32 threads: workgroups that walk over short rows are as many as the card has use for, long rows' pieces and the
+// columns of the weights' gradients are one each.
 bool too_large(int64_t rows, int64_t width)
 {
-    return rows > 0 && (width > INT64_MAX / 16 / rows || ceil_div(width, kPiece) > INT32_MAX / rows || ceil_div(width, kThreads) > INT32_MAX);
+    constexpr int64_t kMost = (int64_t)1 << 32;
+    if (rows == 0) return 2 * width > kMost - 1024;
+    return width > INT64_MAX / 16 / rows || (width > kLongest && ceil_div(width, kPiece) > (kMost - 1) / kThreads / rows);
 }
 
 }  // namespace

@@ -62,7 +62,8 @@ __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, 
     __shared__ float2 table[kTable];
     __shared__ int64_t from[kMostTokens], to[kMostTokens];
     const int half = (int)A.turned / 2, dim = (int)A.dim, turned = (int)A.turned, heads = (int)A.heads;
-    const int64_t first = (int64_t)blockIdx.x * A.tokens, all = A.B * A.T;
+    const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * A.tokens, all = A.B * A.T;
+    if (first >= all) return;
     const int tokens = all - first < A.tokens ? (int)(all - first) : A.tokens;
     for (int i = threadIdx.x; i < tokens * half || i < tokens; i += kThreads) {
         if (i < tokens) {
@@ -168,7 +169,9 @@ extern "C" int sig_rotary(sig_ctx *ctx, const void *x, const int64_t *x_strides,
     const int64_t share = B * T / (8 * (int64_t)ctx->num_cu), room = turned ? kTable / (turned / 2) : kMostTokens;
     A.tokens = (int)(share < 1 ? 1 : share < kMostTokens ? share : kMostTokens);
     if (A.tokens > room) A.tokens = (int)room;
-    const unsigned grid = (unsigned)((B * T + A.tokens - 1) / A.tokens);
+    // (a launch holds fewer than 2^32 threads along an axis)
+    const int64_t blocks = (B * T + A.tokens - 1) / A.tokens, most = ((int64_t)1 << 31) / kThreads;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)((blocks + most - 1) / most));
     with_type(type, [&](auto t) {
         using E = typename decltype(t)::type;
         auto go = [&](auto n) {

@@ -1,0 +1,70 @@
+"""What the sequence operators' entry points launch for a call, on the CPU (tests/host_sequence_launches.cpp): the limits that a launch
+has, and the kernels that the rules of linear attention choose."""
+import re
+
+import pytest
+
+from paper_2501_08455_amd import binding
+from test_host_sanitized import linked, run   # noqa: F401 (a fixture)
+
+F32, BF16, F16 = binding.SIG_F32, binding.SIG_BF16, binding.SIG_F16
+OK, LARGE = binding.SIG_OK, binding.SIG_ERR_TOO_LARGE
+
+
+class Launch:
+    def __init__(self, words):
+        self.kernel, *sizes = words.split(",")
+        self.grid, self.threads = tuple(int(n) for n in sizes[:3]), int(sizes[3])
+        self.workgroups = self.grid[0] * self.grid[1] * self.grid[2]
+
+
+@pytest.fixture(scope="module")
+def launches(linked):   # noqa: F811
+    """launches(calls): (status, most bytes asked for, launches) of each"""
+    exe = linked("host_sequence_launches.cpp")
+
+    def answers(calls):
+        lines = run(exe, calls="".join(" ".join(str(word) for word in call) + "\n" for call in calls)).splitlines()
+        assert len(lines) == len(calls)
+        return [(int(line.split()[0]), int(line.split()[1]), [Launch(w) for w in line.split()[2:]]) for line in lines]
+
+    return answers
+
+
+def within_limits(launch):
+    """A launch holds fewer than 2^32 threads along an axis, and up to 65,535 workgroups along the second and third."""
+    return launch.grid[0] * launch.threads < 1 << 32 and launch.grid[1] < 1 << 16 and launch.grid[2] < 1 << 16
+
+
+HUGE = [("rotary", 1 << 14, 1 << 14, 1, 2, 2, BF16), ("rotary", 1, (1 << 28) + 5, 1, 8, 4, BF16), ("rotary", (1 << 24) + 1, 1, 1, 4096, 4096, BF16),
+        ("rotary", 1, (1 << 31) - 1, 1, 2, 0, BF16)]
+HUGE += [(way, *shape, kind) for way in ("forward", "backward") for kind in (F32, BF16)
+         for shape in (((1 << 24) + 3, 1, 1, 1, 1, 1), ((1 << 24) + 3, 40, 1, 1, 8, 8), (1 << 23, 5, 4, 2, 4, 100), ((1 << 31) - 1, 1, 1, 1, 2, 1),
+                       (1 << 21, 3, 9, 3, 200, 1), (1, 70, (1 << 24) - 1, 1, 4, 4))]
+
+
+def test_no_launch_is_larger_than_launches_are(launches):
+    for call, (rc, _, got) in zip(HUGE, launches(HUGE)):
+        assert rc == OK and got, call
+        for launch in got:
+            assert within_limits(launch), (call, launch.kernel, launch.grid, launch.threads)
+
+
+def test_what_no_launch_can_hold_is_refused(launches):
+    calls = [(way, 1, 70, 1 << 24, 1, 4, 4, F32) for way in ("forward", "backward")]
+    calls += [(way, 1 << 20, 1 << 17, F32) for way in ("norm", "norm_backward")] + [("norm_backward", 0, 1 << 31, F32), ("rotary", 1 << 16, 1 << 15, 1, 2, 2, F32)]
+    for call, (rc, _, got) in zip(calls, launches(calls)):
+        assert rc == LARGE and not got, (call, rc)
+
+
+def test_slices_of_a_batch_hold_all_of_it(launches):
+    """Token by token a workgroup is a head's 64 columns: as many of them as there are, over all launches of a pass."""
+    B, H, V = (1 << 23) + 7, 5, 130
+    ((rc, _, got),) = launches([("forward", B, 1, H, H, 4, V, F32)])
+    assert rc == OK and len(got) > 1
+    assert sum(launch.workgroups for launch in got) == B * H * 3 and all("recurrent" in launch.kernel for launch in got)
+
+
+def test_rows_of_any_number_are_normalised(launches):
+    for rc, _, got in launches([("norm", 1 << 33, 2, BF16), ("norm_backward", 1 << 33, 2, BF16), ("norm", 1 << 15, 16385, F32)]):
+        assert rc == OK and got and all(within_limits(launch) for launch in got)
