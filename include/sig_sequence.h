@@ -107,7 +107,7 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
  *                shared head is the sum over the heads that read it
  *   grad_initial DEVICE, float32, gradient with respect to `state`; may be NULL; overlaps no other argument
  * Context scratch as above, for up to three passes at once; and where heads share keys and values, B * T * heads * (key_dim + value_dim)
- * floats for what is added up.
+ * floats for what is added up (a batch for which that exceeds 8 GiB is taken in slices that share the scratch).
  */
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
                                   const float *log_decay, const float *state, const int64_t *lengths, const void *grad_out,

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostDim = 256;
+constexpr int64_t kMostParts = (int64_t)8 << 30;                            // bytes of scratch for shared heads' gradients
 constexpr int64_t kMostWorkgroups = ((int64_t)1 << 32) / kThreads - 1;      // along an axis: a launch holds fewer than 2^32 threads there
 
 // out[token][shared head][.] = sum over the heads of a shared head of part[token][head][.], in their order.  `lanes` threads (a power
@@ -260,7 +261,12 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
     if (s.B == 0 || (s.T == 0 && !grad_initial)) return SIG_OK;
     if (!log_decay || (s.T > 0 && (!q || !k || !v || !grad_out || !grad_q || !grad_k || !grad_v))) return SIG_ERR_INVALID;
     const int64_t bytes = type_bytes(s.type), state_size = (int64_t)s.heads * s.key_dim * s.value_dim;
-    return in_slices(s, kMostWorkgroups / s.heads, [&](const sig_attention_t &part, int64_t b) {
+    int64_t most = kMostWorkgroups / s.heads;
+    if (s.heads > s.shared_heads && s.T > 0) {
+        const int64_t room = kMostParts / (4 * s.T * s.heads * (s.key_dim + s.value_dim));
+        if (room < most) most = room < 1 ? 1 : room;
+    }
+    return in_slices(s, most, [&](const sig_attention_t &part, int64_t b) {
         return backward(ctx, part, behind(q, b * s.q_strides[0], bytes), behind(k, b * s.k_strides[0], bytes), behind(v, b * s.v_strides[0], bytes), log_decay,
                         behind(state, b * state_size, 4), behind(lengths, b, 8), behind(grad_out, b * s.T * s.heads * s.value_dim, bytes),
                         behind(grad_state, b * state_size, 4), behind(grad_q, b * s.T * s.heads * s.key_dim, bytes),

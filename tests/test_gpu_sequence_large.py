@@ -45,3 +45,22 @@ def test_linear_attention_of_more_heads_than_a_launch_has_workgroups(B, H, G, T)
     want = attention_reference(q[at], k[at], v[at], log_decay, state[at], lengths[at], K ** -0.5, g[at], g_state[at])
     for a, b, name in zip(got, want, ("o", "state", "grad q", "grad k", "grad v", "grad state")):
         assert_near(a[at], b, what=name)
+
+
+@gpu
+def test_shared_heads_gradients_in_slices_of_the_batch():
+    """More scratch than a call takes at once: the last slice's gradients as those of a call of their own (which cuts sequences otherwise, so that
+    sums differ before they are rounded)."""
+    B, T, H, G, K = 9, 65536, 16, 4, 128
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v, g = (torch.randn(B, T, n, K, device="cuda", generator=gen).bfloat16() for n in (H, G, G, H))
+    log_decay = torch.log1p(-torch.exp2(-2.0 - 6.0 * torch.arange(H, device="cuda") / H))
+
+    def gradients(*ins):
+        ins = [t.detach().requires_grad_(True) for t in ins[:3]] + [ins[3]]
+        return torch.autograd.grad(autograd.linear_attention(*ins[:3], log_decay), ins[:3], ins[3])
+
+    got = gradients(q, k, v, g)
+    for b in (0, B - 2, B - 1):
+        for x, y in zip(got, gradients(*(t[b:b + 1] for t in (q, k, v, g)))):
+            assert float((x[b] - y[0]).float().norm()) <= 2.0 ** -8 * float(y.float().norm())

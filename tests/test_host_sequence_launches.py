@@ -68,3 +68,17 @@ def test_slices_of_a_batch_hold_all_of_it(launches):
 def test_rows_of_any_number_are_normalised(launches):
     for rc, _, got in launches([("norm", 1 << 33, 2, BF16), ("norm_backward", 1 << 33, 2, BF16), ("norm", 1 << 15, 16385, F32)]):
         assert rc == OK and got and all(within_limits(launch) for launch in got)
+
+
+def test_shared_heads_gradients_take_no_more_than_8_gib_of_scratch(launches):
+    """... by slices of the batch, each with all launches of the gradient."""
+    small, large, one = ("backward", 8, 4096, 16, 4, 128, 128, BF16), ("backward", 100, 65536, 16, 4, 128, 128, BF16), ("backward", 1, 1 << 20, 16, 4, 128, 128, BF16)
+    (a, few, whole), (b, many, cut), (c, most, single) = launches([small, large, one])
+    assert a == b == c == OK
+    parts = 4 * 16 * 256
+    assert 8 * 4096 * parts <= few < 8 * 4096 * parts + (1 << 28)
+    # a batch element of the second takes 1 GiB: slices of eight
+    assert 8 * 65536 * parts <= many < (8 << 30) + (1 << 28)
+    assert sum("sig_attention_share" in launch.kernel for launch in cut) == 2 * 13 and sum("sig_attention_share" in launch.kernel for launch in whole) == 2
+    # a single sequence cannot be taken apart
+    assert (1 << 20) * parts <= most and sum("sig_attention_share" in launch.kernel for launch in single) == 2
