@@ -48,19 +48,26 @@ struct Cut {
 //     1,024 tokens                 81; 107                      62; 123         82; 195
 //   f32, 128 x 128, 128 heads, 1,024 tokens   198; 353          129; 328        164; 438
 // Workgroups of 128 columns, which share the operands' loads and the pairs of a chunk, where they are more than the units (float32, bound by
-// its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that, and small states' long sequences of
-// less than two a unit (50 sequences of 2,048 tokens, 4 heads of 64 x 64 bfloat16: 94 whole, 79 cut; of 192 x 64 float32 386 whole, 415
-// cut, of 256 x 64 452 and 511), are cut along time, which costs a second read of y and z, the segments' states and two more launches
-// (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64
-// segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of such workgroups at once: two, or three of small
-// states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two, 98 for three).
+// its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that are cut along time, which costs a
+// second read of y and z, the segments' states and two more launches (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and
+// 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64 segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of
+// such workgroups at once: two, or three of small states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two,
+// 98 for three).
+// Long sequences of less than two workgroups of 64 columns a unit are cut too, where that pays.  Whole; cut as the rule has it (us):
+//   bf16, heads   200 of 64 x 64   256 of 64 x 64   256 of 96 x 64   200 of 128 x 64   128 of 128 x 128   140 of 128 x 128   200 of 128 x 128
+//   1,024 tokens  56; 56           53; 58           64; 73           69; 78            66; 87             -                  -
+//   2,048         99; 84           95; 91           124; 124         130; 127          120; 128           148; 150           -
+//   4,096         199; 161         208; 176         240; 219         250; 229          258; 221           294; 268           303; 349 in two
+//   8,192         391; 329         396; 343         472; 441         488; 438          481; 408           -                  -
+// (192 and 256 rows 311; 305 and 338; 394 at 4,096 tokens)
 Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
-    bool wide = false, small = true;
+    bool wide = false, small = true, low = true;
     for (int i = 0; i < passes; ++i) {
         wide = wide || (a[i].columns > 64 && a[i].rows <= 128);      // (registers)
         small = small && a[i].rows <= (type == SIG_BF16 ? 64 : 96);
+        low = low && a[i].rows <= 128;
     }
     auto workgroups = [&](int nv) {
         int64_t n = 0;
@@ -69,9 +76,12 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     };
     Cut cut = {wide && 4 * workgroups(2) >= (type == SIG_BF16 ? 5 : 8) * cus ? 2 : 1, 1, a[0].T};
     const int64_t chunks = (a[0].T + chunk - 1) / chunk, n = workgroups(cut.nv);
-    if (4 * n < 3 * cus || (small && cut.nv == 1 && n < 2 * cus && chunks >= (type == SIG_BF16 ? 32 : 48))) {
+    const auto filling = [&](int nv) { return (small && nv == 1 ? 3 : 2) * cus / workgroups(nv); };      // segments: that many workgroups a unit
+    const bool few = 4 * n < 3 * cus, less = !few && cut.nv == 1 && n < 2 * cus;
+    const bool pays = type == SIG_BF16 ? small ? chunks >= 32 : low && chunks >= 48 && (!wide || filling(2) >= 3) : small && chunks >= 48;
+    if (few || (less && pays)) {
         if (wide) cut.nv = 2;
-        int64_t segments = (small && cut.nv == 1 ? 3 : 2) * cus / workgroups(cut.nv);      // (that many workgroups a unit)
+        int64_t segments = filling(cut.nv);
         if (segments > chunks / 4) segments = chunks / 4;
         if (segments < 1) segments = 1;
         const int64_t each = (chunks + segments - 1) / segments;

@@ -82,3 +82,32 @@ def test_shared_heads_gradients_take_no_more_than_8_gib_of_scratch(launches):
     assert sum("sig_attention_share" in launch.kernel for launch in cut) == 2 * 13 and sum("sig_attention_share" in launch.kernel for launch in whole) == 2
     # a single sequence cannot be taken apart
     assert (1 << 20) * parts <= most and sum("sig_attention_share" in launch.kernel for launch in single) == 2
+
+
+class Chunks:
+    """How a call's chunk launches are cut: tiles of 16 columns a wavefront (64 nv columns a workgroup) and segments along time."""
+
+    def __init__(self, launched, passes=1):
+        found = [(re.search(r"Li(\d+)ELi(\d+)ELi(\d+)ELb([01])E", launch.kernel), launch) for launch in launched if "attention_chunk" in launch.kernel]
+        (sizes, launch), = [x for x in found if x[0].group(4) == "1"]      # the launch with output
+        self.columns, self.segments, self.workgroups = 64 * int(sizes.group(3)), launch.grid[2] // passes, launch.workgroups
+        assert len(found) == (2 if self.segments > 1 else 1)
+
+
+# B, T, heads, K, V, type: whether a sequence is cut along time.  256 compute units
+CUT = [
+    # as many workgroups of 64 columns as units, or up to twice as many: bfloat16 states of 128 rows, long sequences, where three segments of 128 columns fit
+    ((8, 4096, 16, 128, 128, BF16), 4), ((1, 8192, 100, 128, 128, BF16), 5), ((1, 4096, 140, 128, 128, BF16), 3), ((1, 4096, 200, 128, 128, BF16), 1),
+    ((8, 2048, 16, 128, 128, BF16), 1), ((1, 4096, 200, 128, 64, BF16), 2), ((1, 4096, 256, 96, 64, BF16), 2), ((1, 4096, 300, 128, 64, BF16), 1),
+    ((1, 8192, 256, 256, 64, BF16), 1), ((1, 8192, 128, 192, 128, BF16), 1),
+    # small ones from 2,048 tokens on
+    ((50, 2048, 4, 64, 64, BF16), 3), ((50, 1024, 4, 64, 64, BF16), 1),
+    # float32 states of more than 96 rows
+    ((50, 2048, 4, 128, 64, F32), 1), ((50, 2048, 4, 192, 64, F32), 1), ((50, 2048, 4, 256, 64, F32), 1),
+]
+
+
+def test_sequences_are_cut_where_that_was_measured_to_pay(launches):
+    got = launches([("forward", B, T, H, H, K, V, kind) for (B, T, H, K, V, kind), _ in CUT])
+    wrong = [(call, segments, Chunks(launched).segments) for (call, segments), (rc, _, launched) in zip(CUT, got) if rc != OK or Chunks(launched).segments != segments]
+    assert not wrong, wrong
