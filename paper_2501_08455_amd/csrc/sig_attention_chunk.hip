@@ -59,7 +59,9 @@ struct Cut {
 //   2,048         99; 84           95; 91           124; 124         130; 127          120; 128           148; 150           -
 //   4,096         199; 161         208; 176         240; 219         250; 229          258; 221           294; 268           303; 349 in two
 //   8,192         391; 329         396; 343         472; 441         488; 438          481; 408           -                  -
-// (192 and 256 rows 311; 305 and 338; 394 at 4,096 tokens)
+// (192 and 256 rows 311; 305 and 338; 394 at 4,096 tokens.)  Float32 of at most 64 columns only beyond one workgroup a unit, whose second
+// round is then shared out (4,096 tokens: 200 heads of 64 x 64 323; 332, 256 of 96 x 64 432; 457, 280 of 64 x 64 492; 470), of more also
+// below (100 heads of 64 x 128 320; 274).
 Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
@@ -78,7 +80,7 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     const int64_t chunks = (a[0].T + chunk - 1) / chunk, n = workgroups(cut.nv);
     const auto filling = [&](int nv) { return (small && nv == 1 ? 3 : 2) * cus / workgroups(nv); };      // segments: that many workgroups a unit
     const bool few = 4 * n < 3 * cus, less = !few && cut.nv == 1 && n < 2 * cus;
-    const bool pays = type == SIG_BF16 ? small ? chunks >= 32 : low && chunks >= 48 && (!wide || filling(2) >= 3) : small && chunks >= 48;
+    const bool pays = type == SIG_BF16 ? small ? chunks >= 32 : low && chunks >= 48 && (!wide || filling(2) >= 3) : small && chunks >= 48 && (wide || n > cus);
     if (few || (less && pays)) {
         if (wide) cut.nv = 2;
         int64_t segments = filling(cut.nv);

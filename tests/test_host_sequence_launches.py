@@ -111,3 +111,11 @@ def test_sequences_are_cut_where_that_was_measured_to_pay(launches):
     got = launches([("forward", B, T, H, H, K, V, kind) for (B, T, H, K, V, kind), _ in CUT])
     wrong = [(call, segments, Chunks(launched).segments) for (call, segments), (rc, _, launched) in zip(CUT, got) if rc != OK or Chunks(launched).segments != segments]
     assert not wrong, wrong
+
+
+def test_float32_sequences_of_one_workgroup_a_unit_stay_whole(launches):
+    """... where that is 64 columns each; more workgroups than units, or wider states, are cut."""
+    shapes = [((200, 64, 64), 1), ((256, 64, 64), 1), ((256, 96, 64), 1), ((280, 64, 64), 2), ((100, 64, 128), 5), ((400, 64, 64), 1)]
+    got = launches([("forward", 1, 4096, H, H, K, V, F32) for (H, K, V), _ in shapes])
+    for (shape, segments), (rc, _, launched) in zip(shapes, got):
+        assert rc == OK and Chunks(launched).segments == segments, (shape, Chunks(launched).segments)
