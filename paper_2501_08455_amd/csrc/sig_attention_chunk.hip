@@ -52,7 +52,9 @@ struct Cut {
 // second read of y and z, the segments' states and two more launches (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and
 // 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64 segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of
 // such workgroups at once: two, or three of small states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two,
-// 98 for three).
+// 98 for three), of four chunks or more.  Segments are of 128 columns where a sequence has enough of those, nearly, to fill the units, else of
+// 64 (2 to 64 heads of 128 x 128 bfloat16: 300 tokens 30; 23, 1,000 tokens 47 to 58; 34 to 51, 8 heads of 8,000 62; 55; float32 300
+// tokens 60 to 68; 42 to 49).
 // Long sequences of less than two workgroups of 64 columns a unit are cut too, where that pays.  Whole; cut as the rule has it (us):
 //   bf16, heads   200 of 64 x 64   256 of 64 x 64   256 of 96 x 64   200 of 128 x 64   128 of 128 x 128   140 of 128 x 128   200 of 128 x 128
 //   1,024 tokens  56; 56           53; 58           64; 73           69; 78            66; 87             -                  -
@@ -82,7 +84,7 @@ Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
     const bool few = 4 * n < 3 * cus, less = !few && cut.nv == 1 && n < 2 * cus;
     const bool pays = type == SIG_BF16 ? small ? chunks >= 32 : low && chunks >= 48 && (!wide || filling(2) >= 3) : small && chunks >= 48 && (wide || n > cus);
     if (few || (less && pays)) {
-        if (wide) cut.nv = 2;
+        if (wide && 5 * (chunks / 4) >= 4 * filling(2)) cut.nv = 2;
         int64_t segments = filling(cut.nv);
         if (segments > chunks / 4) segments = chunks / 4;
         if (segments < 1) segments = 1;

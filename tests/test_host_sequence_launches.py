@@ -119,3 +119,14 @@ def test_float32_sequences_of_one_workgroup_a_unit_stay_whole(launches):
     got = launches([("forward", 1, 4096, H, H, K, V, F32) for (H, K, V), _ in shapes])
     for (shape, segments), (rc, _, launched) in zip(shapes, got):
         assert rc == OK and Chunks(launched).segments == segments, (shape, Chunks(launched).segments)
+
+
+def test_short_sequences_of_few_heads_keep_their_workgroups(launches):
+    """64 columns a workgroup where time has too few pieces for 128 to fill the units: twice the workgroups for the units that idle."""
+    shapes = [((4, 192, 8, BF16), 64, 1), ((1, 300, 8, F32), 64, 2), ((1, 1000, 24, BF16), 64, 4), ((1, 8000, 8, BF16), 64, 25), ((1, 65536, 8, BF16), 128, 64),
+              ((1, 4096, 48, BF16), 128, 10), ((1, 16384, 8, F32), 128, 64)]
+    got = launches([("forward", B, T, H, H, 128, 128, kind) for (B, T, H, kind), _, _ in shapes])
+    for (shape, columns, segments), (rc, _, launched) in zip(shapes, got):
+        cut = Chunks(launched)
+        assert rc == OK and (cut.columns, cut.segments) == (columns, segments), (shape, cut.columns, cut.segments)
+        assert cut.workgroups == shape[0] * shape[2] * 128 // columns * segments
