@@ -18,8 +18,10 @@
 // products (32 tokens: training 698 us), but 32 where the state has 256 rows (LDS then holds two workgroups) or sequences are short; 32 of float32.
 //
 // A product of matrices multiplies every pair: 0 x infinity where the triangle is empty, and the parts of an infinite number.  A chunk
-// whose output is not finite is therefore worked out again token by token, so that what is not a number reaches what it
-// reaches in the recurrence (launches without output: the whole segment, if its state is not finite).
+// whose output is not finite is therefore worked out again token by token, by the wavefronts of those columns, so that what is not a number
+// reaches what it reaches in the recurrence.  Behind it chunks go on as chunks, unless something in the state is not finite: that lasts, and
+// the rest of the segment goes token by token (8 x 4,096 tokens, 16 heads of 128 x 128 bfloat16, forward: an infinite query in each 619 us, an infinite
+// key 11.5 ms, neither 235).  Launches without output: the whole segment, if its state is not finite.
 #ifndef SIG_ATTENTION_CHUNK_H
 #define SIG_ATTENTION_CHUNK_H
 
@@ -61,30 +63,31 @@ struct TileLoader {
     const T *p;          // of the next tile
     int64_t stride;      // between tokens
     int width;           // values of a token
-    bool there;
-    Pack<T, GROUP> held[COUNT];
+    struct Tile { Pack<T, GROUP> held[COUNT]; };      // a thread's part, on its way
 
-    static __device__ int row() { return threadIdx.x / (WIDE / GROUP); }
-    static __device__ int place() { return threadIdx.x % (WIDE / GROUP) * GROUP; }
+    static __device__ int row_of(int thread) { return thread / (WIDE / GROUP); }
+    static __device__ int place_of(int thread) { return thread % (WIDE / GROUP) * GROUP; }
 
     // token 0 of the first tile is at `tokens`
     __device__ TileLoader(const T *tokens, int64_t stride_, int width_) : stride(stride_), width(width_)
     {
-        there = place() + GROUP <= width;
-        p = tokens + row() * stride + (there ? place() : 0);
+        const int row = row_of(threadIdx.x), place = place_of(threadIdx.x);
+        p = tokens + row * stride + (place + GROUP <= width ? place : 0);
     }
-    // the next tile, of which 1 <= n <= C tokens are there
-    __device__ void load(int n)
+    // the next tile, of which 1 <= n <= C tokens are there; thread: threadIdx.x
+    __device__ void load(Tile &tile, int n, int thread)
     {
-        if (width >= GROUP) {
+        int values = width;
+        asm volatile("" : "+s"(values));      // (compared anew: the answer would be kept in a register of every lane)
+        if (values >= GROUP) {
             if (n == C) {
 #pragma unroll
-                for (int i = 0; i < COUNT; ++i) held[i] = *(const Pack<T, GROUP> *)(p + i * ROWS * stride);
+                for (int i = 0; i < COUNT; ++i) tile.held[i] = *(const Pack<T, GROUP> *)(p + i * ROWS * stride);
             } else {
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i) {
-                    const int r = row() + i * ROWS;
-                    held[i] = *(const Pack<T, GROUP> *)(p + ((r < n ? r : n - 1) - row()) * stride);
+                    const int r = row_of(thread) + i * ROWS;
+                    tile.held[i] = *(const Pack<T, GROUP> *)(p + ((r < n ? r : n - 1) - row_of(thread)) * stride);
                 }
             }
         }
@@ -92,29 +95,31 @@ struct TileLoader {
     }
     // the last tile again
     __device__ void back() { p -= C * stride; }
-    // the tile of the last load(n)
-    __device__ void store(E *tile, int pitch, int n) const
+    // the tile of the last load(from, n, thread)
+    __device__ void store(const Tile &from, E *tile, int pitch, int n, int thread) const
     {
+        const int row = row_of(thread), place = place_of(thread);
+        const bool there = place + GROUP <= width;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            const int r = row() + i * ROWS;
+            const int r = row + i * ROWS;
             const bool ok = there && r < n;
             struct { E v[GROUP]; } values;
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) values.v[j] = (E)held[i].v[j];
+            for (int j = 0; j < GROUP; ++j) values.v[j] = (E)from.held[i].v[j];
             using u4 = __attribute__((ext_vector_type(4))) unsigned;
             u4 bits = __builtin_bit_cast(u4, values);
             bits = ok ? bits : u4{};
-            if (W == WIDE || place() < W) *(u4 *)(tile + r * pitch + place()) = bits;
+            if (W == WIDE || place < W) *(u4 *)(tile + r * pitch + place) = bits;
         }
         // the last values of tokens that are no whole number of groups (after the zeros of the same thread, which then reads from place 0)
-        const int rest = width % GROUP, c = place();
+        const int rest = width % GROUP, c = place;
         if (width < W && rest && c < width && c + GROUP > width) {
-            const T *from = p - C * stride + c;
+            const T *last = p - C * stride + c;
 #pragma unroll 1
-            for (int r = row(); r < n; r += ROWS, from += ROWS * stride)
+            for (int r = row; r < n; r += ROWS, last += ROWS * stride)
 #pragma unroll 1
-                for (int j = 0; j < rest; ++j) tile[r * pitch + c + j] = (E)from[j];
+                for (int j = 0; j < rest; ++j) tile[r * pitch + c + j] = (E)last[j];
         }
     }
 };
@@ -190,19 +195,18 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     if ((int)blockIdx.y * VT >= A.columns) return;
     __shared__ __attribute__((aligned(16))) E xs[OUTPUT ? C * XPITCH : 8], ys[C * YPITCH], zs[C * ZPITCH];
     __shared__ Frag triangle[OUTPUT ? MT * STEPS * SPLIT * 64 : 1];
-    __shared__ int spoilt;                        // whether a wavefront has met what is not finite
+    __shared__ int spoilt, lasting;               // whether a wavefront has met what is not finite in a chunk, and in the state
     __shared__ float after[C + 2];                // out_scale l^(i+1)
     __shared__ float gap_weight[C + 16];          // out_scale update_scale l^(i-15), zeros up to i = 14
     __shared__ float left_weight[2 * C];          // update_scale l^(C-1-i+e), zeros from i = C on
 
     const int64_t head = blockIdx.x % A.heads, b = blockIdx.x / A.heads;
-    const int lane = threadIdx.x % 64, line = lane % 16, quad = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int c0 = blockIdx.y * VT, width = A.columns - c0, column = wave * 16 * NV + line;     // of the workgroup, and of the lane in it
+    const int c0 = blockIdx.y * VT, width = A.columns - c0;
     const int64_t length = attention_length(A, b), first = segment * G.segment_tokens;
     const int64_t last = first + G.segment_tokens < length && segment + 1 < G.segments ? first + G.segment_tokens : length;
     const float g = A.log_decay[head];
-    if (threadIdx.x == 0) spoilt = 0;
+    if (threadIdx.x == 0) spoilt = lasting = 0;
     const auto power = [&](int i) { return i == 0 ? 1.0f : expf((float)i * g); };
     if (OUTPUT) {
         for (int i = threadIdx.x; i < C + 2; i += THREADS) after[i] = A.out_scale * power(i);
@@ -220,8 +224,24 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     const T *z = (const T *)A.z + b * A.zs[0] + head / A.z_group * A.zs[2] + start * A.zs[1] + c0;
     O *o = (O *)A.o + b * A.os[0] + head * A.os[2] + start * A.os[1] + c0;
 
-    // the state: tile (kt, nv) holds, in a lane, its column at rows first_row + row_of(kt) + 0..3
-    const int first_row = 4 * SUB * quad;
+    // The state: tile (kt, nv) holds, in a lane, its column at rows first_row + row_of(kt) + 0..3.  Each part of the kernel works its places out
+    // anew, from a lane's number that the compiler takes for another one each time: it would keep them, and what follows from them, in registers
+    // that the loop over chunks does not have.
+    struct Place {
+        int lane, thread, line, quad, first_row, column;      // the last four of the lane's tiles, the column in the workgroup's
+
+        __device__ explicit Place(int wave)
+        {
+            int all = -1;
+            asm volatile("" : "+s"(all));
+            lane = __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
+            thread = 64 * wave + lane;
+            line = lane % 16;
+            quad = lane / 16;
+            first_row = 4 * SUB * quad;
+            column = wave * 16 * NV + line;
+        }
+    };
     const auto row_of = [](int kt) { return kt / SUB * M::STEP + 4 * (kt % SUB); };
     f4 s[KT][NV];
     const int64_t head_state = (int64_t)A.rows * A.columns, at_head = (int64_t)b * A.heads + head;
@@ -230,6 +250,7 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     const bool copied = segment == 0 && G.segments > 1 && A.state && A.state == A.state_out, own = segment > 0 || copied;
     const float *from = own ? kept + (copied ? G.segments - 1 : -1) * A.B * A.heads * head_state : A.state ? A.state + at_head * head_state : nullptr;
     float *state_to = !OUTPUT ? kept : segment + 1 == G.segments && A.state_out ? A.state_out + at_head * head_state : nullptr;
+    const Place before(wave);
 #pragma unroll
     for (int nv = 0; nv < NV; ++nv) {
         if constexpr (!OUTPUT) {
@@ -237,8 +258,8 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
             for (int kt = 0; kt < KT; ++kt) s[kt][nv] = f4{};
         } else {
             const int64_t row_stride = own ? A.columns : A.row_stride, column_stride = own ? 1 : A.column_stride;
-            const float *at = from + first_row * row_stride + (c0 + column + 16 * nv) * column_stride;
-            int rows = from && column + 16 * nv < width ? A.rows - first_row : 0;
+            const float *at = from + before.first_row * row_stride + (c0 + before.column + 16 * nv) * column_stride;
+            int rows = from && before.column + 16 * nv < width ? A.rows - before.first_row : 0;
             asm volatile("" : "+v"(rows));
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
@@ -249,208 +270,26 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
 
     TileLoader<T, E, C, K, THREADS> xl(x + first * xstep, xstep, A.rows), yl(y + first * ystep, ystep, A.rows);
     TileLoader<T, E, C, VT, THREADS> zl(z + first * zstep, zstep, width);
-    auto load = [&](int64_t t) {
+    using StateTile = typename TileLoader<T, E, C, K, THREADS>::Tile;
+    using ValueTile = typename TileLoader<T, E, C, VT, THREADS>::Tile;
+    auto load = [&](StateTile &xt, StateTile &yt, ValueTile &zt, int64_t t, int thread) {
         const int n = last - t < C ? (int)(last - t) : C;
-        if (OUTPUT) xl.load(n);
-        yl.load(n);
-        zl.load(n);
+        if (OUTPUT) xl.load(xt, n, thread);
+        yl.load(yt, n, thread);
+        zl.load(zt, n, thread);
     };
-    if (first < last) load(first);
+    auto store = [&](const StateTile &xt, const StateTile &yt, const ValueTile &zt, int n, int thread) {
+        if (OUTPUT) xl.store(xt, xs, XPITCH, n, thread);
+        yl.store(yt, ys, YPITCH, n, thread);
+        zl.store(zt, zs, ZPITCH, n, thread);
+    };
     __syncthreads();
 
-    O *to = o + (first + line) * ostep + wave * 16 * NV + 4 * quad;      // the lane's outputs of the next chunk
     // Loads from LDS are issued a block of products ahead (left alone, the compiler waits for each in turn), and the splitting of the
     // next operand goes between the products: a product keeps its unit busy for four vector instructions.
     int64_t t0 = first;
     bool again = false;          // OUTPUT: whether this wavefront still owes the chunk in LDS
-    for (; t0 < last; t0 += C) {
-        const int n = last - t0 < C ? (int)(last - t0) : C;
-        if (OUTPUT) xl.store(xs, XPITCH, n);
-        yl.store(ys, YPITCH, n);
-        zl.store(zs, ZPITCH, n);
-        __syncthreads();
-        if (t0 + C < last) load(t0 + C);
-
-        O *to_chunk = to;
-        to += C * ostep;
-        f4 out[OUTPUT ? MT : 1][NV] = {};
-        Frag zf[STEPS][NV];
-        if constexpr (OUTPUT) {
-            // this wavefront's tiles of the triangle: tokens 16 m + line against 16 j + 4 quad + 0..3
-            for (int tile = wave; tile < MT * (MT + 1) / 2; tile += WAVES) {
-                const int m = (int)(0x3333222110ull >> 4 * tile & 15), j = tile - m * (m + 1) / 2;
-                f4 dots = {};
-                float weight[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) weight[i] = gap_weight[15 + 16 * (m - j) + line - 4 * quad - i];
-                constexpr int TB = KSTEPS < 4 ? KSTEPS : 4;
-#pragma unroll
-                for (int k0 = 0; k0 < KSTEPS; k0 += TB) {
-                    Frag left[TB], right[TB];
-#pragma unroll
-                    for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) {
-                        left[kk] = M::along_rows(ys, YPITCH, 16 * j, (k0 + kk) * M::STEP);
-                        right[kk] = M::along_rows(xs, XPITCH, 16 * m, (k0 + kk) * M::STEP);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) dots = M::multiply(left[kk], right[kk], dots);
-                }
-                float values[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) values[i] = j < m || 4 * quad + i <= line ? weight[i] * dots[i] : 0.0f;      // (a later token may be infinite)
-                M::template put<SPLIT>(values, triangle + (m * STEPS + j / SUB) * SPLIT * 64 + lane, j % SUB);
-            }
-            // what lies before the chunk
-            Frag xf[2][MT], sf[2][SPLIT];
-            auto state_step = [&](int kk, int nv, Frag (&to)[SPLIT]) {
-                float values[4 * SUB];
-#pragma unroll
-                for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][nv][e % 4];
-                M::template split<SPLIT>(values, to);
-            };
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xf[0][m] = M::along_rows(xs, XPITCH, 16 * m, 0);
-            state_step(0, 0, sf[0]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int kk = 0; kk < KSTEPS; ++kk)
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    const int now = (kk * NV + nv) % 2;
-                    if (nv == 0 && kk + 1 < KSTEPS) {
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) xf[(kk + 1) % 2][m] = M::along_rows(xs, XPITCH, 16 * m, (kk + 1) * M::STEP);
-                    } else if (nv == NV - 1 && kk + 1 == KSTEPS) {
-#pragma unroll
-                        for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-                            for (int i = 0; i < NV; ++i) zf[st][i] = M::template along_columns<false>(zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * i);
-                    }
-                    if (nv + 1 < NV) state_step(kk, nv + 1, sf[1 - now]);
-                    else if (kk + 1 < KSTEPS) state_step(kk + 1, 0, sf[1 - now]);
-#pragma unroll
-                    for (int p = 0; p < SPLIT; ++p)
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) out[m][nv] = M::multiply(sf[now][p], xf[kk % 2][m], out[m][nv]);
-                    interleave<MT, SPLIT * MT * M::PRODUCTS>();
-                }
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const float w = after[16 * m + line + 1 - A.reversed];
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv) out[m][nv] *= w;
-            }
-            __syncthreads();
-            // the triangle
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                Frag pairs[MT][SPLIT];
-#pragma unroll
-                for (int m = st * SUB; m < MT; ++m)
-#pragma unroll
-                    for (int p = 0; p < SPLIT; ++p) pairs[m][p] = triangle[((m * STEPS + st) * SPLIT + p) * 64 + lane];
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int p = 0; p < SPLIT; ++p)
-#pragma unroll
-                    for (int m = st * SUB; m < MT; ++m)
-#pragma unroll
-                        for (int nv = 0; nv < NV; ++nv) out[m][nv] = M::multiply(zf[st][nv], pairs[m][p], out[m][nv]);
-            }
-            float worst = 0.0f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) worst = fmaf(out[m][nv][i], 0.0f, worst);     // a NaN from anything that is not finite
-            again = __any(!(worst == 0.0f));
-            if (again) {
-                spoilt = 1;
-            } else {
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (16 * m + line >= n) continue;
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv) {
-                        O *at = to_chunk + 16 * m * ostep + 16 * nv;
-                        Pack<O, 4> values;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) values.v[j] = from_float<O>(out[m][nv][j]);
-                        const int left = width - (wave * 16 * NV + 16 * nv + 4 * quad);
-                        if (left >= 4) {
-                            store_pack(at, values);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 3; ++j)
-                                if (j < left) at[j] = values.v[j];
-                        }
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv) zf[st][nv] = M::template along_columns<false>(zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * nv);
-        }
-        if (!again) {
-            // the state behind the chunk (a finite one; see Decay)
-            const float shrink = expm1f((float)n * g);
-            constexpr int BLOCKS = KT / YB, ALL = STEPS * BLOCKS;
-            static_assert(KT % YB == 0);
-            Frag yf[2][YB], wf[2][NV][PARTS];
-            auto y_block = [&](int block, Frag (&to)[YB]) {
-#pragma unroll
-                for (int i = 0; i < YB; ++i) {
-                    const int kt = block % BLOCKS * YB + i;
-                    to[i] = M::template along_columns<true>(ys, YPITCH, block / BLOCKS * M::STEP, kt / SUB * M::STEP, kt % SUB);
-                }
-            };
-            auto z_step = [&](int st, Frag (&to)[NV][PARTS]) {
-                float weight[4 * SUB];
-#pragma unroll
-                for (int e = 0; e < 4 * SUB; ++e) weight[e] = left_weight[C - n + st * M::STEP + e / 4 * 16 + 4 * quad + e % 4];
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    float values[4 * SUB];
-#pragma unroll
-                    for (int e = 0; e < 4 * SUB; ++e) values[e] = weight[e] * M::value(zf[st][nv], e);
-                    M::template split<PARTS>(values, to[nv]);
-                }
-            };
-            auto shrink_block = [&](int block) {
-#pragma unroll
-                for (int kt = block * YB; kt < (block + 1) * YB; ++kt)
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[kt][nv][i] = fmaf(s[kt][nv][i], shrink, s[kt][nv][i]);
-            };
-            y_block(0, yf[0]);
-            shrink_block(0);
-            z_step(0, wf[0]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int block = 0; block < ALL; ++block) {
-                const int st = block / BLOCKS, k0 = block % BLOCKS * YB;
-                if (block + 1 < ALL) y_block(block + 1, yf[(block + 1) % 2]);
-                if (block + 1 < BLOCKS) shrink_block(block + 1);
-                if (block % BLOCKS == BLOCKS - 1 && st + 1 < STEPS) z_step(st + 1, wf[(st + 1) % 2]);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int i = 0; i < YB; ++i) s[k0 + i][nv] = M::multiply(yf[block % 2][i], wf[st % 2][nv][p], s[k0 + i][nv]);
-                interleave<YB * M::COLUMN_READS, PARTS * NV * YB * M::PRODUCTS>();
-            }
-        }
-        __syncthreads();
-        if (OUTPUT && spoilt) break;
-    }
-    if constexpr (!OUTPUT) {
+    const auto lasts = [&] {      // whether something in the workgroup's state is not finite
         float worst = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -458,48 +297,256 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
             for (int nv = 0; nv < NV; ++nv)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) worst = fmaf(s[kt][nv][i], 0.0f, worst);
-        if (__syncthreads_or(!(worst == 0.0f))) {
-            // the whole segment again, token by token
+        if (__any(!(worst == 0.0f))) lasting = 1;
+        __syncthreads();
+        return lasting != 0;
+    };
+    while (true) {
+        const Place place(wave);
+        const int line = place.line, quad = place.quad, lane = place.lane;
+        O *to = o + (t0 + line) * ostep + wave * 16 * NV + 4 * quad;      // the lane's outputs of the next chunk
+        StateTile xt = {}, yt = {};      // (or what an earlier turn left there would be kept through all of it)
+        ValueTile zt = {};
+        if (t0 < last) load(xt, yt, zt, t0, place.thread);
+        for (; t0 < last; t0 += C) {
+            const int n = last - t0 < C ? (int)(last - t0) : C;
+            store(xt, yt, zt, n, place.thread);
+            __syncthreads();
+            if (t0 + C < last) load(xt, yt, zt, t0 + C, place.thread);
+
+            O *to_chunk = to;
+            to += C * ostep;
+            f4 out[OUTPUT ? MT : 1][NV] = {};
+            Frag zf[STEPS][NV];
+            if constexpr (OUTPUT) {
+                // this wavefront's tiles of the triangle: tokens 16 m + line against 16 j + 4 quad + 0..3
+                for (int tile = wave; tile < MT * (MT + 1) / 2; tile += WAVES) {
+                    const int m = (int)(0x3333222110ull >> 4 * tile & 15), j = tile - m * (m + 1) / 2;
+                    f4 dots = {};
+                    float weight[4];
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+                    for (int i = 0; i < 4; ++i) weight[i] = gap_weight[15 + 16 * (m - j) + line - 4 * quad - i];
+                    constexpr int TB = KSTEPS < 4 ? KSTEPS : 4;
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) s[kt][nv] = f4{};
-            yl = TileLoader<T, E, C, K, THREADS>(y + first * ystep, ystep, A.rows);
-            zl = TileLoader<T, E, C, VT, THREADS>(z + first * zstep, zstep, width);
-            t0 = first - C;
+                    for (int k0 = 0; k0 < KSTEPS; k0 += TB) {
+                        Frag left[TB], right[TB];
+#pragma unroll
+                        for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) {
+                            left[kk] = M::along_rows(lane, ys, YPITCH, 16 * j, (k0 + kk) * M::STEP);
+                            right[kk] = M::along_rows(lane, xs, XPITCH, 16 * m, (k0 + kk) * M::STEP);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int kk = 0; kk < TB && k0 + kk < KSTEPS; ++kk) dots = M::multiply(left[kk], right[kk], dots);
+                    }
+                    float values[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) values[i] = j < m || 4 * quad + i <= line ? weight[i] * dots[i] : 0.0f;      // (a later token may be infinite)
+                    M::template put<SPLIT>(values, triangle + (m * STEPS + j / SUB) * SPLIT * 64 + lane, j % SUB);
+                }
+                // what lies before the chunk
+                Frag xf[2][MT], sf[2][SPLIT];
+                auto state_step = [&](int kk, int nv, Frag (&to)[SPLIT]) {
+                    float values[4 * SUB];
+#pragma unroll
+                    for (int e = 0; e < 4 * SUB; ++e) values[e] = s[kk * SUB + e / 4][nv][e % 4];
+                    M::template split<SPLIT>(values, to);
+                };
+#pragma unroll
+                for (int m = 0; m < MT; ++m) xf[0][m] = M::along_rows(lane, xs, XPITCH, 16 * m, 0);
+                state_step(0, 0, sf[0]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kk = 0; kk < KSTEPS; ++kk)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) {
+                        const int now = (kk * NV + nv) % 2;
+                        if (nv == 0 && kk + 1 < KSTEPS) {
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) xf[(kk + 1) % 2][m] = M::along_rows(lane, xs, XPITCH, 16 * m, (kk + 1) * M::STEP);
+                        } else if (nv == NV - 1 && kk + 1 == KSTEPS) {
+#pragma unroll
+                            for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                                for (int i = 0; i < NV; ++i) zf[st][i] = M::template along_columns<false>(lane, zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * i);
+                        }
+                        if (nv + 1 < NV) state_step(kk, nv + 1, sf[1 - now]);
+                        else if (kk + 1 < KSTEPS) state_step(kk + 1, 0, sf[1 - now]);
+#pragma unroll
+                        for (int p = 0; p < SPLIT; ++p)
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) out[m][nv] = M::multiply(sf[now][p], xf[kk % 2][m], out[m][nv]);
+                        interleave<MT, SPLIT * MT * M::PRODUCTS>();
+                    }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const float w = after[16 * m + line + 1 - A.reversed];
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) out[m][nv] *= w;
+                }
+                __syncthreads();
+                // the triangle
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) {
+                    Frag pairs[MT][SPLIT];
+#pragma unroll
+                    for (int m = st * SUB; m < MT; ++m)
+#pragma unroll
+                        for (int p = 0; p < SPLIT; ++p) pairs[m][p] = triangle[((m * STEPS + st) * SPLIT + p) * 64 + lane];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int p = 0; p < SPLIT; ++p)
+#pragma unroll
+                        for (int m = st * SUB; m < MT; ++m)
+#pragma unroll
+                            for (int nv = 0; nv < NV; ++nv) out[m][nv] = M::multiply(zf[st][nv], pairs[m][p], out[m][nv]);
+                }
+                float worst = 0.0f;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) worst = fmaf(out[m][nv][i], 0.0f, worst);     // a NaN from anything that is not finite
+                again = __any(!(worst == 0.0f));
+                if (again) {
+                    spoilt = 1;
+                } else {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        if (16 * m + line >= n) continue;
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv) {
+                            O *at = to_chunk + 16 * m * ostep + 16 * nv;
+                            Pack<O, 4> values;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) values.v[j] = from_float<O>(out[m][nv][j]);
+                            const int left = width - (wave * 16 * NV + 16 * nv + 4 * quad);
+                            if (left >= 4) {
+                                store_pack(at, values);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 3; ++j)
+                                    if (j < left) at[j] = values.v[j];
+                            }
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) zf[st][nv] = M::template along_columns<false>(lane, zs, ZPITCH, st * M::STEP, wave * 16 * NV + 16 * nv);
+            }
+            if (!again) {
+                // the state behind the chunk (a finite one; see Decay)
+                const float shrink = expm1f((float)n * g);
+                constexpr int BLOCKS = KT / YB, ALL = STEPS * BLOCKS;
+                static_assert(KT % YB == 0);
+                Frag yf[2][YB], wf[2][NV][PARTS];
+                auto y_block = [&](int block, Frag (&to)[YB]) {
+#pragma unroll
+                    for (int i = 0; i < YB; ++i) {
+                        const int kt = block % BLOCKS * YB + i;
+                        to[i] = M::template along_columns<true>(lane, ys, YPITCH, block / BLOCKS * M::STEP, kt / SUB * M::STEP, kt % SUB);
+                    }
+                };
+                auto z_step = [&](int st, Frag (&to)[NV][PARTS]) {
+                    float weight[4 * SUB];
+#pragma unroll
+                    for (int e = 0; e < 4 * SUB; ++e) weight[e] = left_weight[C - n + st * M::STEP + e / 4 * 16 + 4 * quad + e % 4];
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) {
+                        float values[4 * SUB];
+#pragma unroll
+                        for (int e = 0; e < 4 * SUB; ++e) values[e] = weight[e] * M::value(zf[st][nv], e);
+                        M::template split<PARTS>(values, to[nv]);
+                    }
+                };
+                auto shrink_block = [&](int block) {
+#pragma unroll
+                    for (int kt = block * YB; kt < (block + 1) * YB; ++kt)
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[kt][nv][i] = fmaf(s[kt][nv][i], shrink, s[kt][nv][i]);
+                };
+                y_block(0, yf[0]);
+                shrink_block(0);
+                z_step(0, wf[0]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int block = 0; block < ALL; ++block) {
+                    const int st = block / BLOCKS, k0 = block % BLOCKS * YB;
+                    if (block + 1 < ALL) y_block(block + 1, yf[(block + 1) % 2]);
+                    if (block + 1 < BLOCKS) shrink_block(block + 1);
+                    if (block % BLOCKS == BLOCKS - 1 && st + 1 < STEPS) z_step(st + 1, wf[(st + 1) % 2]);
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                            for (int i = 0; i < YB; ++i) s[k0 + i][nv] = M::multiply(yf[block % 2][i], wf[st % 2][nv][p], s[k0 + i][nv]);
+                    interleave<YB * M::COLUMN_READS, PARTS * NV * YB * M::PRODUCTS>();
+                }
+            }
+            __syncthreads();
+            if (OUTPUT && spoilt) break;
         }
-    } else if (t0 + C < last) {
-        // (loaded anew behind the chunk in LDS: its registers are wanted)
-        xl.back();
-        yl.back();
-        zl.back();
-    }
-    // token by token from here on: first, with output, the chunk in LDS for those who could not take it
-    int c = column;
-    asm volatile("" : "+v"(c));      // (nothing of this loop is worked out ahead of the other, which has no registers to keep it)
-    for (; t0 < last; t0 += C) {
-        const int n = last - t0 < C ? (int)(last - t0) : C;
-        if (t0 >= first && (!OUTPUT || again))
-            chunk_by_token<OUTPUT>(A, g, n, xs, XPITCH, ys, YPITCH, zs, ZPITCH, s, first_row, row_of, c, [&](int r, int nv, float value) {
-                if (quad == 0 && c + 16 * nv < width) o[(t0 + r) * ostep + c + 16 * nv] = from_float<O>(value);
-            });
-        again = true;
-        __syncthreads();
-        if (t0 + C >= last) break;
-        const int more = last - t0 - C < C ? (int)(last - t0 - C) : C;
-        load(t0 + C);
-        if (OUTPUT) xl.store(xs, XPITCH, more);
-        yl.store(ys, YPITCH, more);
-        zl.store(zs, ZPITCH, more);
-        __syncthreads();
+        if constexpr (!OUTPUT) {
+            if (lasts()) {
+                // the whole segment again, token by token
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) s[kt][nv] = f4{};
+                yl = TileLoader<T, E, C, K, THREADS>(y + first * ystep, ystep, A.rows);
+                zl = TileLoader<T, E, C, VT, THREADS>(z + first * zstep, zstep, width);
+                t0 = first - C;
+            }
+        } else if (t0 + C < last) {
+            // (loaded anew behind the chunk in LDS: its registers are wanted)
+            xl.back();
+            yl.back();
+            zl.back();
+        }
+        // Token by token: first, with output, the chunk in LDS for those who could not take it.  From there on in chunks again, unless something
+        // in the state is not finite: that stays so, and so does what reads it.
+        bool chunks = false;
+        const Place alone(wave);
+        for (; t0 < last; t0 += C) {
+            const int n = last - t0 < C ? (int)(last - t0) : C;
+            if (t0 >= first && (!OUTPUT || again))
+                chunk_by_token<OUTPUT>(A, g, n, xs, XPITCH, ys, YPITCH, zs, ZPITCH, s, alone.first_row, row_of, alone.column, [&](int r, int nv, float value) {
+                    if (alone.quad == 0 && alone.column + 16 * nv < width) o[(t0 + r) * ostep + alone.column + 16 * nv] = from_float<O>(value);
+                });
+            again = true;
+            const bool stays = !OUTPUT || lasts();
+            if (!OUTPUT) __syncthreads();
+            if (t0 + C >= last) break;
+            if (!stays) {
+                spoilt = 0;
+                again = false;
+                chunks = true;
+                t0 += C;
+                break;
+            }
+            const int more = last - t0 - C < C ? (int)(last - t0 - C) : C;
+            StateTile x_next = {}, y_next = {};
+            ValueTile z_next = {};
+            load(x_next, y_next, z_next, t0 + C, alone.thread);
+            store(x_next, y_next, z_next, more, alone.thread);
+            __syncthreads();
+        }
+        if (!chunks) break;
     }
 
     if constexpr (OUTPUT) {
         // behind the length: zeros, a segment's own (four columns a thread)
         const int64_t end = segment + 1 < G.segments ? first + G.segment_tokens : A.T;
         constexpr int LANES = VT / 4;
-        const int c4 = threadIdx.x % LANES * 4, left = width - c4;
-        for (int64_t t = (first > length ? first : length) + threadIdx.x / LANES; t < end; t += THREADS / LANES) {
+        const int thread = Place(wave).thread, c4 = thread % LANES * 4, left = width - c4;
+        for (int64_t t = (first > length ? first : length) + thread / LANES; t < end; t += THREADS / LANES) {
             O *rest = (O *)A.o + b * A.os[0] + head * A.os[2] + t * A.os[1] + c0 + c4;
             if (left >= 4) {
                 store_pack(rest, Pack<O, 4>{});
@@ -510,10 +557,11 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
         if (!state_to) return;
     }
     const int64_t row_stride = OUTPUT ? A.row_stride : A.columns, column_stride = OUTPUT ? A.column_stride : 1;
+    const Place behind(wave);
 #pragma unroll
     for (int nv = 0; nv < NV; ++nv) {
-        float *to = state_to + first_row * row_stride + (c0 + c + 16 * nv) * column_stride;
-        int rows = c + 16 * nv < width ? A.rows - first_row : 0;
+        float *to = state_to + behind.first_row * row_stride + (c0 + behind.column + 16 * nv) * column_stride;
+        int rows = behind.column + 16 * nv < width ? A.rows - behind.first_row : 0;
         asm volatile("" : "+v"(rows));
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)

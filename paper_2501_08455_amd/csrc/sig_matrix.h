@@ -1,6 +1,6 @@
 // Matrix products of 16 x 16 tiles on gfx950, for operands kept in bfloat16 or in float32.
 //
-// A fragment is one wavefront's share of a 16 x STEP operand: lane l holds line l % 16 (a row of the left operand, a column of the
+// A fragment is one wavefront's share of a 16 x STEP operand: lane l (`lane` below, of 64) holds line l % 16 (a row of the left operand, a column of the
 // right one; both have the same layout) at 4 SUB places of the summed axis.  A product's result tile holds, in lane l, column
 // l % 16 at rows 4 (l / 16) + 0..3.  The order along a summed axis is free as long as both operands agree, so SUB result tiles are
 // a fragment as they lie (lines = columns, summed axis = rows), without a detour through LDS, where the other operand is read to match:
@@ -31,17 +31,15 @@ struct Matrix<float> {
 
     static __device__ constexpr int place(int, int r) { return r; }
     // lines = rows of `m` (pitch in values) from `line` on, summed axis = its columns from `at` on
-    static __device__ Frag along_rows(const float *m, int pitch, int line, int at)
+    static __device__ Frag along_rows(int lane, const float *m, int pitch, int line, int at)
     {
-        const int lane = threadIdx.x % kWaveLanes;
         return *(const f4 *)(m + (line + lane % 16) * pitch + at + 4 * (lane / 16));
     }
     // lines = columns of `m`, summed axis = its rows from `at` on.  The columns are those from `line` on, or with GAP the places of tile
     // `sub` of a step that begins there
     template <bool GAP>
-    static __device__ Frag along_columns(const float *m, int pitch, int at, int line, int = 0)
+    static __device__ Frag along_columns(int lane, const float *m, int pitch, int at, int line, int = 0)
     {
-        const int lane = threadIdx.x % kWaveLanes;
         const float *p = m + (at + 4 * (lane / 16)) * pitch + line + lane % 16;
         return f4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
     }
@@ -66,9 +64,6 @@ struct Matrix<float> {
     {
         *to = f4{x[0], x[1], x[2], x[3]};
     }
-
-private:
-    static constexpr int kWaveLanes = 64;
 };
 
 template <>
@@ -80,16 +75,15 @@ struct Matrix<bf16> {
     static constexpr int PRODUCTS = 1, COLUMN_READS = 2;
 
     static __device__ constexpr int place(int sub, int r) { return r / 4 * 8 + 4 * sub + r % 4; }
-    static __device__ Frag along_rows(const bf16 *m, int pitch, int line, int at)
+    static __device__ Frag along_rows(int lane, const bf16 *m, int pitch, int line, int at)
     {
-        const int lane = threadIdx.x % kWaveLanes;
         return *(const b8 *)(m + (line + lane % 16) * pitch + at + 8 * (lane / 16));
     }
     // The transposing LDS read: 16 lanes name the quarters of four rows of 16 values, and lane i receives value i of each row.
     template <bool GAP>
-    static __device__ Frag along_columns(const bf16 *m, int pitch, int at, int line, int sub = 0)
+    static __device__ Frag along_columns(int lane, const bf16 *m, int pitch, int at, int line, int sub = 0)
     {
-        const int lane = threadIdx.x % kWaveLanes, i = lane % 16;
+        const int i = lane % 16;
         const bf16 *p = m + (at + 4 * (lane / 16) + i / 4) * pitch + line + 4 * sub + (GAP ? 8 : 4) * (i % 4);
         using Read = __attribute__((address_space(3))) s4;
         const s4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)p);
@@ -114,8 +108,6 @@ struct Matrix<bf16> {
     }
 
 private:
-    static constexpr int kWaveLanes = 64;
-
     // (two at a time, as the conversion takes them; a bfloat16 is the upper half of its float32)
     template <int PARTS, int N, typename V>
     static __device__ void digits(const float *x, V *parts)

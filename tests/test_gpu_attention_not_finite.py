@@ -121,3 +121,51 @@ def test_one_token_after_the_other_keeps_infinite_states(kind):
     for t in range(6):
         assert_same(binding.linear_attention_step(q[:, t], k[:, t], v[:, t], log_decay, state), want[0][:, t], t)
     assert_same(state, want[1], "state")
+
+
+def microseconds(call):
+    """the fastest of a few calls"""
+    call()
+    best = math.inf
+    for _ in range(5):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        call()
+        b.record()
+        b.synchronize()
+        best = min(best, 1000.0 * a.elapsed_time(b))
+    return best
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_a_passing_infinity_costs_its_own_chunk_only(kind):
+    """An infinite query reaches its own output and no state, an infinite upstream gradient the gradient of its own query: the chunks behind are
+    worked on as chunks again.  (One of 64 chunks token by token took a sixth more; all of them token by token 18 to 36 times as long.)"""
+    B, T, H, K = 8, 2048, 64, 64
+    q, k, v = (torch.randn(B, T, H, K, device="cuda").to(kind) for _ in range(3))
+    log_decay = torch.full((H,), -0.05, device="cuda")
+    call = lambda: binding.linear_attention(q, k, v, log_decay)   # noqa: E731
+    clean, want = microseconds(call), call()
+    q[:, 5, :, 3] = math.inf
+    assert microseconds(call) <= 3.0 * clean
+    got = call()
+    assert not torch.isfinite(got[:, 5]).any()
+    # (the rest of the spoilt chunk is worked out in another order)
+    others = [t for t in range(T) if t != 5]
+    assert float((got[:, others] - want[:, others]).float().norm()) <= tolerance(kind) * float(want[:, others].float().norm())
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_chunks_after_several_spoilt_ones(kind):
+    """Spoilt chunks one behind another, apart, the first and the last, ragged, forward and both reversed passes; and a state that stays infinite
+    behind chunks that were only passed through."""
+    x = inputs(3, 500, 2, 1, 40, 72, kind, seed=160)
+    for t in (0, 40, 70, 100, 101, 300, 499):
+        x[0][1, t, 0, 2], x[5][1, 499 - t, 1, 4] = math.inf, -math.inf
+    check(*x)
+    x = inputs(1, 400, 3, 3, 128, 64, kind, seed=170)
+    x[0][0, 20, 1, 5], x[5][0, 390, 1, 7] = math.nan, math.nan
+    x[1][0, 200, 1, 5] = math.inf
+    check(*x)
