@@ -79,10 +79,11 @@ AttentionArgs pass(const sig_attention_t &s, const float *log_decay, const int64
 // Up to this many tokens go one after the other: a chunk's products cost as much for one token as for all of it.  Measured (us, token by
 // token; as a chunk):
 //   forward, tokens                            2           4           8            16
-//   bf16, 128 sequences, 16 heads of 64 x 64   17; 31      22; 31      32; 30       53; 30
-//   bf16, 64 sequences, 16 heads of 128 x 128  31; 47      40; 47      61; 48       103; 47
-//   f32, 128 sequences, 4 heads of 64 x 64     7.6; 11.4   9.6; 11.4   14.5; 11.4   24.9; 11.7
-// The gradient's passes are a launch each token by token, and one in chunks: 64 x 64 as above 75; 77 with two tokens, 99; 75 with four.
+//   bf16, 128 sequences, 16 heads of 64 x 64   9; 16       14; 16      22; 16       38; 16
+//   bf16, 64 sequences, 16 heads of 128 x 128  12; 19      20; 19      36; 19       67; 19
+//   f32, 128 sequences, 4 heads of 64 x 64     5.4; 9.7    7.7; 9.6    12.6; 9.8    22.5; 10.0
+// The gradient's passes are a launch each token by token, and one in chunks: 64 x 64 as above 27; 40 with two tokens, 39; 40 with four, 128 x 128
+// 36; 49 and 59; 50.
 constexpr int kRecurrentTokens = 4, kRecurrentGradientTokens = 2;
 
 bool by_token(const AttentionArgs *a, bool gradient) { return a[0].T <= (gradient ? kRecurrentGradientTokens : kRecurrentTokens); }

@@ -12,10 +12,11 @@
 // everyone reads.  Output tiles are taken as their transpose, in which a lane holds neighbouring columns of one token.
 //
 // Bound by neither memory nor the matrix units, but by what a chunk's steps wait for one after the other (operands from LDS, barriers) on the
-// two workgroups that a unit holds.  Measured: 65,536 tokens, 8 heads of 128 x 128 bfloat16, 242 us (2.2 TB/s of what goes in and out; matrix
-// units busy for 29% of the main launch, vector instructions 40%); 8 x 4,096 tokens, 16 heads, training, 660 us; 64 x 255 tokens, 4
-// heads of 64 x 64 float32, 26 us (2.6 TB/s).  Chunks of 64 tokens of bfloat16, since each also rounds the state anew for its
-// products (32 tokens: training 698 us), but 32 where the state has 256 rows (LDS then holds two workgroups) or sequences are short; 32 of float32.
+// two workgroups that a unit holds.  Measured, on two cards: 65,536 tokens, 8 heads of 128 x 128 bfloat16, 234 and 243 us (2.2 TB/s of what goes in and
+// out; matrix units busy for 29% of the main launch, vector instructions 40%); 8 x 4,096 tokens, 16 heads, training, 688 and 714 us; 64 x 255
+// tokens, 4 heads of 64 x 64 float32, 26 us (2.6 TB/s).  Chunks of 64 tokens of bfloat16, since each also rounds the state anew for its
+// products (32 tokens take as long: that batch 0.99 times, 64 sequences of 3,000 tokens 1.015), but 32 where the state has 256 rows (LDS then holds two
+// workgroups) or sequences are short; 32 of float32.
 //
 // A product of matrices multiplies every pair: 0 x infinity where the triangle is empty, and the parts of an infinite number.  A chunk
 // whose output is not finite is therefore worked out again token by token, by the wavefronts of those columns, so that what is not a number
@@ -187,7 +188,8 @@ __global__ __launch_bounds__(kChunkThreads, C == 32 || K <= 192 ? 2 : 1) void si
     constexpr int MT = C / 16, STEPS = C / M::STEP, KSTEPS = K / M::STEP, KT = K / 16, SUB = M::SUB;
     // The state itself keeps all digits of float32: each weighted z goes into its update as fragments that add up to it.  As operands of the
     // outputs' products the state and the triangle of pairs are two bfloat16 fragments, 16 digits, where those outputs are rounded to 8 (24 digits
-    // leave the same errors: 65,536 tokens, 8 heads of 128 x 128, 258 us instead of 239; a training batch 792 instead of 714).
+    // leave the same errors: 65,536 tokens, 8 heads of 128 x 128, 258 us instead of 239; a training batch 792 instead of 714.  With two fragments of
+    // each weighted z the batch took 673, but the gradients' state then had 16 digits too).
     constexpr int PARTS = M::EXACT, SPLIT = SUB == 2 ? 2 : 1;
     constexpr int YB = KT % 4 == 0 ? 4 : KT % 3 == 0 ? 3 : KT;      // tiles of the state whose operands are loaded at once
     const int pass = blockIdx.z % G.passes, segment = blockIdx.z / G.passes;
@@ -582,9 +584,9 @@ inline int chunk_rows(int rows, int type)
 
 // Up to so many tokens bfloat16 goes in chunks of 32 too (more workgroups a unit, fewer tokens to fill up).  Measured (us, chunks of 64; of 32):
 //   tokens                                        16         48         96         192        256        3,000
-//   128 sequences, 16 heads of 64 x 64            26; 18     27; 23     39; 28     53; 45     64; 59     748; 783
-//   64 sequences, 16 heads of 128 x 128, training 126; 89    137; 122   209; 164   314; 293   396; 379   4,091; 4,274
-//   4 sequences, 8 heads of 128 x 128             11; 9      11; 12     16; 15     20; 23     25; 28     82; 84
+//   128 sequences, 16 heads of 64 x 64            25; 17     26; 22     37; 27     49; 42     61; 53     754; 766
+//   64 sequences, 16 heads of 128 x 128, training 90; 70     97; 98     148; 126   210; 208   283; 279   3,132; 3,178
+//   4 sequences, 8 heads of 128 x 128             10; 8      10; 10     13; 11     16; 17     19; 20     65; 65
 constexpr int kShortTokens = 192;
 
 // The instance for `G`: up to 64 nv columns a workgroup

@@ -44,26 +44,26 @@ struct Cut {
 
 // How many columns a workgroup takes and how many workgroups share a sequence, measured (us, forward; gradient):
 //   bf16, 128 x 128, 128 heads     one segment of 128 columns   of 64 columns   four segments of 128 columns
-//     4,096 tokens                 325; 421                     277; 521        222; 556
-//     1,024 tokens                 81; 107                      62; 123         82; 195
-//   f32, 128 x 128, 128 heads, 1,024 tokens   198; 353          129; 328        164; 438
+//     4,096 tokens                 319; 495                     224; 523        216; 586
+//     1,024 tokens                 81; 113                      61; 124         80; 188
+//   f32, 128 x 128, 128 heads, 1,024 tokens   199; 352          130; 332        166; 438
 // Workgroups of 128 columns, which share the operands' loads and the pairs of a chunk, where they are more than the units (float32, bound by
 // its products: where they are twice as many); else of 64 where those are about one a unit; fewer than that are cut along time, which costs a
-// second read of y and z, the segments' states and two more launches (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 462, 285, 243 and
-// 270; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64 segments 355, 48, 40 and 49).  As many segments as fill the units with what they hold of
+// second read of y and z, the segments' states and two more launches (8 heads, 65,536 tokens: 16, 32, 64 and 96 segments 472, 268, 231 and
+// 262; 16 heads of 64 x 64, 8,192 tokens: 1, 16, 32 and 64 segments 324, 48, 43 and 51).  As many segments as fill the units with what they hold of
 // such workgroups at once: two, or three of small states (61 sequences of 2,819 tokens at most, 3 heads of 64 x 33 bfloat16: 131 us cut for two,
 // 98 for three), of four chunks or more.  Segments are of 128 columns where a sequence has enough of those, nearly, to fill the units, else of
 // 64 (2 to 64 heads of 128 x 128 bfloat16: 300 tokens 30; 23, 1,000 tokens 47 to 58; 34 to 51, 8 heads of 8,000 62; 55; float32 300
 // tokens 60 to 68; 42 to 49).
 // Long sequences of less than two workgroups of 64 columns a unit are cut too, where that pays.  Whole; cut as the rule has it (us):
-//   bf16, heads   200 of 64 x 64   256 of 64 x 64   256 of 96 x 64   200 of 128 x 64   128 of 128 x 128   140 of 128 x 128   200 of 128 x 128
-//   1,024 tokens  56; 56           53; 58           64; 73           69; 78            66; 87             -                  -
-//   2,048         99; 84           95; 91           124; 124         130; 127          120; 128           148; 150           -
-//   4,096         199; 161         208; 176         240; 219         250; 229          258; 221           294; 268           303; 349 in two
-//   8,192         391; 329         396; 343         472; 441         488; 438          481; 408           -                  -
-// (192 and 256 rows 311; 305 and 338; 394 at 4,096 tokens.)  Float32 of at most 64 columns only beyond one workgroup a unit, whose second
-// round is then shared out (4,096 tokens: 200 heads of 64 x 64 323; 332, 256 of 96 x 64 432; 457, 280 of 64 x 64 492; 470), of more also
-// below (100 heads of 64 x 128 320; 274).
+//   bf16, heads   200 of 64 x 64   256 of 64 x 64   256 of 96 x 64   200 of 128 x 64   100 of 128 x 128   128 of 128 x 128   140 of 128 x 128
+//   1,024 tokens  49; 54           47; 55           58; 70           62; 75            59; 74             63; 84             78; 96
+//   2,048         86; 81           86; 86           113; 118         115; 123          110; 106           111; 123           145; 147
+//   4,096         166; 161         167; 174         223; 212         223; 220          219; 175           221; 209           283; 267
+//   8,192         325; 326         334; 344         460; 416         444; 419          459; 338           448; 394           567; 487
+// (4,096 tokens of 200 heads of 128 x 128, which fill the units with two segments, 298; 334, of 128 heads of 256 x 128 346; 359.)  Float32 of at most
+// 64 columns only beyond one workgroup a unit, whose second round is then shared out (4,096 tokens: 200 heads of 64 x 64 317; 323, 256 of 96 x 64
+// 454; 470, 280 of 64 x 64 487; 463), of more also below (100 heads of 64 x 128 317; 274).
 Cut cut_of(const AttentionArgs *a, int passes, int type, int cus)
 {
     const int chunk = type == SIG_BF16 ? 64 : 32;
