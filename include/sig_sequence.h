@@ -31,7 +31,8 @@ enum sig_type { SIG_F32 = 0, SIG_BF16 = 1, SIG_F16 = 2 };
  *   stats        DEVICE, float32 [rows][2], what sig_layer_norm_backward needs (mean, 1 / sqrt(...)); may be NULL
  * rows == 0 returns SIG_OK and launches nothing; width < 1, rows < 0 or a NaN or negative eps are SIG_ERR_INVALID; rows of more than 16,384
  * values that are 2^24 pieces of 8,192 or more are SIG_ERR_TOO_LARGE.
- * NaN and Inf spoil their own row only.  Any width: rows of up to 16,384 values stay on chip between their
+ * NaN and Inf spoil their own row only.  Statistics have float32's range: a row whose squared deviations add up to more than 3e38 has a variance of
+ * infinity, and h = 0.  Any width: rows of up to 16,384 values stay on chip between their
  * statistics and their output, longer ones are read twice and cut across workgroups (context scratch of about 2 floats for
  * every 8,192 values).
  */
