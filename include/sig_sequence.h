@@ -1,14 +1,14 @@
 /*
  * sig_sequence.h -- C ABI of libsig's sequence-model operators: what stands behind the every-prefix signature in a model
- * that is trained on it.  Layer norm of rows, rotary positions, and linear attention with a decay for each head, each
- * with its gradient.  The conventions are those of sig.h: DEVICE pointers, a hipStream_t passed as void*, no
+ * that is trained on it.  Layer norm of rows, rotary positions, linear attention with a decay for each head, and softmax attention
+ * with a sliding window, each with its gradient; and the paged cache that the latter is served from.  The conventions are those of sig.h: DEVICE pointers, a hipStream_t passed as void*, no
  * synchronisation, a status code for every failure, context scratch as described there (each entry point says what it
  * keeps there), deterministic results (no atomics, fixed summation order).
  *
  * Values are float32, bfloat16 or float16 in memory (enum sig_type).  Sums, statistics and states are in float32 or more; each
  * output is rounded once.  Arithmetic is float32's too, but for one thing: attention of bfloat16 over more than four tokens (more than two in
  * the gradient) multiplies with the state, and with the products of queries and keys, rounded to 16 digits, for outputs that
- * have 8.  The state itself, and so state_out and grad_initial, keeps float32's.  Pointers are aligned to their type, no more is asked for.
+ * have 8.  The state itself, and so state_out and grad_initial, keeps float32's.  (Softmax attention rounds its probabilities: see there.)  Pointers are aligned to their type, no more is asked for.
  */
 #ifndef SIG_SEQUENCE_H
 #define SIG_SEQUENCE_H
@@ -113,6 +113,46 @@ int sig_linear_attention(sig_ctx *ctx, const sig_attention_t *shape, const void 
 int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, const void *q, const void *k, const void *v,
                                   const float *log_decay, const float *state, const int64_t *lengths, const void *grad_out,
                                   const float *grad_state, void *grad_q, void *grad_k, void *grad_v, float *grad_initial, void *hip_stream);
+
+/*
+ * Softmax attention with a sliding window and first tokens that stay visible.  Token t of a sequence sees token s <= t if t - s < window
+ * (window == 0: any) or s < sinks.  With z_ts = scale * q_t . k_s over what t sees:
+ *   o_t = sum_s exp(z_ts) v_s / sum_s exp(z_ts)
+ *   q            DEVICE, [B][T][heads][key_dim] of `type`
+ *   k, v         DEVICE, [B][T][shared_heads][key_dim or value_dim]; head h reads shared head h / (heads / shared_heads)
+ *                strides in values between batches, tokens and heads; the last axis is contiguous
+ *   lengths      DEVICE, int64 [B], tokens of each sequence (taken into 0 ... T); NULL: T.  The tokens behind them are not read and
+ *                give zeros
+ *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous
+ *   stats        DEVICE, float32 [B][heads][T][2], what sig_window_attention_backward needs (the largest z, as a power of two, and one over the
+ *                sum of exp(z - largest)); may be NULL.  Nothing is written for the tokens behind the lengths
+ * 16-bit operands are multiplied as they are, and the probabilities (before they are divided by their sum) rounded to that type for their product
+ * with v; sums are float32's.  What a token does not see may be anything, NaN and infinities too; what is not finite spoils the tokens that see it.
+ * Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); a scale that is not finite is SIG_ERR_INVALID; 2^31 - 1024 tokens or more, 2^31 heads
+ * (B * heads) or more, or 2^39 tokens of heads, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  No context scratch.
+ */
+typedef struct sig_window_t {
+    int64_t B, T;
+    int32_t heads, shared_heads, key_dim, value_dim;
+    int32_t type;
+    float scale;
+    int64_t window, sinks;
+    int64_t q_strides[3], k_strides[3], v_strides[3];
+} sig_window_t;
+
+int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths, void *out,
+                         float *stats, void *hip_stream);
+
+/*
+ * Gradient of sig_window_attention with respect to q, k and v.
+ *   out, stats   as sig_window_attention wrote them
+ *   grad_out     DEVICE, [B][T][heads][value_dim] of `type`, contiguous; what stands behind the lengths is not read
+ *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
+ *                shared head is the sum over the heads that read it
+ * Products of float16 are float32's here.  Context scratch of B * heads * T floats.
+ */
+int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
+                                  const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -106,6 +106,14 @@ def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, r
     return call(q, k, v, log_decay, state, lengths, scale, return_state)
 
 
+def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
+    """binding.window_attention with a gradient with respect to `q`, `k` and `v`."""
+    call = (binding._torch_lib or binding.torch_lib()).autograd_window_attention
+    if torch.jit.is_tracing():
+        return _TracedCall.apply(lambda q, k, v, n: call(q, k, v, window, sinks, n, scale), q, k, v, lengths)
+    return call(q, k, v, window, sinks, lengths, scale)
+
+
 def capture(step_fn, warmup=3):
     """One call of `step_fn()` as a HIP graph: (graph, what the captured call returned).
 

@@ -48,6 +48,14 @@ class sig_attention_t(ctypes.Structure):
                 ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
 
 
+class sig_window_t(ctypes.Structure):
+    """Shape of a sig_window_attention call (include/sig_sequence.h)."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("heads", ctypes.c_int32), ("shared_heads", ctypes.c_int32),
+                ("key_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("window", ctypes.c_int64), ("sinks", ctypes.c_int64),
+                ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
+
+
 class SigError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -116,6 +124,10 @@ def load():
     lib.sig_linear_attention.argtypes = [vp, ctypes.POINTER(sig_attention_t)] + [vp] * 9
     lib.sig_linear_attention_backward.restype = i32
     lib.sig_linear_attention_backward.argtypes = [vp, ctypes.POINTER(sig_attention_t)] + [vp] * 13
+    lib.sig_window_attention.restype = i32
+    lib.sig_window_attention.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 7
+    lib.sig_window_attention_backward.restype = i32
+    lib.sig_window_attention_backward.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 11
     lib.sig_probe_copy.restype = i32
     lib.sig_probe_copy.argtypes = [vp, vp, i64, vp]
     lib.sig_probe_write.restype = i32
@@ -381,3 +393,12 @@ def linear_attention_step(q, k, v, log_decay, state, scale=None, out_state=None)
     """linear_attention of one token: `q` [B, H, K], `k` [B, G, K], `v` [B, G, V].  Updates `state` in place, or writes the new one to
     `out_state`.  Returns o [B, H, V]."""
     return (_torch_lib or torch_lib()).linear_attention_step(q, k, v, log_decay, state, scale, out_state)
+
+
+def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
+    """Softmax attention of each token over itself and the tokens before it: o_t = sum_s p_ts v_s, p_ts = exp(scale q_t . k_s) over their sum.
+
+    `q` [B, T, H, K], `k` [B, T, G, K], `v` [B, T, G, V] of one type (float32, bfloat16, float16), H a multiple of G (heads share
+    keys and values), K and V up to 256.  With `window`, a token sees the last `window` tokens, itself included, and the first `sinks` tokens of
+    the sequence; None: all.  `lengths` [B]: tokens from there on are not read and give zeros; `scale` None: K ** -0.5.  Returns o [B, T, H, V]."""
+    return (_torch_lib or torch_lib()).window_attention(q, k, v, window, sinks, lengths, scale)

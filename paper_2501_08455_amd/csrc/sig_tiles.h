@@ -1,0 +1,342 @@
+// Matrix products of M x M tiles on gfx950 for softmax attention, and the LDS tiles that feed them.
+//
+// A product's result tile holds, in lane l of a wavefront, column l % M at the rows row_of(l, i), i < REGS.  A fragment is the wavefront's share of an
+// operand of M lines and STEP places of the summed axis: lane l holds line l % M.  The order along a summed axis is free as long as
+// both operands agree:
+//   rows       neighbouring places: lines = rows of an LDS tile, summed axis = its columns.  The other operand is loaded to match
+//              (fragment_of)
+//   columns    the places that a result tile's registers hold, so that results are operands as they lie: lines = columns of an LDS
+//              tile, summed axis = its rows
+//
+// 16-bit values: 32 x 32 tiles, since each fragment that is read from LDS then feeds twice the products that 16 x 16 has for it.  LDS
+// gives 128 bytes a cycle to four matrix units, and a wavefront with 32 lines asks for just that at the units' full rate.  Float32: 16 x 16, an
+// eighth of the rate or less, where the wavefront's own operands take half of the registers.
+#ifndef SIG_TILES_H
+#define SIG_TILES_H
+
+#include <type_traits>
+
+#include "sig_types.h"
+
+namespace sig {
+
+using f4 = __attribute__((ext_vector_type(4))) float;
+using f16v = __attribute__((ext_vector_type(16))) float;
+
+// What bfloat16 and float16 share
+template <typename E_>
+struct NarrowTiles {
+    using E = E_;
+    static constexpr int M = 32, STEP = 16, REGS = 16;
+    static constexpr int GROUP = 8;                 // values of 16 bytes
+    using Frag = __attribute__((ext_vector_type(8))) E;
+    using Result = f16v;
+
+    static __device__ constexpr int row_of(int lane, int i) { return i / 4 * 8 + lane / 32 * 4 + i % 4; }
+    // of the columns form: place along the summed axis of element e
+    static __device__ constexpr int place_of(int lane, int e) { return e / 4 * 8 + lane / 32 * 4 + e % 4; }
+    // of the rows form: the first of a lane's neighbouring places
+    static __device__ constexpr int first_of(int lane) { return lane / 32 * 8; }
+
+    template <typename Tile>
+    static __device__ Frag rows(int lane, const E *tile, int line, int at)
+    {
+        return *(const Frag *)(tile + (lane % 32 * Tile::PITCH + lane / 32 * 8) + (line * Tile::PITCH + at));
+    }
+    // The transposing LDS read: 16 lanes name the quarters of four rows of 16 values, and lane i receives value i of each row.
+    template <typename Tile>
+    static __device__ Frag columns(int lane, const E *tile, int at, int line)
+    {
+        using s4 = __attribute__((ext_vector_type(4))) short;
+        using Read = __attribute__((address_space(3))) s4;
+        const int i = lane % 16;
+        const E *p = tile + ((lane / 32 * 4 + i / 4) * Tile::PITCH + lane / 16 % 2 * 16 + i % 4 * 4);
+        const s4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + (at * Tile::PITCH + line)));
+        const s4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + ((at + 8) * Tile::PITCH + line)));
+        return __builtin_bit_cast(Frag, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // fragment number `step` of the columns form out of result tiles
+    static __device__ Frag of_results(const Result *tiles, int step)
+    {
+        Frag f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (E)tiles[step / 2][step % 2 * 8 + e];
+        return f;
+    }
+};
+
+// ... and in 16 x 16 tiles
+template <typename E_>
+struct SmallNarrowTiles {
+    using E = E_;
+    static constexpr int M = 16, STEP = 32, REGS = 4;
+    static constexpr int GROUP = 8;
+    using Frag = __attribute__((ext_vector_type(8))) E;
+    using Result = f4;
+
+    static __device__ constexpr int row_of(int lane, int i) { return lane / 16 * 4 + i; }
+    static __device__ constexpr int place_of(int lane, int e) { return e / 4 * 16 + lane / 16 * 4 + e % 4; }
+    static __device__ constexpr int first_of(int lane) { return lane / 16 * 8; }
+
+    template <typename Tile>
+    static __device__ Frag rows(int lane, const E *tile, int line, int at)
+    {
+        return *(const Frag *)(tile + (lane % 16 * Tile::PITCH + lane / 16 * 8) + (line * Tile::PITCH + at));
+    }
+    template <typename Tile>
+    static __device__ Frag columns(int lane, const E *tile, int at, int line)
+    {
+        using s4 = __attribute__((ext_vector_type(4))) short;
+        using Read = __attribute__((address_space(3))) s4;
+        const int i = lane % 16;
+        const E *p = tile + ((lane / 16 * 4 + i / 4) * Tile::PITCH + i % 4 * 4);
+        const s4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + (at * Tile::PITCH + line)));
+        const s4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read *)(p + ((at + 16) * Tile::PITCH + line)));
+        return __builtin_bit_cast(Frag, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    static __device__ Frag of_results(const Result *tiles, int step)
+    {
+        Frag f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (E)tiles[2 * step + e / 4][e % 4];
+        return f;
+    }
+};
+
+// Tiles<E>, and SmallTiles<E> where a line has more than 128 values, of which fewer then fit the registers
+template <typename E>
+struct Tiles;
+template <typename E>
+struct SmallTiles;
+
+template <>
+struct Tiles<bf16> : NarrowTiles<bf16> {
+    static __device__ Result multiply(Frag left, Frag right, Result sum) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(left, right, sum, 0, 0, 0); }
+};
+
+template <>
+struct Tiles<f16> : NarrowTiles<f16> {
+    static __device__ Result multiply(Frag left, Frag right, Result sum) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(left, right, sum, 0, 0, 0); }
+};
+
+template <>
+struct SmallTiles<bf16> : SmallNarrowTiles<bf16> {
+    static __device__ Result multiply(Frag left, Frag right, Result sum) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(left, right, sum, 0, 0, 0); }
+};
+
+template <>
+struct SmallTiles<f16> : SmallNarrowTiles<f16> {
+    static __device__ Result multiply(Frag left, Frag right, Result sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(left, right, sum, 0, 0, 0); }
+};
+
+template <>
+struct Tiles<float> {
+    using E = float;
+    static constexpr int M = 16, STEP = 16, REGS = 4;
+    static constexpr int GROUP = 4;
+    using Frag = f4;
+    using Result = f4;
+
+    static __device__ constexpr int row_of(int lane, int i) { return lane / 16 * 4 + i; }
+    static __device__ constexpr int place_of(int lane, int e) { return lane / 16 * 4 + e; }
+    static __device__ constexpr int first_of(int lane) { return lane / 16 * 4; }
+
+    template <typename Tile>
+    static __device__ Frag rows(int lane, const float *tile, int line, int at)
+    {
+        return *(const Frag *)(tile + (lane % 16 * Tile::PITCH + lane / 16 * 4) + (line * Tile::PITCH + at));
+    }
+    template <typename Tile>
+    static __device__ Frag columns(int lane, const float *tile, int at, int line)
+    {
+        const float *p = tile + (lane / 16 * 4 * Tile::PITCH + lane % 16) + (at * Tile::PITCH + line);
+        return f4{p[0], p[Tile::PITCH], p[2 * Tile::PITCH], p[3 * Tile::PITCH]};
+    }
+    static __device__ Frag of_results(const Result *tiles, int step) { return tiles[step]; }
+    static __device__ Result multiply(Frag left, Frag right, Result sum)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(left[i], right[i], sum, 0, 0, 0);
+        return sum;
+    }
+};
+
+template <>
+struct SmallTiles<float> : Tiles<float> {};
+
+// Rows of D values in LDS, PITCH apart: an odd number of 16 bytes, so that the 16 rows of a 16-byte read (rows) find all 64 banks, and
+// one that keeps the 32-byte pieces of four rows of a transposing read in different ones.
+template <typename E, int D>
+struct LdsTile {
+    static constexpr int BANK_GROUPS = D * (int)sizeof(E) / 16 % 16;
+    static constexpr int PITCH = D + (sizeof(E) == 4 ? 4 : BANK_GROUPS == 0 || BANK_GROUPS == 4 ? 24 : 8);
+};
+
+// The wavefront's own operand, one line a lane: fragments to match the rows form, zeros where `there` is false
+template <typename X, int STEPS, typename T>
+__device__ inline void fragments_of(typename X::Frag *f, int lane, const T *line, int dim, bool there, bool negated)
+{
+    using E = typename X::E;
+    constexpr int N = X::GROUP;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const int at = j * X::STEP + X::first_of(lane);
+        f[j] = typename X::Frag{};
+        if (there && at + N <= dim) {
+            const Pack<T, N> got = load_pack<T, N>(line + at);
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[j][e] = (E)got.v[e];
+        } else if (there) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (at + e < dim) f[j][e] = (E)line[at + e];
+        }
+        if (negated) f[j] = -f[j];
+    }
+}
+
+// ROWS x D values, global memory -> registers -> LDS, by THREADS threads: zeros beyond the rows and values that are there.  Loads of whole groups are
+// unconditional (what is not there is read from a place that is, and dropped on the way to LDS), so that all are in flight at once.
+template <typename T, typename E, int D, int ROWS, int THREADS>
+struct TileMover {
+    static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = ROWS * GROUPS / THREADS;
+    static_assert(ROWS * GROUPS % THREADS == 0);
+    using Group = struct { E v[GROUP]; };
+    Pack<T, GROUP> held[COUNT];
+
+    static __device__ int row_of(int i) { return (threadIdx.x + i * THREADS) / GROUPS; }
+    static __device__ int place_of(int i) { return (threadIdx.x + i * THREADS) % GROUPS * GROUP; }
+
+    // rows 0 ... n - 1 are there, n >= 1
+    __device__ void load(const T *first, int64_t stride, int dim, int n)
+    {
+        if (dim >= GROUP) {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int place = place_of(i);
+                held[i] = load_pack<T, GROUP>(first + min(row_of(i), n - 1) * stride + (place + GROUP <= dim ? place : 0));
+            }
+        }
+        if (dim % GROUP) {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int place = place_of(i);
+                if (place < dim && place + GROUP > dim) {
+                    const T *p = first + min(row_of(i), n - 1) * stride;
+#pragma unroll
+                    for (int j = 0; j < GROUP; ++j) {
+                        held[i].v[j] = (T)0.0f;
+                        if (place + j < dim) held[i].v[j] = p[place + j];
+                    }
+                }
+            }
+        }
+    }
+    // whether this thread holds something that is not finite
+    __device__ bool spoilt(int dim, int n) const
+    {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) any = any || (!__builtin_isfinite((float)held[i].v[j]) && row_of(i) < n && place_of(i) < dim);
+        return any;
+    }
+    __device__ void store(E *tile, int dim, int n) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            Group values;
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) values.v[j] = (E)held[i].v[j];
+            const f4 bits = __builtin_bit_cast(f4, values);
+            *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = row_of(i) < n && place_of(i) < dim ? bits : f4{};
+        }
+    }
+};
+
+// acc[t] += columns(tile)' x p, tile by tile of D / M: `p` are STEPS fragments along the tile's rows
+template <typename X, int D, int STEPS>
+__device__ inline void product_along_rows(int lane, const typename X::E *tile, const typename X::Frag *p, typename X::Result *acc)
+{
+    using E = typename X::E;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+#pragma unroll
+        for (int t = 0; t < D / X::M; ++t) acc[t] = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j * X::STEP, t * X::M), p[j], acc[t]);
+        __builtin_amdgcn_sched_barrier(0);      // (else all reads are moved to the front, and more registers are asked for than there are)
+    }
+}
+
+// Tiles that are partly hidden and hold something that is not finite: that is set to 0 in LDS before the product along the rows, by all threads ...
+template <typename E, int D, int ROWS, int THREADS>
+__device__ inline void leave_finite(E *tile)
+{
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < ROWS * D; i += THREADS) {
+        E *x = tile + i / D * LdsTile<E, D>::PITCH + i % D;
+        if (!__builtin_isfinite((float)*x)) *x = (E)0.0f;
+    }
+    __syncthreads();
+}
+
+// ... and behind it added by the lanes whose column sees its row, of the n rows at `first`.  A product counts them: the tile becomes 1 where there is
+// one, and the other operand where it is seen.  NANS: as NaN, which is what it comes to where its factors are signed; else NaN, infinity
+// and minus infinity as they are, their factors being positive.  By all threads; `idle` wavefronts only help with the tile.
+template <typename X, int D, int ROWS, int THREADS, bool NANS, typename T, typename Seen>
+__device__ inline void add_not_finite(int lane, typename X::E *tile, const T *first, int64_t stride, int dim, int n, bool idle, typename X::Result *acc, Seen seen)
+{
+    using E = typename X::E;
+#pragma unroll 1
+    for (int kind = 0; kind < (NANS ? 1 : 3); ++kind) {
+        __syncthreads();
+#pragma unroll 1
+        for (int i = threadIdx.x; i < ROWS * D; i += THREADS) {
+            const int row = i / D, c = i % D;
+            const float x = row < n && c < dim ? (float)first[row * stride + c] : 0.0f;
+            const bool is = NANS ? !__builtin_isfinite(x) : kind == 0 ? x != x : kind == 1 ? x == INFINITY : x == -INFINITY;
+            tile[row * LdsTile<E, D>::PITCH + c] = (E)(is ? 1.0f : 0.0f);
+        }
+        __syncthreads();
+        if (idle) continue;
+        const float what = kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY;
+#pragma unroll
+        for (int t = 0; t < D / X::M; ++t) {
+            typename X::Result counts = {};
+#pragma unroll 1
+            for (int j = 0; j < ROWS; j += X::STEP) {
+                typename X::Frag sees;
+#pragma unroll
+                for (int e = 0; e < X::GROUP; ++e) sees[e] = (E)(seen(j + X::place_of(lane, e)) ? 1.0f : 0.0f);
+                counts = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j, t * X::M), sees, counts);
+            }
+#pragma unroll
+            for (int i = 0; i < X::REGS; ++i) acc[t][i] += counts[i] > 0.0f ? what : 0.0f;
+        }
+    }
+}
+
+// s[t] += rows(tile) x own, tile by tile of COUNT M rows
+template <typename X, int D, int COUNT>
+__device__ inline void product_of_rows(int lane, const typename X::E *tile, const typename X::Frag *own, typename X::Result *s)
+{
+    using E = typename X::E;
+#pragma unroll
+    for (int step = 0; step < D / X::STEP; ++step) {
+#pragma unroll
+        for (int t = 0; t < COUNT; ++t) s[t] = X::multiply(X::template rows<LdsTile<E, D>>(lane, tile, t * X::M, step * X::STEP), own[step], s[t]);
+        if (step % 2) __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// over the lanes that hold one column of a result tile
+template <int M, typename F>
+__device__ inline float over_column(float x, F f)
+{
+    if (M == 16) x = f(x, __shfl_xor(x, 16));
+    return f(x, __shfl_xor(x, 32));
+}
+
+}  // namespace sig
+#endif

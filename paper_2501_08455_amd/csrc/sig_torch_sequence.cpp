@@ -414,6 +414,91 @@ at::Tensor step(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, c
     return o.squeeze(1);
 }
 
+// ---------------------------------------------------------------- softmax attention with a sliding window
+// one int64 for each batch element, or nothing
+at::Tensor per_element(const at::Tensor &t, const at::Tensor &q, int64_t B, const char *name)
+{
+    if (!t.defined()) return t;
+    same_place(t, q, name);
+    if (t.dim() != 1 || t.size(0) != B || (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt))
+        refuse(std::string(name) + " must be int64 or int32, one for each batch element");
+    return t.to(at::kLong).contiguous();
+}
+
+const int64_t *whole_numbers(const at::Tensor &t) { return t.defined() ? t.const_data_ptr<int64_t>() : nullptr; }
+
+struct WindowAttention {
+    at::Tensor q, k, v, lengths;
+    sig_window_t shape;
+
+    // q, k, v: [batch, length, heads, .]; window 0: none
+    WindowAttention(const at::Tensor &q_, const at::Tensor &k_, const at::Tensor &v_, const at::Tensor &lengths_, int64_t window, int64_t sinks, double scale)
+    {
+        const int type = type_of(q_, "q");
+        same_type(k_, q_, "k");
+        same_type(v_, q_, "v");
+        const int64_t B = q_.size(0), T = q_.size(1), H = q_.size(2), K = q_.size(3), G = k_.size(2), V = v_.size(3);
+        if (k_.size(0) != B || k_.size(1) != T || k_.size(3) != K) refuse("k must have the batch, length and components of q");
+        if (v_.size(0) != B || v_.size(1) != T || v_.size(2) != G) refuse("v must have the batch, length and heads of k");
+        if (G < 1 || H < 1 || H % G) refuse("the heads of q must be a multiple of the heads of k and v");
+        if (std::max({H, K, V}) > INT32_MAX) refuse("too many heads or components");
+        if (!std::isfinite((float)scale)) refuse("scale must be finite");
+        lengths = per_element(lengths_, q_, B, "lengths");
+        q = unit_rows(q_);
+        k = unit_rows(k_);
+        v = unit_rows(v_);
+        shape = {B, T, (int32_t)H, (int32_t)G, (int32_t)K, (int32_t)V, type, (float)scale, window, sinks, {}, {}, {}};
+        for (int i = 0; i < 3; ++i) {
+            shape.q_strides[i] = q.stride(i);
+            shape.k_strides[i] = k.stride(i);
+            shape.v_strides[i] = v.stride(i);
+        }
+    }
+
+    at::Tensor forward(at::Tensor *stats) const
+    {
+        const auto plain = q.options().memory_format(at::MemoryFormat::Contiguous);
+        at::Tensor out = at::empty({shape.B, shape.T, shape.heads, shape.value_dim}, plain);
+        if (stats) *stats = at::empty({shape.B, shape.heads, shape.T, 2}, plain.dtype(at::kFloat));
+        check(sig_window_attention(default_ctx, &shape, data(q), data(k), data(v), whole_numbers(lengths), own_data(out), stats ? own_floats(*stats) : nullptr,
+                                   current_stream()), "sig_window_attention");
+        return out;
+    }
+};
+
+struct DifferentiableWindowAttention : torch::autograd::Function<DifferentiableWindowAttention> {
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const Maybe &lengths_, int64_t window,
+                              int64_t sinks, double scale)
+    {
+        at::AutoDispatchBelowADInplaceOrView below_autograd;
+        const at::Tensor lengths = given(lengths_);
+        at::Tensor stats;
+        const at::Tensor out = WindowAttention(q, k, v, lengths, window, sinks, scale).forward(&stats);
+        ctx->save_for_backward({q, k, v, lengths, stats, out});
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["sinks"] = sinks;
+        ctx->saved_data["scale"] = scale;
+        return out;
+    }
+
+    static variable_list backward(AutogradContext *ctx, const variable_list &grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        variable_list out(7);
+        {
+            at::AutoDispatchBelowADInplaceOrView below_autograd;
+            const WindowAttention a(saved[0], saved[1], saved[2], saved[3], ctx->saved_data["window"].toInt(), ctx->saved_data["sinks"].toInt(),
+                                    ctx->saved_data["scale"].toDouble());
+            const at::Tensor g = grads[0].contiguous();
+            for (int i = 0; i < 3; ++i) out[i] = at::empty(saved[i].sizes(), saved[i].options().memory_format(at::MemoryFormat::Contiguous));
+            check_in_backward(sig_window_attention_backward(default_ctx, &a.shape, data(a.q), data(a.k), data(a.v), whole_numbers(a.lengths), data(saved[5]),
+                                                            floats(saved[4]), data(g), own_data(out[0]), own_data(out[1]), own_data(out[2]), current_stream()),
+                              "sig_window_attention_backward");
+        }
+        return first_order_only(std::move(out), saved, grads);
+    }
+};
+
 // ---------------------------------------------------------------- Python
 bool optional_tensor_arg(PyObject *o, at::Tensor *t)
 {
@@ -547,6 +632,54 @@ PyObject *py_linear_attention_step(PyObject *, PyObject *const *args, Py_ssize_t
     });
 }
 
+// a whole number of at least `least`
+bool count_arg(PyObject *o, int64_t least, const char *name, int64_t *value)
+{
+    PyObject *number = PyNumber_Index(o);
+    if (!number) return false;
+    const long long v = PyLong_AsLongLong(number);
+    Py_DECREF(number);
+    if (v == -1 && PyErr_Occurred()) return false;
+    if (v < least) {
+        PyErr_Format(PyExc_ValueError, "%s must be at least %lld", name, (long long)least);
+        return false;
+    }
+    *value = v;
+    return true;
+}
+
+// (window or None, sinks) of an attention call
+bool window_args(PyObject *window, PyObject *sinks, int64_t *w, int64_t *s)
+{
+    *w = 0;
+    return (window == Py_None || count_arg(window, 1, "window", w)) && count_arg(sinks, 0, "sinks", s);
+}
+
+// (q, k, v, window, sinks, lengths, scale)
+template <bool DIFFERENTIABLE>
+PyObject *py_window_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!arity(n, 7)) return nullptr;
+    const at::Tensor *t[3];
+    for (int i = 0; i < 3; ++i)
+        if (!(t[i] = tensor_arg(args[i]))) return nullptr;
+    int64_t window, sinks;
+    at::Tensor lengths;
+    double scale;
+    if (!window_args(args[3], args[4], &window, &sinks) || !optional_tensor_arg(args[5], &lengths) || !scale_arg(args[6], *t[0], &scale)) return nullptr;
+    return guarded([&] {
+        at::Tensor o = unlocked([&] {
+            const char *names[] = {"q", "k", "v"};
+            for (int i = 0; i < 3; ++i) four_dimensions(*t[i], names[i]);
+            if (DIFFERENTIABLE && tracked({t[0], t[1], t[2]}))
+                return DifferentiableWindowAttention::apply(*t[0], *t[1], *t[2], maybe(lengths), window, sinks, scale);
+            at::AutoDispatchBelowADInplaceOrView below_autograd;
+            return WindowAttention(*t[0], *t[1], *t[2], lengths, window, sinks, scale).forward(nullptr);
+        });
+        return THPVariable_Wrap(std::move(o));
+    });
+}
+
 }  // namespace
 
 PyMethodDef sig_torch::sequence_methods[] = {
@@ -558,4 +691,6 @@ PyMethodDef sig_torch::sequence_methods[] = {
     {"autograd_linear_attention", FASTCALL(py_linear_attention<true>),
      "linear_attention(q, k, v, log_decay, state, lengths, scale, return_state) with a gradient"},
     {"linear_attention_step", FASTCALL(py_linear_attention_step), "linear_attention_step(q, k, v, log_decay, state, scale, out_state)"},
+    {"window_attention", FASTCALL(py_window_attention<false>), "window_attention(q, k, v, window, sinks, lengths, scale)"},
+    {"autograd_window_attention", FASTCALL(py_window_attention<true>), "window_attention(q, k, v, window, sinks, lengths, scale) with a gradient"},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,96 @@
+// Entry points of softmax attention with a sliding window (include/sig_sequence.h): argument checks and launches.
+#include "sig_window.h"
+
+#include "sig_context.h"
+
+using namespace sig;
+
+namespace {
+
+constexpr int kMostDim = 256;
+constexpr double kLog2E = 1.4426950408889634;
+
+int check(const sig_ctx *ctx, const sig_window_t *s)
+{
+    if (!ctx || !s || s->B < 0 || s->T < 0 || s->heads < 1 || s->shared_heads < 1 || s->heads % s->shared_heads || s->key_dim < 1 || s->value_dim < 1 ||
+        s->window < 0 || s->sinks < 0 || !valid_type(s->type) || !(fabsf(s->scale) <= FLT_MAX))
+        return SIG_ERR_INVALID;
+    if (s->key_dim > kMostDim || s->value_dim > kMostDim) return SIG_ERR_UNSUPPORTED;
+    // (a grid of 2^24 x 2^15 workgroups of 64 tokens or more)
+    if (s->T >= INT32_MAX - 1023 || s->B > INT32_MAX / s->heads || (s->T > 0 && s->B * s->heads > ((int64_t)1 << 39) / (s->T + 127))) return SIG_ERR_TOO_LARGE;
+    return SIG_OK;
+}
+
+WindowArgs arguments(const sig_window_t &s, const void *q, const void *k, const void *v, const int64_t *lengths)
+{
+    WindowArgs A = {};
+    A.q = q;
+    A.k = k;
+    A.v = v;
+    for (int i = 0; i < 3; ++i) {
+        A.qs[i] = s.q_strides[i];
+        A.ks[i] = s.k_strides[i];
+        A.vs[i] = s.v_strides[i];
+    }
+    A.lengths = lengths;
+    A.B = s.B;
+    A.T = (int)s.T;
+    A.heads = s.heads;
+    A.group = s.heads / s.shared_heads;
+    A.K = s.key_dim;
+    A.V = s.value_dim;
+    A.window = (int)(s.window == 0 || s.window > s.T ? s.T : s.window);
+    A.sinks = (int)(s.sinks > s.T ? s.T : s.sinks);
+    A.scale = s.scale;
+    // (a scale of 0 is taken as the smallest one, so that the scores of what is hidden stay minus infinity)
+    A.power = fmaxf((float)(fabs((double)s.scale) * kLog2E), FLT_MIN);
+    A.negated = s.scale < 0.0f;
+    return A;
+}
+
+hipError_t launch(const WindowArgs &A, int type, WindowPass pass, hipStream_t st)
+{
+    return type == SIG_F32 ? launch_window_f32(A, pass, st) : type == SIG_BF16 ? launch_window_bf16(A, pass, st) : launch_window_f16(A, pass, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths, void *out,
+                         float *stats, void *hip_stream)
+{
+    const int rc = check(ctx, shape);
+    if (rc != SIG_OK) return rc;
+    if (shape->B == 0 || shape->T == 0) return SIG_OK;
+    if (!q || !k || !v || !out) return SIG_ERR_INVALID;
+    WindowArgs A = arguments(*shape, q, k, v, lengths);
+    A.out = out;
+    A.stats = (float2 *)stats;
+    return launch(A, shape->type, WINDOW_FORWARD, (hipStream_t)hip_stream) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+}
+
+int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
+                                  const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream)
+{
+    int rc = check(ctx, shape);
+    if (rc != SIG_OK) return rc;
+    if (shape->B == 0 || shape->T == 0) return SIG_OK;
+    if (!q || !k || !v || !out || !stats || !grad_out || !grad_q || !grad_k || !grad_v) return SIG_ERR_INVALID;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    WindowArgs A = arguments(*shape, q, k, v, lengths);
+    A.out = (void *)out;
+    A.stats = (float2 *)stats;
+    A.grad_out = grad_out;
+    A.grad_q = grad_q;
+    A.grad_k = grad_k;
+    A.grad_v = grad_v;
+    Scratch scratch;
+    rc = scratch.get(ctx, (size_t)(A.B * A.heads) * A.T * sizeof(float), st, &A.delta);
+    if (rc != SIG_OK) return rc;
+    hipError_t e = launch(A, shape->type, WINDOW_QUERY_GRADIENT, st);
+    if (e == hipSuccess) e = launch(A, shape->type, WINDOW_KEY_GRADIENT, st);
+    return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,253 @@
+"""Softmax attention with a sliding window and first tokens that stay visible, against its definition in 64 bits on the CPU.
+
+Tolerances.  u is the rounding unit of the type (2^-24, 2^-8 and 2^-11 for float32, bfloat16 and float16).  Each output is rounded once, and so
+is each factor of a product's sum that is not an operand (the probabilities p, the gradient's terms p (g . v - D)), and the output that D = g . o is
+worked out from: u each, relative to what the sum adds up without its signs.  Float32 sums and exponents of a few
+units add 64 * 2^-24.  Frobenius norms of errors are therefore held to 2 u + 64 * 2^-24 times the norm of the same sum with all magnitudes:
+  o: p |v|     grad v: p' |g|     grad q, grad k: c w |k|, c w' |q| with w = p (|g| . |v| + |g| . |o|)
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2501_08455_amd import autograd, binding
+
+gpu = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def noise(*shape, seed=0, kind=torch.float32):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed * 7919 + sum(shape)), dtype=torch.float64).to(kind)
+
+
+def seen_by(T, window, sinks):
+    at = torch.arange(T)
+    gap = at[:, None] - at
+    return (gap >= 0) & ((gap < (window or T + 1)) | (at < sinks))
+
+
+def reference(q, k, v, window, sinks, lengths, scale, grad=None):
+    """{name: (value, norm of the sum of magnitudes)}"""
+    q, k, v = (t.detach().cpu().double() for t in (q, k, v))
+    B, T, H, K = q.shape
+    G, V = k.shape[2], v.shape[3]
+    r, c = H // G, K ** -0.5 if scale is None else scale
+    n = torch.full((B,), T) if lengths is None else lengths.cpu().clamp(0, T)
+    live = (torch.arange(T) < n[:, None])
+    q, k, v = (torch.where(live[:, :, None, None], t, 0.0) for t in (q, k, v))
+    q, k, v = q.transpose(1, 2), k.transpose(1, 2).repeat_interleave(r, 1), v.transpose(1, 2).repeat_interleave(r, 1)
+    seen = seen_by(T, window, sinks)
+    p = torch.softmax((c * (q @ k.transpose(2, 3))).masked_fill(~seen, -math.inf), -1) * live[:, None, :, None]
+    o = p @ v
+    shape = lambda t: t.transpose(1, 2)      # noqa: E731
+    out = {"o": (shape(o), float((p @ v.abs()).norm()))}
+    if grad is not None:
+        g = torch.where(live[:, :, None, None], grad.cpu().double(), 0.0).transpose(1, 2)
+        u = p * (g @ v.transpose(2, 3) - (g * o).sum(-1, keepdim=True))
+        w = p * (g.abs() @ v.abs().transpose(2, 3) + (g * o).abs().sum(-1, keepdim=True))
+        heads = lambda t: t.unflatten(1, (G, r)).sum(2)      # noqa: E731
+        out["grad q"] = (shape(c * u @ k), abs(c) * float((w @ k.abs()).norm()))
+        out["grad k"] = (shape(heads(c * u.transpose(2, 3) @ q)), abs(c) * float(heads(w.transpose(2, 3) @ q.abs()).norm()))
+        out["grad v"] = (shape(heads(p.transpose(2, 3) @ g)), float(heads(p.transpose(2, 3) @ g.abs()).norm()))
+    return out
+
+
+def assert_near(got, want, what=""):
+    value, size = want
+    kind, got = got.dtype, got.detach().cpu().double()
+    assert got.shape == value.shape, (what, got.shape, value.shape)
+    err = float((got - value).norm())
+    assert err <= (2 * UNIT[kind] + 64 * 2.0 ** -24) * size or err == 0.0, (what, err / size if size else err)
+
+
+SHAPES = [   # B, T, heads, shared, K, V, window, sinks
+    (1, 1, 1, 1, 1, 1, None, 0), (3, 2, 2, 1, 5, 3, 1, 0), (2, 33, 4, 2, 40, 72, 5, 2), (2, 129, 2, 1, 64, 64, None, 0), (1, 300, 2, 2, 128, 128, 64, 3),
+    (2, 257, 4, 4, 33, 130, 100, 70), (1, 200, 8, 1, 256, 256, None, 0), (1, 500, 2, 2, 64, 64, 1, 0), (2, 160, 3, 3, 96, 24, 31, 33), (1, 1000, 1, 1, 128, 128, 128, 128),
+    (2, 70, 6, 2, 192, 16, 1000, 0), (1, 129, 1, 1, 65, 129, 128, 1), (5, 64, 2, 2, 8, 8, 63, 1), (1, 700, 8, 2, 64, 64, 129, 5), (8, 40, 3, 1, 7, 11, 3, 39),
+    (2, 400, 2, 2, 80, 80, 200, 300), (9, 31, 8, 8, 32, 32, 2, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_outputs_and_gradients(shape, kind):
+    B, T, H, G, K, V, window, sinks = shape
+    q, k, v = (noise(B, T, h, d, seed=i, kind=kind).cuda().requires_grad_(True) for i, (h, d) in enumerate(((H, K), (G, K), (G, V))))
+    g = noise(B, T, H, V, seed=4, kind=kind).cuda()
+    o = autograd.window_attention(q, k, v, window=window, sinks=sinks)
+    grads = torch.autograd.grad(o, (q, k, v), g)
+    want = reference(q, k, v, window, sinks, None, None, g)
+    assert_near(o, want["o"], "o")
+    for name, got, leaf in zip(("grad q", "grad k", "grad v"), grads, (q, k, v)):
+        assert got.dtype == leaf.dtype and got.is_contiguous()
+        assert_near(got, want[name], name)
+    assert torch.equal(o, binding.window_attention(q.detach(), k.detach(), v.detach(), window=window, sinks=sinks))
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("window,sinks", [(None, 0), (20, 3), (1, 0)])
+def test_ragged_sequences(window, sinks, kind):
+    """What stands behind a sequence is not read, and gives zeros."""
+    B, T, H, G, K, V = 7, 150, 4, 2, 40, 24
+    lengths = torch.tensor([0, 1, 31, 150, 128, 400, -3], device="cuda")
+    q, k, v = (noise(B, T, h, d, seed=i, kind=kind).cuda() for i, (h, d) in enumerate(((H, K), (G, K), (G, V))))
+    g = noise(B, T, H, V, seed=4, kind=kind).cuda()
+    want = reference(q, k, v, window, sinks, lengths, None, g)
+    behind = torch.arange(T, device="cuda") >= lengths[:, None]
+    q, k, v, g = (t.masked_fill(behind[:, :, None, None], math.nan) for t in (q, k, v, g))
+    q, k, v = (t.requires_grad_(True) for t in (q, k, v))
+    o = autograd.window_attention(q, k, v, window=window, sinks=sinks, lengths=lengths)
+    grads = torch.autograd.grad(o, (q, k, v), g)
+    for name, got in zip(("o", "grad q", "grad k", "grad v"), (o, *grads)):
+        assert_near(got, want[name], name)
+        assert not got.detach().masked_select(behind[:, :, None, None]).any()
+    assert torch.equal(o, autograd.window_attention(q, k, v, window=window, sinks=sinks, lengths=lengths.int()))
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_strides(kind):
+    """Views of one projection, transposed and broadcast operands, an odd offset, a reversed axis, a last axis apart."""
+    B, T, H, K = 2, 90, 4, 24
+    fused = noise(B, T, 3 * H, K, seed=1, kind=kind).cuda()
+    by_head = noise(B, H, T, K, seed=2, kind=kind).cuda().transpose(1, 2)
+    shared = noise(1, T, 1, K, seed=3, kind=kind).cuda().expand(B, T, 2, K)
+    odd = noise(B * T * H * K + 1, seed=4, kind=kind).cuda()[1:].view(B, T, H, K)
+    flipped = noise(B, T, H, 2 * K, seed=6, kind=kind).cuda()[..., ::2]
+    for q, k, v in ((fused[:, :, :H], fused[:, :, H:2 * H], fused[:, :, 2 * H:]), (by_head, odd, flipped), (odd, shared, shared), (flipped, by_head, odd)):
+        q, k, v = (t.detach().requires_grad_(True) for t in (q, k, v))
+        g = noise(B, T, H, K, seed=5, kind=kind).cuda().transpose(0, 1).contiguous().transpose(0, 1)
+        o = autograd.window_attention(q, k, v, window=17, sinks=2)
+        grads = torch.autograd.grad(o, (q, k, v), g)
+        want = reference(q, k, v, 17, 2, None, None, g)
+        for name, got in zip(("o", "grad q", "grad k", "grad v"), (o, *grads)):
+            assert_near(got, want[name], name)
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.3, 0.5])
+def test_scales(scale, kind):
+    q, k, v = (noise(2, 70, 2, 16, seed=i, kind=kind).cuda().requires_grad_(True) for i in range(3))
+    g = noise(2, 70, 2, 16, seed=4, kind=kind).cuda()
+    o = autograd.window_attention(q, k, v, window=30, sinks=1, scale=scale)
+    want = reference(q, k, v, 30, 1, None, scale, g)
+    for name, got in zip(("o", "grad q", "grad k", "grad v"), (o, *torch.autograd.grad(o, (q, k, v), g))):
+        assert_near(got, want[name], name)
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+def test_large_scores(kind):
+    """Scores of some hundreds: one key takes all.  z has an error of 2^-24 of a few hundred there, so p's is up to 2^-24 * 400 * 4, over the types' own."""
+    q, k, v = (noise(1, 200, 2, 64, seed=i, kind=kind).cuda() for i in range(3))
+    q, k = q * 8, k * 8
+    o = binding.window_attention(q, k, v, window=64, sinks=2)
+    value, size = reference(q, k, v, 64, 2, None, None)["o"]
+    assert float((o.cpu().double() - value).norm()) <= (2 * UNIT[kind] + (64 + 1600) * 2.0 ** -24) * size
+
+
+def visible_reference(q, k, v, window, sinks, g):
+    """Row by row, only over what is seen (in a product of matrices what is hidden would count)."""
+    q, k, v, g = (t.cpu().double() for t in (q, k, v, g))
+    T, c = q.shape[0], q.shape[1] ** -0.5
+    seen = seen_by(T, window, sinks)
+    o, gq, gk, gv = (torch.zeros_like(t) for t in (v, q, k, v))
+    for t in range(T):
+        at = seen[t].nonzero()[:, 0]
+        p = torch.softmax(c * (k[at] @ q[t]), 0)
+        o[t] = (p[:, None] * v[at]).sum(0)
+        u = p * (v[at] @ g[t] - (g[t] * o[t]).sum())
+        gq[t] = c * (u[:, None] * k[at]).sum(0)
+        gk[at] += c * u[:, None] * q[t]
+        gv[at] += p[:, None] * g[t]
+    return o, gq, gk, gv
+
+
+@gpu
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("what", ["q", "k", "v", "grad"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("where", [0, 37, 128, 199])
+def test_what_is_not_finite_reaches_only_what_sees_it(where, bad, what, kind):
+    T, window, sinks, K = 200, 23, 2, 40
+    ops = dict(q=noise(T, K, seed=1, kind=kind), k=noise(T, K, seed=2, kind=kind), v=noise(T, K, seed=3, kind=kind), grad=noise(T, K, seed=4, kind=kind))
+    ops[what][where, 7] = bad
+    want = visible_reference(ops["q"], ops["k"], ops["v"], window, sinks, ops["grad"])
+    q, k, v, g = (ops[n].cuda()[None, :, None] for n in ("q", "k", "v", "grad"))
+    q, k, v = (t.requires_grad_(True) for t in (q, k, v))
+    o = autograd.window_attention(q, k, v, window=window, sinks=sinks)
+    for name, got, value in zip(("o", "grad q", "grad k", "grad v"), (o, *torch.autograd.grad(o, (q, k, v), g)), want):
+        got = got.detach().cpu().double()[0, :, 0]
+        finite = torch.isfinite(value)
+        assert torch.equal(torch.isfinite(got), finite), (name, (torch.isfinite(got) != finite).nonzero()[:4])
+        if name == "o":
+            assert torch.equal(torch.isnan(got), torch.isnan(value)) and torch.equal(got[torch.isinf(got)], value[torch.isinf(value)])
+        # (rows apart from what is not finite: as elsewhere, and the sums of magnitudes are at most a few times the values' norm)
+        assert float((got[finite] - value[finite]).norm()) <= 8 * (2 * UNIT[kind] + 64 * 2.0 ** -24) * float(value[finite].norm()), name
+
+
+@gpu
+def test_gradient_against_differences():
+    """(f(x + h d) - f(x - h d)) / 2 h along random directions d, f summed in 64 bits from float32 outputs.  With h = 2^-7 the third derivative leaves
+    some h^2 = 6e-5, and outputs of 2^-24 each, 3,600 of them with random signs, 60 * 2^-24 / h = 5e-4 of the gradient's norm of one direction, about 1."""
+    B, T, H, G, K, V = 1, 60, 2, 1, 20, 30
+    x = [noise(B, T, h, d, seed=i).cuda() for i, (h, d) in enumerate(((H, K), (G, K), (G, V)))]
+    g = noise(B, T, H, V, seed=4).cuda()
+    leaves = [t.clone().requires_grad_(True) for t in x]
+    grads = torch.autograd.grad(autograd.window_attention(*leaves, window=11, sinks=3), leaves, g)
+
+    def f(*t):
+        return float((binding.window_attention(*t, window=11, sinks=3).double() * g.double()).sum())
+
+    for i in range(3):
+        d = noise(*x[i].shape, seed=10 + i).cuda()
+        d = d / d.norm()
+        h = 2.0 ** -7
+        up, down = list(x), list(x)
+        up[i], down[i] = x[i] + h * d, x[i] - h * d
+        slope, want = (f(*up) - f(*down)) / (2 * h), float((grads[i].double() * d.double()).sum())
+        assert abs(slope - want) <= 2e-3 * max(1.0, abs(want)), (i, slope, want)
+
+
+@gpu
+def test_the_same_bits_every_time():
+    q, k, v = (noise(2, 500, 4, 64, seed=i, kind=torch.bfloat16).cuda().requires_grad_(True) for i in range(3))
+    g = noise(2, 500, 4, 64, seed=4, kind=torch.bfloat16).cuda()
+    first = None
+    for _ in range(4):
+        o = autograd.window_attention(q, k, v, window=100, sinks=4)
+        got = (o, *torch.autograd.grad(o, (q, k, v), g))
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+@gpu
+def test_refusals():
+    q = torch.zeros(2, 5, 4, 8, device="cuda")
+    call = binding.window_attention
+    for bad in (dict(window=0), dict(window=-1), dict(sinks=-1), dict(scale=math.inf), dict(scale=math.nan), dict(lengths=torch.zeros(3, device="cuda", dtype=torch.int64)),
+                dict(lengths=torch.zeros(2, device="cuda")), dict(lengths=torch.zeros(2, dtype=torch.int64))):
+        with pytest.raises(ValueError):
+            call(q, q, q, **bad)
+    for k, v in ((q[:, :, :3], q[:, :, :3]), (q[:, :4], q[:, :4]), (q[..., :7], q), (q, q[:, :, :2]), (q.bfloat16(), q), (q, q.cpu()), (q[0], q)):
+        with pytest.raises(ValueError):
+            call(q, k, v)
+    with pytest.raises(ValueError):
+        call(q.double(), q.double(), q.double())
+    with pytest.raises(TypeError):
+        call(q, q, q, window=2.5)
+    with pytest.raises(binding.SigError) as error:
+        call(*(torch.zeros(1, 2, 1, 257, device="cuda") for _ in range(3)))
+    assert error.value.status == binding.SIG_ERR_UNSUPPORTED
+    for shape in ((0, 5, 4, 8), (2, 0, 4, 8)):
+        x = torch.zeros(shape, device="cuda", requires_grad=True)
+        o = autograd.window_attention(x, x, x)
+        assert o.shape == shape and torch.autograd.grad(o.sum(), x)[0].shape == shape
+    x = q.clone().requires_grad_(True)
+    (gx,) = torch.autograd.grad(autograd.window_attention(x, x, x).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivative"):
+        gx.sum().backward()
