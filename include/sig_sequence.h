@@ -21,7 +21,7 @@
 extern "C" {
 #endif
 
-enum sig_type { SIG_F32 = 0, SIG_BF16 = 1, SIG_F16 = 2 };
+enum sig_type { SIG_F32 = 0, SIG_BF16 = 1, SIG_F16 = 2, SIG_E4M3 = 3 /* of a cache's pages only */ };
 
 /*
  * Layer norm of each row:  h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps),  y = h * weight + bias.
@@ -153,6 +153,81 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
                                   const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
+
+/*
+ * A paged cache of keys and values.  The place p of a sequence b is slot p % page_tokens of page table[b][p / page_tokens], for all heads.
+ *   keys, values DEVICE, [pages][heads][page_tokens][key_dim or value_dim] of `type`; strides in values between pages, heads and slots;
+ *                the last axis is contiguous, pages do not overlap
+ *   key_scales, value_scales   DEVICE, float32 [pages][heads], contiguous, for pages of SIG_E4M3 (8 bits: 4 of exponent, 3 of fraction, the largest
+ *                value 448): a value stands for itself times its page's and head's scale.  NULL for the other types
+ *   table        DEVICE, int32 [sequences][table_pages], rows table_stride apart
+ * Places behind the table's end, and places whose page is not one of 0 ... pages - 1, do not exist: nothing is written there and nothing seen.  So
+ * pages that a window has left may go to other sequences.  Calls that only read may share pages; a page that two sequences of one call write to
+ * holds what either wrote, slot by slot (in 8 bits: with either's scale).
+ */
+typedef struct sig_cache_t {
+    int64_t pages, page_tokens;
+    int32_t heads, key_dim, value_dim;
+    int32_t type;
+    void *keys, *values;
+    float *key_scales, *value_scales;
+    int64_t key_strides[3], value_strides[3];
+    const int32_t *table;
+    int64_t table_pages, table_stride;
+} sig_cache_t;
+
+/*
+ * Keys and values of new tokens into a cache: token t of sequence b, which holds lengths[b], goes to place lengths[b] + t.  Keys are turned on the way
+ * as sig_rotary does it, and so are the tokens' queries, into an array of their own.
+ *   k, v         DEVICE, [B][T][cache heads][key_dim or value_dim] of `type`; strides as everywhere
+ *   q, q_out     DEVICE, [B][T][heads][key_dim] of `type`, q_out contiguous and apart from q; both NULL where heads == 0
+ *   lengths      DEVICE, int64 [B] (negative ones are taken as 0)
+ *   counts       DEVICE, int64 [B], new tokens of each sequence (taken into 0 ... T); NULL: T.  Those behind them are not read; their queries
+ *                give zeros
+ *   positions    DEVICE, of `position_type`, position_strides[2] values apart between sequences and tokens; NULL: the places
+ *   frequencies  DEVICE, float64 [turned / 2]; turned, interleaved, scale: see sig_rotary.  turned == 0 and scale == 1 leave keys as they are
+ * The cache's type is `type`, or SIG_E4M3.  Then a page's scale is the smallest power of two (2^-126 or more) that is at least the largest
+ * magnitude / 448 of what it holds of a head (1 for zeros), and never less than it was while the page keeps earlier tokens: a page
+ * whose slot 0 is written by the call keeps none, what another one holds is rounded anew when its scale grows (which changes only values below 2^-6 of
+ * the new scale).  Values are rounded once, from float32; what is not finite is NaN there and counts as 0.
+ * Limits of sig_rotary for turned; 2^31 tokens (B * T) or more, or heads or values of a token, SIG_ERR_TOO_LARGE.  No context scratch.
+ */
+typedef struct sig_append_t {
+    int64_t B, T;
+    int32_t heads, type;
+    int64_t q_strides[3], k_strides[3], v_strides[3];
+    const void *positions;
+    int32_t position_type, interleaved;
+    int64_t position_strides[2];
+    const double *frequencies;
+    int64_t turned;
+    double scale;
+} sig_append_t;
+
+int sig_cache_append(sig_ctx *ctx, const sig_cache_t *cache, const sig_append_t *shape, const void *q, const void *k, const void *v,
+                     const int64_t *lengths, const int64_t *counts, void *q_out, void *hip_stream);
+
+/*
+ * Softmax attention of the last tokens of each sequence over a cache: query t of sequence b stands at place lengths[b] - counts[b] + t and sees what
+ * sig_window_attention's token there sees.  T == 1 is the form for single tokens.
+ *   q            DEVICE, [B][T][heads][key_dim] of `type`; head h reads the cache's head h / (heads / cache heads)
+ *   lengths      DEVICE, int64 [B]: what each sequence holds, these tokens included (places behind the table's end do not exist)
+ *   counts       DEVICE, int64 [B], queries of each sequence (taken into 0 ... T); NULL: T.  Those behind them are not read and give zeros
+ *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous.  A query that sees nothing gives zeros
+ * The cache's type is `type`, or SIG_E4M3.  Probabilities of 16-bit calls keep 16 (bfloat16) and 22 (float16) digits; sums are float32's.
+ * Limits of sig_window_attention, and 2^31 - 1024 places at most; more than 2^31 groups of 16 queries are SIG_ERR_TOO_LARGE.  Context scratch where sequences are
+ * cut along their places because there are few: (value_dim + 2) floats for each query and part, of at most two workgroups' parts for each compute unit.
+ */
+typedef struct sig_queries_t {
+    int64_t B, T;
+    int32_t heads, type;
+    float scale;
+    int64_t window, sinks;
+    int64_t q_strides[3];
+} sig_queries_t;
+
+int sig_cache_attention(sig_ctx *ctx, const sig_cache_t *cache, const sig_queries_t *shape, const void *q, const int64_t *lengths, const int64_t *counts,
+                        void *out, void *hip_stream);
 
 #ifdef __cplusplus
 }

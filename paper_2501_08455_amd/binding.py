@@ -20,7 +20,7 @@ SIG_ERR_NO_DEVICE = 5
 
 SIG_ERR_UNSUPPORTED = 6
 SIG_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
-SIG_F32, SIG_BF16, SIG_F16 = 0, 1, 2
+SIG_F32, SIG_BF16, SIG_F16, SIG_E4M3 = 0, 1, 2, 3
 SIG_POSITION_I32, SIG_POSITION_I64, SIG_POSITION_F32, SIG_POSITION_F64 = 0, 1, 2, 3
 SIG_VARIANT_AUTO = 0
 SIG_VARIANT_HBM_STREAMING = 1
@@ -54,6 +54,28 @@ class sig_window_t(ctypes.Structure):
                 ("key_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("window", ctypes.c_int64), ("sinks", ctypes.c_int64),
                 ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3)]
+
+
+class sig_cache_t(ctypes.Structure):
+    """A paged cache (include/sig_sequence.h)."""
+    _fields_ = [("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("heads", ctypes.c_int32), ("key_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("keys", ctypes.c_void_p), ("values", ctypes.c_void_p),
+                ("key_scales", ctypes.c_void_p), ("value_scales", ctypes.c_void_p), ("key_strides", ctypes.c_int64 * 3),
+                ("value_strides", ctypes.c_int64 * 3), ("table", ctypes.c_void_p), ("table_pages", ctypes.c_int64), ("table_stride", ctypes.c_int64)]
+
+
+class sig_append_t(ctypes.Structure):
+    """Shape of a sig_cache_append call (include/sig_sequence.h)."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("heads", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3),
+                ("positions", ctypes.c_void_p), ("position_type", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("position_strides", ctypes.c_int64 * 2), ("frequencies", ctypes.c_void_p), ("turned", ctypes.c_int64), ("scale", ctypes.c_double)]
+
+
+class sig_queries_t(ctypes.Structure):
+    """Shape of a sig_cache_attention call (include/sig_sequence.h)."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("heads", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("window", ctypes.c_int64), ("sinks", ctypes.c_int64), ("q_strides", ctypes.c_int64 * 3)]
 
 
 class SigError(RuntimeError):
@@ -128,6 +150,10 @@ def load():
     lib.sig_window_attention.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 7
     lib.sig_window_attention_backward.restype = i32
     lib.sig_window_attention_backward.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 11
+    lib.sig_cache_append.restype = i32
+    lib.sig_cache_append.argtypes = [vp, ctypes.POINTER(sig_cache_t), ctypes.POINTER(sig_append_t)] + [vp] * 7
+    lib.sig_cache_attention.restype = i32
+    lib.sig_cache_attention.argtypes = [vp, ctypes.POINTER(sig_cache_t), ctypes.POINTER(sig_queries_t)] + [vp] * 5
     lib.sig_probe_copy.restype = i32
     lib.sig_probe_copy.argtypes = [vp, vp, i64, vp]
     lib.sig_probe_write.restype = i32
@@ -402,3 +428,25 @@ def window_attention(q, k, v, window=None, sinks=0, lengths=None, scale=None):
     keys and values), K and V up to 256.  With `window`, a token sees the last `window` tokens, itself included, and the first `sinks` tokens of
     the sequence; None: all.  `lengths` [B]: tokens from there on are not read and give zeros; `scale` None: K ** -0.5.  Returns o [B, T, H, V]."""
     return (_torch_lib or torch_lib()).window_attention(q, k, v, window, sinks, lengths, scale)
+
+
+def cache_append(k, v, keys, values, table, lengths, counts=None, q=None, positions=None, frequencies=None, interleaved=False, scale=1.0,
+                 key_scales=None, value_scales=None):
+    """Keys and values of new tokens, `k` [B, T, G, K] and `v` [B, T, G, V], into a paged cache, in place: token t of a sequence that holds
+    lengths[b] goes to place p = lengths[b] + t, which is slot p % P of page table[b, p // P].
+
+    `keys` [pages, G, P, K] and `values` [pages, G, P, V] have the type of k and v, or are float8_e4m3fn with `key_scales` and `value_scales` (float32
+    [pages, G]): then a page's scale is the smallest power of two that fits what the page holds of a head, and grows with it.  `table` is int32
+    [B, n]; places without a page (behind the table, or whose entry is not a page's number) are not written.  `counts` [B]: new tokens of each
+    sequence (None: T); those behind them are not read.  With `frequencies` keys are turned by rotary positions on the way (see rotary):
+    the places, or `positions`.  `q` [B, T, H, K], the tokens' queries: returns them turned, as a new tensor (zeros behind the counts); else returns None."""
+    return (_torch_lib or torch_lib()).cache_append(k, v, keys, values, table, lengths, counts, q, positions, frequencies, interleaved, scale,
+                                                    key_scales, value_scales)
+
+
+def cache_attention(q, keys, values, table, lengths, window=None, sinks=0, scale=None, counts=None, key_scales=None, value_scales=None):
+    """window_attention of the last tokens of each sequence over a paged cache (see cache_append): `q` [B, T, H, K], query t at place
+    lengths[b] - counts[b] + t (`counts` None: T), where lengths[b] counts what the sequence holds, these tokens included.  T = 1 is one token of
+    each sequence.  Places without a page are not seen, and pages that a window has left are not read.  Returns o [B, T, H, V]; zeros
+    behind the counts, and for a query that sees nothing."""
+    return (_torch_lib or torch_lib()).cache_attention(q, keys, values, table, lengths, window, sinks, scale, counts, key_scales, value_scales)

@@ -25,6 +25,7 @@ SOURCES = ["sig_api.hip", "sig_streaming.hip", "sig_combine.hip", "sig_onchip_ta
            "sig_layer_norm.hip", "sig_rotary.hip", "sig_attention.hip", "sig_attention_recurrent.hip", "sig_attention_chunk.hip",
            "sig_attention_chunk_bf16.hip", "sig_attention_chunk_f32.hip", "sig_attention_chunk_f16.hip",
            "sig_window.hip", "sig_window_bf16.hip", "sig_window_f32.hip", "sig_window_f16.hip",
+           "sig_cache_append.hip", "sig_cache_attention.hip", "sig_cache_attention_bf16.hip", "sig_cache_attention_f32.hip", "sig_cache_attention_f16.hip",
            "sig_backward.hip", "sig_backward_segments.hip", "sig_backward_general.hip", "sig_bracket.hip", "sig_stream_gradient.hip", "sig_levelscan.hip", "sig_levelscan_rows.hip", "sig_probe.hip"]
 
 TORCH_SOURCES = ["sig_torch.cpp", "sig_torch_sequence.cpp"]

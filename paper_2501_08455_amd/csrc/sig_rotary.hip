@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "sig_context.h"
+#include "sig_turn.h"
 #include "sig_types.h"
 
 using namespace sig;
@@ -31,25 +32,6 @@ struct RotaryArgs {
     int places;                      // threads of a line, a power of two
 };
 
-__device__ double position_of(const RotaryArgs &A, int64_t b, int64_t t)
-{
-    const int64_t at = b * A.ps[0] + t * A.ps[1];
-    switch (A.position_type) {
-    case SIG_POSITION_I32: return (double)((const int32_t *)A.positions)[at];
-    case SIG_POSITION_I64: return (double)((const int64_t *)A.positions)[at];
-    case SIG_POSITION_F32: return (double)((const float *)A.positions)[at];
-    default: return ((const double *)A.positions)[at];
-    }
-}
-
-// cos and sin of position * frequency.  The turns are reduced in 64 bits: a position of a million times a frequency of one
-// radian has no digit left behind the point in 32.
-__device__ void turn(double position, double frequency, float *c, float *s)
-{
-    const double turns = position * (frequency * 0.15915494309189535);
-    sincospif(2.0f * (float)(turns - rint(turns)), s, c);
-}
-
 // N neighbouring values, or N pairs of the half layout, are a turned unit, M neighbouring values a copied one; a line is a token's head, its
 // turned units first.  The last copied unit ends with the line, if that means that it overlaps the one before, or, where there are fewer
 // than M values to copy, is those.  `places` threads take a line.  (Copied values in the turned units' width: 10 and 20 of 40 and 20 of 80 bfloat16
@@ -74,7 +56,7 @@ __global__ __launch_bounds__(kThreads) void sig_rotary_kernel(const T *x, T *y, 
         if (i < tokens * half) {
             const int64_t token = first + i / half;
             float c, s;
-            turn(position_of(A, token / A.T, token % A.T), A.frequencies[i % half], &c, &s);
+            turn(position_at(A.positions, A.position_type, token / A.T * A.ps[0] + token % A.T * A.ps[1]), A.frequencies[i % half], &c, &s);
             table[i] = make_float2(A.scale * c, A.inverse ? -A.scale * s : A.scale * s);
         }
     }

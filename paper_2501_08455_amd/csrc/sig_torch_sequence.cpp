@@ -499,6 +499,149 @@ struct DifferentiableWindowAttention : torch::autograd::Function<DifferentiableW
     }
 };
 
+// ---------------------------------------------------------------- paged cache
+struct Cache {
+    at::Tensor table, key_scales, value_scales;
+    sig_cache_t shape = {};
+
+    // keys, values: [pages, heads, tokens of a page, .]; x: a tensor of the call, whose type they have, or 8 bits
+    Cache(const at::Tensor &keys, const at::Tensor &values, const at::Tensor &table_, const at::Tensor &key_scales_, const at::Tensor &value_scales_,
+          const at::Tensor &x, bool written)
+    {
+        shape.type = type_of(x, "the tensors of new tokens");
+        const bool narrow = keys.scalar_type() == at::kFloat8_e4m3fn;
+        for (const auto &[t, name] : {std::pair<const at::Tensor &, const char *>{keys, "keys"}, {values, "values"}}) {
+            same_place(t, x, name);
+            if (t.dim() != 4) refuse(std::string(name) + " must have four dimensions: pages, heads, tokens of a page, components");
+            if (t.scalar_type() != keys.scalar_type()) refuse("keys and values must have the same type");
+            if (!narrow && t.scalar_type() != x.scalar_type()) refuse(std::string(name) + " must have the type of the other operands, or float8_e4m3fn");
+            if (t.size(3) > 1 && t.stride(3) != 1) refuse("the last axis of " + std::string(name) + " must be contiguous");
+            if (written && t.numel() > 0) at::assert_no_internal_overlap(t);
+            for (int i = 0; i < 3; ++i)
+                if (t.size(i) != keys.size(i)) refuse("keys and values must have the same pages, heads and tokens");
+        }
+        if (keys.size(1) < 1 || keys.size(2) < 1 || keys.size(3) < 1 || values.size(3) < 1) refuse("a page must have heads, tokens and components");
+        if (std::max({keys.size(1), keys.size(3), values.size(3)}) > INT32_MAX) refuse("too many heads or components");
+        if (narrow) {
+            shape.type = SIG_E4M3;
+            for (const auto &[t, name] : {std::pair<const at::Tensor &, const char *>{key_scales_, "key_scales"}, {value_scales_, "value_scales"}}) {
+                if (!t.defined()) refuse(std::string("pages of 8 bits need ") + name);
+                same_place(t, x, name);
+                if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != keys.size(0) || t.size(1) != keys.size(1) || !t.is_contiguous())
+                    refuse(std::string(name) + " must be float32 [pages, heads], contiguous");
+            }
+            key_scales = key_scales_;
+            value_scales = value_scales_;
+        } else if (key_scales_.defined() || value_scales_.defined()) {
+            refuse("scales belong to pages of 8 bits (float8_e4m3fn)");
+        }
+        same_place(table_, x, "table");
+        if (table_.dim() != 2 || table_.size(0) != x.size(0) || table_.scalar_type() != at::kInt) refuse("table must be int32 [batch, pages of a sequence]");
+        table = unit_rows(table_);
+        shape.pages = keys.size(0);
+        shape.heads = (int32_t)keys.size(1);
+        shape.page_tokens = keys.size(2);
+        shape.key_dim = (int32_t)keys.size(3);
+        shape.value_dim = (int32_t)values.size(3);
+        shape.keys = written ? own_data(keys) : (void *)data(keys);
+        shape.values = written ? own_data(values) : (void *)data(values);
+        if (narrow) {
+            shape.key_scales = written ? own_floats(key_scales) : (float *)floats(key_scales);
+            shape.value_scales = written ? own_floats(value_scales) : (float *)floats(value_scales);
+        }
+        for (int i = 0; i < 3; ++i) {
+            shape.key_strides[i] = keys.stride(i);
+            shape.value_strides[i] = values.stride(i);
+        }
+        shape.table = table.const_data_ptr<int32_t>();
+        shape.table_pages = table.size(1);
+        shape.table_stride = table.stride(0);
+    }
+};
+
+at::Tensor needed_per_element(const at::Tensor &t, const at::Tensor &x, const char *name)
+{
+    if (!t.defined()) refuse(std::string(name) + " must be given");
+    return per_element(t, x, x.size(0), name);
+}
+
+// the turned queries, or an undefined tensor
+at::Tensor cache_append(const at::Tensor &k_, const at::Tensor &v_, const at::Tensor &keys, const at::Tensor &values, const at::Tensor &table, const at::Tensor &lengths_,
+                        const at::Tensor &counts_, const at::Tensor &q_, const at::Tensor &positions, const at::Tensor &frequencies_, bool interleaved, double scale,
+                        const at::Tensor &key_scales, const at::Tensor &value_scales)
+{
+    const int type = type_of(k_, "k");
+    four_dimensions(k_, "k");
+    four_dimensions(v_, "v");
+    same_type(v_, k_, "v");
+    const Cache cache(keys, values, table, key_scales, value_scales, k_, true);
+    const int64_t B = k_.size(0), T = k_.size(1), K = cache.shape.key_dim;
+    if (k_.size(2) != cache.shape.heads || k_.size(3) != K) refuse("k must have the heads and components of keys");
+    if (v_.size(0) != B || v_.size(1) != T || v_.size(2) != cache.shape.heads || v_.size(3) != cache.shape.value_dim)
+        refuse("v must have the batch and length of k, and the heads and components of values");
+    const at::Tensor lengths = needed_per_element(lengths_, k_, "lengths"), counts = per_element(counts_, k_, B, "counts");
+    const at::Tensor k = unit_rows(k_), v = unit_rows(v_);
+    at::Tensor q, out, frequencies;
+    sig_append_t shape = {};
+    shape.B = B;
+    shape.T = T;
+    shape.type = type;
+    if (q_.defined()) {
+        four_dimensions(q_, "q");
+        same_type(q_, k_, "q");
+        if (q_.size(0) != B || q_.size(1) != T || q_.size(3) != K) refuse("q must have the batch, length and components of k");
+        if (q_.size(2) < 1 || q_.size(2) > INT32_MAX) refuse("q must have heads");
+        q = unit_rows(q_);
+        out = at::empty(q.sizes(), q.options().memory_format(at::MemoryFormat::Contiguous));
+        shape.heads = (int32_t)q.size(2);
+    }
+    for (int i = 0; i < 3; ++i) {
+        if (q.defined()) shape.q_strides[i] = q.stride(i);
+        shape.k_strides[i] = k.stride(i);
+        shape.v_strides[i] = v.stride(i);
+    }
+    shape.interleaved = interleaved;
+    shape.scale = scale;
+    std::optional<RotaryPlace> place;
+    if (frequencies_.defined()) {
+        // (places, where positions are not given, are not a tensor of the call)
+        place.emplace(k, positions.defined() ? positions : lengths.unsqueeze(1).expand({B, T}), frequencies_);
+        shape.frequencies = place->frequencies.const_data_ptr<double>();
+        shape.turned = 2 * place->frequencies.size(0);
+        if (positions.defined()) {
+            shape.positions = data(place->positions);
+            shape.position_type = place->type;
+            shape.position_strides[0] = place->strides[0];
+            shape.position_strides[1] = place->strides[1];
+        }
+    } else if (positions.defined()) {
+        refuse("positions need frequencies");
+    }
+    check(sig_cache_append(default_ctx, &cache.shape, &shape, data(q), data(k), data(v), whole_numbers(lengths), whole_numbers(counts), own_data(out), current_stream()),
+          "sig_cache_append");
+    for (const at::Tensor &t : {keys, values, cache.key_scales, cache.value_scales})
+        if (t.defined()) t.unsafeGetTensorImpl()->bump_version();
+    return out;
+}
+
+at::Tensor cache_attention(const at::Tensor &q_, const at::Tensor &keys, const at::Tensor &values, const at::Tensor &table, const at::Tensor &lengths_, int64_t window,
+                           int64_t sinks, double scale, const at::Tensor &counts_, const at::Tensor &key_scales, const at::Tensor &value_scales)
+{
+    const int type = type_of(q_, "q");
+    four_dimensions(q_, "q");
+    const Cache cache(keys, values, table, key_scales, value_scales, q_, false);
+    const int64_t H = q_.size(2);
+    if (q_.size(3) != cache.shape.key_dim) refuse("q must have the components of keys");
+    if (H < 1 || H > INT32_MAX || H % cache.shape.heads) refuse("the heads of q must be a multiple of the heads of the cache");
+    if (!std::isfinite((float)scale)) refuse("scale must be finite");
+    const at::Tensor lengths = needed_per_element(lengths_, q_, "lengths"), counts = per_element(counts_, q_, q_.size(0), "counts"), q = unit_rows(q_);
+    at::Tensor out = at::empty({q.size(0), q.size(1), H, cache.shape.value_dim}, q.options().memory_format(at::MemoryFormat::Contiguous));
+    const sig_queries_t shape = {q.size(0), q.size(1), (int32_t)H, type, (float)scale, window, sinks, {q.stride(0), q.stride(1), q.stride(2)}};
+    check(sig_cache_attention(default_ctx, &cache.shape, &shape, data(q), whole_numbers(lengths), whole_numbers(counts), own_data(out), current_stream()),
+          "sig_cache_attention");
+    return out;
+}
+
 // ---------------------------------------------------------------- Python
 bool optional_tensor_arg(PyObject *o, at::Tensor *t)
 {
@@ -680,6 +823,49 @@ PyObject *py_window_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// (k, v, keys, values, table, lengths, counts, q, positions, frequencies, interleaved, scale, key_scales, value_scales)
+PyObject *py_cache_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!arity(n, 14)) return nullptr;
+    at::Tensor t[14];
+    for (int i : {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 12, 13}) {
+        if (i < 6 && !tensor_arg(args[i])) return nullptr;
+        if (!optional_tensor_arg(args[i], &t[i])) return nullptr;
+    }
+    bool interleaved;
+    double scale;
+    if (!flag_arg(args[10], &interleaved) || !double_arg(args[11], &scale)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        at::Tensor q = unlocked([&] {
+            at::AutoDispatchBelowADInplaceOrView below_autograd;
+            return cache_append(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], t[9], interleaved, scale, t[12], t[13]);
+        });
+        if (!q.defined()) Py_RETURN_NONE;
+        return THPVariable_Wrap(std::move(q));
+    });
+}
+
+// (q, keys, values, table, lengths, window, sinks, scale, counts, key_scales, value_scales)
+PyObject *py_cache_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!arity(n, 11)) return nullptr;
+    at::Tensor t[11];
+    for (int i : {0, 1, 2, 3, 4, 8, 9, 10}) {
+        if (i < 5 && !tensor_arg(args[i])) return nullptr;
+        if (!optional_tensor_arg(args[i], &t[i])) return nullptr;
+    }
+    int64_t window, sinks;
+    double scale;
+    if (!window_args(args[5], args[6], &window, &sinks) || !scale_arg(args[7], t[0], &scale)) return nullptr;
+    return guarded([&] {
+        at::Tensor o = unlocked([&] {
+            at::AutoDispatchBelowADInplaceOrView below_autograd;
+            return cache_attention(t[0], t[1], t[2], t[3], t[4], window, sinks, scale, t[8], t[9], t[10]);
+        });
+        return THPVariable_Wrap(std::move(o));
+    });
+}
+
 }  // namespace
 
 PyMethodDef sig_torch::sequence_methods[] = {
@@ -693,4 +879,8 @@ PyMethodDef sig_torch::sequence_methods[] = {
     {"linear_attention_step", FASTCALL(py_linear_attention_step), "linear_attention_step(q, k, v, log_decay, state, scale, out_state)"},
     {"window_attention", FASTCALL(py_window_attention<false>), "window_attention(q, k, v, window, sinks, lengths, scale)"},
     {"autograd_window_attention", FASTCALL(py_window_attention<true>), "window_attention(q, k, v, window, sinks, lengths, scale) with a gradient"},
+    {"cache_append", FASTCALL(py_cache_append),
+     "cache_append(k, v, keys, values, table, lengths, counts, q, positions, frequencies, interleaved, scale, key_scales, value_scales)"},
+    {"cache_attention", FASTCALL(py_cache_attention),
+     "cache_attention(q, keys, values, table, lengths, window, sinks, scale, counts, key_scales, value_scales)"},
     {nullptr, nullptr, 0, nullptr}};
