@@ -19,9 +19,29 @@ namespace sig {
 
 constexpr int kCacheThreads = 256, kCacheWaves = kCacheThreads / 64;
 constexpr int kQueries = 16;      // of a workgroup
+constexpr int kMostSplits = 1024;      // (a workgroup's queries times their parts are at most that)
+#ifndef CACHE_WAVES
+#define CACHE_WAVES 2
+#endif
+
+// 0 ... 2^31 - 1 over a divisor, as a product
+struct Quotient {
+    uint64_t factor;
+    int shift;
+    explicit Quotient(int64_t divisor)
+    {
+        int bits = 0;
+        while (((int64_t)1 << bits) < divisor) ++bits;
+        shift = 31 + bits;
+        factor = (((uint64_t)1 << shift) + divisor - 1) / divisor;
+    }
+    Quotient() = default;
+    __device__ int operator()(int x) const { return (int)((uint64_t)x * factor >> shift); }
+};
 
 struct CacheAttentionArgs {
     CacheArgs cache;
+    Quotient quotient;                  // by the tokens of a page
     const void *q;
     int64_t qs[3];
     const int64_t *lengths, *counts;
@@ -59,56 +79,64 @@ __device__ inline bool query_place(const CacheAttentionArgs &A, int64_t id, Quer
     return true;
 }
 
-// what is not finite left out, or 1 where there is what `kind` counts: NaN, infinity, minus infinity
-template <typename X>
-__device__ inline typename X::Frag only_finite(typename X::Frag f)
+// 16 bytes of a row of `dim` values, from value `at` on, as they are kept: row_load, and row_values of what it got when that is used.  The last values of a
+// row that is no whole number of loads are the upper ones of a load that ends with the row; beyond the row there are zeros.
+using Row = __attribute__((ext_vector_type(4))) unsigned;
+
+template <typename C, bool WHOLE>
+__device__ inline Row row_load(const C *row, int at, int dim)
 {
-#pragma unroll
-    for (int e = 0; e < X::GROUP; ++e) f[e] = __builtin_isfinite((float)f[e]) ? f[e] : (typename X::E)0.0f;
-    return f;
+    constexpr int COUNT = 16 / sizeof(C), BITS = 8 * sizeof(C);
+    if (WHOLE || dim >= COUNT) return load_words<C, COUNT>(row + (WHOLE || at + COUNT <= dim ? at : dim - COUNT));
+    using Word = std::conditional_t<sizeof(C) == 1, uint8_t, std::conditional_t<sizeof(C) == 2, uint16_t, uint32_t>>;
+    unsigned __int128 bits = 0;
+#pragma unroll 1
+    for (int j = 0; j < dim; ++j) bits = bits >> BITS | (unsigned __int128)__builtin_bit_cast(Word, row[j]) << (128 - BITS);
+    return __builtin_bit_cast(Row, bits);
 }
-template <typename X>
-__device__ inline typename X::Frag only_kind(typename X::Frag f, int kind)
+template <typename C, bool WHOLE>
+__device__ inline Row row_values(Row got, int at, int dim)
 {
-#pragma unroll
-    for (int e = 0; e < X::GROUP; ++e) {
-        const float x = (float)f[e];
-        f[e] = (typename X::E)((kind == 0 ? x != x : kind == 1 ? x == INFINITY : x == -INFINITY) ? 1.0f : 0.0f);
-    }
-    return f;
+    constexpr int COUNT = 16 / sizeof(C), BITS = 8 * sizeof(C);
+    if constexpr (WHOLE) return got;
+    const int over = at + COUNT - dim;
+    if (dim % COUNT && over > 0 && over < COUNT) got = __builtin_bit_cast(Row, __builtin_bit_cast(unsigned __int128, got) >> (over * BITS));
+    return over >= COUNT ? Row{} : got;
 }
 
-// GROUP values of a row of `dim` from component `at` on, as they are kept; zeros beyond the row
-template <typename C, int GROUP>
-__device__ inline Pack<C, GROUP> row_values(const C *row, int at, int dim)
+// values FIRST ... of a row's 16 bytes as an operand's
+template <typename X, typename C, int FIRST>
+__device__ inline typename X::Frag operand(Row got)
 {
-    Pack<C, GROUP> got = {};
-    if (at + GROUP <= dim) {
-        got = load_pack<C, GROUP>(row + at);
+    if constexpr (std::is_same_v<C, Narrow>) {
+        using Pair = __attribute__((ext_vector_type(2))) bf16;
+        Row words;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int word = (int)got[FIRST / 4 + j];
+            words[2 * j] = __builtin_bit_cast(unsigned, (Pair)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, false));
+            words[2 * j + 1] = __builtin_bit_cast(unsigned, (Pair)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, true));
+        }
+        return __builtin_bit_cast(typename X::Frag, words);
     } else {
-#pragma unroll
-        for (int j = 0; j < GROUP; ++j)
-            if (at + j < dim) got.v[j] = row[at + j];
+        return __builtin_bit_cast(typename X::Frag, got);
     }
-    return got;
 }
 
-template <typename E, typename C>
-__device__ inline E widened(C x)
-{
-    if constexpr (std::is_same_v<C, Narrow>) return (E)from_narrow(x);
-    else return (E)x;
-}
-
-// T: of q and out; C: of the cache in memory (Narrow: 8 bits); X: of the products
-template <typename T, typename C, typename X, int D>
-__global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2 : 1) void sig_cache_attention_kernel(CacheAttentionArgs A)
+// T: of q and out; C: of the cache in memory (Narrow: 8 bits); X: of the products; PARTS: of X's type that hold one of q's or a probability; WHOLE: keys
+// and values have D components
+template <typename T, typename C, typename X, int D, int QUERY_PARTS, int PARTS, bool WHOLE>
+__global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? CACHE_WAVES : 1) void sig_cache_attention_kernel(CacheAttentionArgs A)
 {
     using E = typename X::E;
     using Tile = LdsTile<E, D>;
     constexpr bool NARROW = std::is_same_v<C, Narrow>;
-    constexpr int M = X::M, BLOCK = X::STEP, KEYS = BLOCK / M, STEPS = D / X::STEP, OUT = D / M, GROUP = X::GROUP, PARTS = sizeof(E) == 2 ? 2 : 1;
-    static_assert(M == kQueries && X::REGS == 4);
+    constexpr int M = X::M, STEPS = D / X::STEP, OUT = D / M, GROUP = X::GROUP;
+    // places of a block: 8 KB of keys as the products want them (so 64 registers of loads on their way), and as many of values
+    constexpr int BYTES = D * (int)sizeof(E), BLOCK = 8192 / BYTES < X::STEP ? X::STEP : 8192 / BYTES > 64 ? 64 : 8192 / BYTES, KEYS = BLOCK / M, PRODUCTS = BLOCK / X::STEP;
+    constexpr int LOAD = 16 / (int)sizeof(C), OPERANDS = LOAD / GROUP, KEY_LOADS = STEPS / OPERANDS;      // values of a load, operands that they make
+    constexpr int ROW_LOADS = D / LOAD, VALUE_LOADS = BLOCK * ROW_LOADS / 64;
+    static_assert(M == kQueries && X::REGS == 4 && BLOCK * ROW_LOADS % 64 == 0 && STEPS % OPERANDS == 0);
     constexpr int ROOM = BLOCK * Tile::PITCH * (int)sizeof(E) > kQueries * D * 4 ? BLOCK * Tile::PITCH * (int)sizeof(E) : kQueries * D * 4;      // bytes
     __shared__ __attribute__((aligned(16))) char room[kCacheWaves][ROOM];
     __shared__ float maxima[kCacheWaves][kQueries], sums[kCacheWaves][kQueries];
@@ -117,67 +145,93 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, K = A.cache.K, V = A.cache.V, column = lane % M;
     E *values = (E *)room[wave];
 
-    // the lane's query, and the places that it sees: those of the window from `low` on, and the first tokens
+    // the lane's query, and the places that it sees: those of the window, and the first tokens
     const int64_t number = (int64_t)p.tile * kQueries + column, token = number / A.group;
     const bool there = number < p.count;
     const int own = there ? (int)(p.first + token) : -1;
     const int window = (int)(A.window == 0 || A.window > INT32_MAX ? INT32_MAX : A.window), sinks = (int)(A.sinks > INT32_MAX ? INT32_MAX : A.sinks);
-    auto seen = [&](int place) { return place <= own && (own - place < window || place < sinks); };
-    typename X::Frag q[STEPS];
-    fragments_of<X, STEPS>(q, lane, (const T *)A.q + p.b * A.qs[0] + (there ? token : 0) * A.qs[1] + (p.shared * A.group + (there ? number % A.group : 0)) * A.qs[2], K, there, A.negated);
+    // (all of it compared, here and below: branches for single values cost more than the comparisons)
+    auto seen = [&](int place) { return (place <= own) & ((own - place < window) | (place < sinks)); };
+    typename X::Frag q[QUERY_PARTS][STEPS];
+    {
+        const T *line = (const T *)A.q + p.b * A.qs[0] + (there ? token : 0) * A.qs[1] + (p.shared * A.group + (there ? number % A.group : 0)) * A.qs[2];
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
+            // (where the keys' loads have the components of this step)
+            const int at = step / OPERANDS * 4 * LOAD + lane / 16 * LOAD + step % OPERANDS * GROUP;
+            constexpr int COUNT = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int first = 0; first < GROUP; first += COUNT) {
+                const auto got = __builtin_bit_cast(__attribute__((ext_vector_type(COUNT))) T, row_values<T, false>(row_load<T, false>(line, at + first, K), at + first, K));
+#pragma unroll
+                for (int e = 0; e < COUNT; ++e) {
+                    float x = there ? to_float(got[e]) : 0.0f;
+                    if (A.negated) x = -x;
+#pragma unroll
+                    for (int part = 0; part < QUERY_PARTS; ++part) {
+                        q[part][step][first + e] = (E)x;
+                        x -= (float)q[part][step][first + e];
+                        if (x != x) x = 0.0f;      // (infinity less infinity)
+                    }
+                }
+            }
+        }
+    }
 
     // blocks of places that some query of the tile sees
     const int64_t from = (int64_t)p.tile * kQueries, until = min(from + kQueries, p.count);
     int low = 0, high = 0, front = 0, count = 0;
-    if (from < until) {
+    int lowest = 0, highest = -1;      // places of the tile's queries
+    if (from < until && A.cache.pages > 0) {
         const int64_t exist = A.cache.table_pages * A.cache.page_tokens;
-        const int highest = (int)min(p.first + (until - 1) / A.group, exist - 1);
-        low = (int)max((int64_t)0, p.first + from / A.group - window + 1);
-        front = (min(sinks, min(low, highest + 1)) + BLOCK - 1) / BLOCK;
+        lowest = (int)(p.first + from / A.group);
+        highest = (int)(p.first + (until - 1) / A.group);
+        const int last = (int)min((int64_t)highest, exist - 1);
+        low = (int)max((int64_t)0, (int64_t)lowest - window + 1);
+        front = (min(sinks, min(low, last + 1)) + BLOCK - 1) / BLOCK;
         low = max(low / BLOCK, front);
-        high = highest < 0 ? 0 : highest / BLOCK + 1;
+        high = last < 0 ? 0 : last / BLOCK + 1;
         count = front + max(0, high - low);
     }
     const int first_block = (int)((int64_t)count * p.split / A.splits), last_block = (int)((int64_t)count * (p.split + 1) / A.splits);
     auto at_of = [&](int j) { return (j < front ? j : low + j - front) * BLOCK; };
 
-    // a block's loads: lane l % BLOCK looks up place l, keys go to where the product wants them, values row by row
-    constexpr int ROW_GROUPS = D / GROUP, LOADS = BLOCK * ROW_GROUPS / 64;
-    static_assert(BLOCK * ROW_GROUPS % 64 == 0);
-    Pack<C, GROUP> keys[KEYS][STEPS], held[LOADS];
-    int64_t key_row = 0, value_row = 0;      // of the lane's place
+    // A block's loads: lane l % BLOCK looks up place l, a block ahead; keys go to where the product wants them, values row by row.  What has no page
+    // is read from one that exists, and hidden.
+    int entry = -1;                          // of the table
+    auto look_up = [&](int j) {
+        const int page = A.quotient(at_of(j) + lane % BLOCK);
+        entry = page < A.cache.table_pages ? A.cache.table[p.b * A.cache.table_stride + page] : -1;
+    };
+    Row keys[KEYS][KEY_LOADS], held[VALUE_LOADS];
     float key_scale = 1.0f, value_scale = 1.0f;
-    bool exists = false;                     // ... and is seen by some query
-    auto load = [&](int j) {
-        const int place = at_of(j) + lane % BLOCK;
-        const int64_t page = A.cache.page_of(p.b, place / A.cache.page_tokens), slot = place % A.cache.page_tokens;
-        // (places that no query sees are not read)
-        exists = page >= 0 && place < high * BLOCK && place < p.n;
-        const int64_t at = exists ? page : 0;
-        key_row = at * A.cache.keys.page + p.shared * A.cache.keys.head + (exists ? slot : 0) * A.cache.keys.slot;
-        value_row = at * A.cache.values.page + p.shared * A.cache.values.head + (exists ? slot : 0) * A.cache.values.slot;
+    uint64_t existing = 0;
+    int64_t key_row = 0, value_row = 0;      // of the lane's place
+    auto find = [&](int j) {
+        const int place = at_of(j) + lane % BLOCK, slot = place - A.quotient(place) * A.cache.page_tokens;
+        const bool exists = entry >= 0 && entry < A.cache.pages && place < p.n;
+        const int64_t page = exists ? entry : 0, in_page = exists ? slot : 0;
+        existing = __ballot(exists);
+        key_row = page * A.cache.keys.page + p.shared * A.cache.keys.head + in_page * A.cache.keys.slot;
+        value_row = page * A.cache.values.page + p.shared * A.cache.values.head + in_page * A.cache.values.slot;
         if constexpr (NARROW) {
-            key_scale = exists ? A.cache.keys.scales[at * A.cache.heads + p.shared] : 0.0f;
-            value_scale = exists ? A.cache.values.scales[at * A.cache.heads + p.shared] : 0.0f;
+            key_scale = A.cache.keys.scales[page * A.cache.heads + p.shared];
+            value_scale = A.cache.values.scales[page * A.cache.heads + p.shared];
         }
+    };
+    auto load_keys = [&] {
 #pragma unroll
         for (int t = 0; t < KEYS; ++t) {
-            const int source = t * M + column;
-            const bool ok = __shfl((int)exists, source);
-            const C *row = (const C *)A.cache.keys.values + __shfl(key_row, source);
+            const C *row = (const C *)A.cache.keys.values + __shfl(key_row, t * M + column);
 #pragma unroll
-            for (int step = 0; step < STEPS; ++step) {
-                keys[t][step] = Pack<C, GROUP>{};
-                if (ok) keys[t][step] = row_values<C, GROUP>(row, step * X::STEP + X::first_of(lane), K);
-            }
+            for (int i = 0; i < KEY_LOADS; ++i) keys[t][i] = row_load<C, WHOLE>(row, i * 4 * LOAD + lane / 16 * LOAD, K);
         }
+    };
+    auto load_values = [&] {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int number = lane + i * 64, source = number / ROW_GROUPS;
-            const bool ok = __shfl((int)exists, source);
-            const C *row = (const C *)A.cache.values.values + __shfl(value_row, source);
-            held[i] = Pack<C, GROUP>{};
-            if (ok) held[i] = row_values<C, GROUP>(row, number % ROW_GROUPS * GROUP, V);
+        for (int i = 0; i < VALUE_LOADS; ++i) {
+            const C *row = (const C *)A.cache.values.values + __shfl(value_row, (lane + i * 64) / ROW_LOADS);
+            held[i] = row_load<C, WHOLE>(row, (lane + i * 64) % ROW_LOADS * LOAD, V);
         }
     };
 
@@ -185,116 +239,189 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     float m = -INFINITY, sum = 0.0f;
     bool any = false;
     int j = first_block + wave;
-    if (j < last_block) load(j);
-    for (; j < last_block; j += kCacheWaves) {
+    if (j < last_block) {
+        look_up(j);
+        find(j);
+        load_keys();
+        load_values();
+        if (j + kCacheWaves < last_block) look_up(j + kCacheWaves);
+    }
+    // Something that is not finite and not seen by all queries: such blocks are left out, and taken by themselves afterwards (CAREFUL; a branch in
+    // the middle would cost every block its registers)
+    bool left_out = false;
+    auto take = [&](int j, auto careful, bool more) {
+        constexpr bool CAREFUL = decltype(careful)::value;
         const int at = at_of(j);
         typename X::Result s[KEYS] = {};
 #pragma unroll
-        for (int step = 0; step < STEPS; ++step)
+        for (int i = 0; i < KEY_LOADS; ++i)
 #pragma unroll
             for (int t = 0; t < KEYS; ++t) {
-                typename X::Frag k;
+                const Row got = row_values<C, WHOLE>(keys[t][i], i * 4 * LOAD + lane / 16 * LOAD, K);
+                const typename X::Frag k = operand<X, C, 0>(got);
 #pragma unroll
-                for (int e = 0; e < GROUP; ++e) k[e] = widened<E>(keys[t][step].v[e]);
-                s[t] = X::multiply(k, q[step], s[t]);
+                for (int part = 0; part < QUERY_PARTS; ++part) s[t] = X::multiply(k, q[part][i * OPERANDS], s[t]);
+                if constexpr (OPERANDS == 2) {
+                    const typename X::Frag more = operand<X, C, GROUP>(got);
+#pragma unroll
+                    for (int part = 0; part < QUERY_PARTS; ++part) s[t] = X::multiply(more, q[part][i * OPERANDS + 1], s[t]);
+                }
             }
+        // (the next block's loads go out as soon as there is room for them, so that some are always on their way)
+        const uint64_t existed = existing;
+        const float key_scales = key_scale, value_scales = value_scale;
+        if (more) {
+            find(j + kCacheWaves);
+            load_keys();
+        }
+        // whether every query sees every place of the block
+        constexpr uint64_t ALL = ~(uint64_t)0 >> (64 - BLOCK);
+        const uint64_t exist = existed & ALL;
+        const bool all = exist == ALL && at + BLOCK - 1 <= lowest && (highest - at < window || at + BLOCK <= sinks);
         bool spoilt = false;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int number = lane + i * 64, source = number / ROW_GROUPS;
-            const float scale = NARROW ? __shfl(value_scale, source) : 1.0f;
-            struct { E v[GROUP]; } row;
+        for (int i = 0; i < VALUE_LOADS; ++i) {
+            const int source = (lane + i * 64) / ROW_LOADS;
+            E *to = values + source * Tile::PITCH + (lane + i * 64) % ROW_LOADS * LOAD;
+            const Row got = row_values<C, WHOLE>(held[i], (lane + i * 64) % ROW_LOADS * LOAD, V);
+            *(typename X::Frag *)to = operand<X, C, 0>(got);
+            if constexpr (OPERANDS == 2) *(typename X::Frag *)(to + GROUP) = operand<X, C, GROUP>(got);
+            if (!all) {
 #pragma unroll
-            for (int e = 0; e < GROUP; ++e) {
-                row.v[e] = widened<E>(held[i].v[e]);
-                if constexpr (NARROW) row.v[e] = (E)((float)row.v[e] * scale);
-                spoilt = spoilt || !__builtin_isfinite((float)row.v[e]);
+                for (int e = 0; e < 4; ++e) {
+                    // (8 bits: NaN is all ones but for the sign)
+                    if constexpr (NARROW) spoilt |= (((got[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                    else spoilt |= word_spoilt<C>(got[e]);
+                }
             }
-            *(f4 *)(values + source * Tile::PITCH + number % ROW_GROUPS * GROUP) = __builtin_bit_cast(f4, row);
         }
-        spoilt = __any(spoilt);
-        const bool existed = exists;
-        const float key_scales = key_scale;
         // (the wavefront's own stores before its own reads: the order that LDS keeps)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (j + kCacheWaves < last_block) load(j + kCacheWaves);
+        if (more) {
+            load_values();
+            if (j + 2 * kCacheWaves < last_block) look_up(j + 2 * kCacheWaves);
+        }
+        const bool not_finite = !all && __any(spoilt);
+        if (not_finite != CAREFUL) {
+            left_out = true;
+            return;
+        }
+        if constexpr (NARROW) {
+#pragma unroll
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) s[t][i] *= __shfl(key_scales, t * M + X::row_of(lane, i));
+        }
+        if (!all) {
+#pragma unroll
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) {
+                    const int row = t * M + X::row_of(lane, i);
+                    const bool ok = (exist >> row & 1) & seen(at + row);
+                    any |= ok;
+                    s[t][i] = ok ? s[t][i] : -INFINITY;
+                }
+        }
+        __builtin_amdgcn_sched_barrier(0);
         float most = -INFINITY;
-        bool hidden = false;
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
-            for (int i = 0; i < X::REGS; ++i) {
-                const int row = t * M + X::row_of(lane, i);
-                if constexpr (NARROW) s[t][i] *= __shfl(key_scales, row);
-                const bool exists_there = __shfl((int)existed, row), ok = exists_there && seen(at + row);
-                any = any || ok;
-                hidden = hidden || !ok;
-                s[t][i] = ok ? s[t][i] : -INFINITY;
-                most = fmaxf(most, s[t][i]);
-            }
+            for (int i = 0; i < X::REGS; ++i) most = fmaxf(most, s[t][i]);
+        any |= all & there;
         most = over_column<M>(most, fmaxf);
         const float next = fmaxf(m, most * A.power), base = next == -INFINITY ? 0.0f : next;
         const float shrink = __builtin_amdgcn_exp2f(m - base);
         m = next;
-        float part = 0.0f;
+        float total = 0.0f;
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) {
                 s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -base));
-                part += s[t][i];
+                total += s[t][i];
+                // (the values' scale goes into the probabilities: one number for a place instead of one for each of its values)
+                if constexpr (NARROW) {
+                    const float scale = __shfl(value_scales, t * M + X::row_of(lane, i));
+                    s[t][i] = s[t][i] == 0.0f ? 0.0f : s[t][i] * scale;      // (the scale of what is hidden may be anything)
+                }
             }
-        sum = fmaf(sum, shrink, part);
+        sum = fmaf(sum, shrink, total);
 #pragma unroll
         for (int t = 0; t < OUT; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
-        typename X::Frag probabilities[PARTS];
+        typename X::Frag probabilities[PARTS][PRODUCTS];
 #pragma unroll
-        for (int part_of = 0; part_of < PARTS; ++part_of) {
-            probabilities[part_of] = X::of_results(s, 0);
-            if (part_of + 1 < PARTS)
+        for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                for (int t = 0; t < KEYS; ++t)
+            for (int step = 0; step < PRODUCTS; ++step) {
+                constexpr int TILES = X::STEP / M;
+                probabilities[part][step] = X::of_results(s, step);
+                if (part + 1 < PARTS)
 #pragma unroll
-                    for (int i = 0; i < X::REGS; ++i) s[t][i] -= (float)probabilities[part_of][t * X::REGS + i];
-        }
-        if (spoilt && __any(hidden)) {
-            // what is not finite counts for the queries that see it (see sig_window.h)
-            typename X::Frag sees;
+                    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int e = 0; e < GROUP; ++e) {
-                const bool exists_there = __shfl((int)existed, X::place_of(lane, e));
-                sees[e] = (E)(exists_there && seen(at + X::place_of(lane, e)) ? 1.0f : 0.0f);
+                        for (int i = 0; i < X::REGS; ++i) s[step * TILES + t][i] -= (float)probabilities[part][step][t * X::REGS + i];
             }
-#pragma unroll
-            for (int t = 0; t < OUT; ++t) {
-                const typename X::Frag v = X::template columns<Tile>(lane, values, 0, t * M);
-#pragma unroll
-                for (int part_of = 0; part_of < PARTS; ++part_of) acc[t] = X::multiply(only_finite<X>(v), probabilities[part_of], acc[t]);
+        if constexpr (CAREFUL) {
+            // query by query, with zeros for what that one does not see
 #pragma unroll 1
-                for (int kind = 0; kind < 3; ++kind) {
-                    const typename X::Result counts = X::multiply(only_kind<X>(v, kind), sees, typename X::Result{});
-                    const float what = kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY;
+            for (int c = 0; c < M; ++c) {
+                const int its_own = __shfl(own, c);
 #pragma unroll
-                    for (int i = 0; i < X::REGS; ++i) acc[t][i] += counts[i] > 0.0f ? what : 0.0f;
+                for (int step = 0; step < PRODUCTS; ++step) {
+                    unsigned sees = 0;
+#pragma unroll
+                    for (int e = 0; e < GROUP; ++e) {
+                        const int row = step * X::STEP + X::place_of(lane, e), place = at + row;
+                        sees |= ((unsigned)(exist >> row) & (unsigned)((place <= its_own) & ((its_own - place < window) | (place < sinks)))) << e;
+                    }
+#pragma unroll
+                    for (int t = 0; t < OUT; ++t) {
+                        typename X::Frag v = X::template columns<Tile>(lane, values, step * X::STEP, t * M);
+#pragma unroll
+                        for (int e = 0; e < GROUP; ++e) v[e] = sees >> e & 1 ? v[e] : (E)0.0f;
+                        typename X::Result r = {};
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) r = X::multiply(v, probabilities[part][step], r);
+#pragma unroll
+                        for (int i = 0; i < X::REGS; ++i) acc[t][i] += column == c ? r[i] : 0.0f;
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < OUT; ++t) {
-                const typename X::Frag v = X::template columns<Tile>(lane, values, 0, t * M);
+            for (int step = 0; step < PRODUCTS; ++step)
 #pragma unroll
-                for (int part_of = 0; part_of < PARTS; ++part_of) acc[t] = X::multiply(v, probabilities[part_of], acc[t]);
-            }
+                for (int t = 0; t < OUT; ++t) {
+                    const typename X::Frag v = X::template columns<Tile>(lane, values, step * X::STEP, t * M);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) acc[t] = X::multiply(v, probabilities[part][step], acc[t]);
+                    if (t % 2) __builtin_amdgcn_sched_barrier(0);
+                }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    for (; j < last_block; j += kCacheWaves) take(j, std::false_type(), j + kCacheWaves < last_block);
+    if (left_out) {
+#pragma unroll 1
+        for (j = first_block + wave; j < last_block; j += kCacheWaves) {
+            look_up(j);
+            find(j);
+            load_keys();
+            load_values();
+            take(j, std::true_type(), false);
+        }
     }
 
     // the four wavefronts' sums.  One that has seen only scores of minus infinity has a sum of 1 with a maximum of minus infinity, one that has seen
     // nothing 0
     sum = over_column<M>(sum, [](float a, float b) { return a + b; });
     any = over_column<M>(any ? 1.0f : 0.0f, fmaxf) > 0.0f;
+    if (!there) m = -INFINITY, sum = 0.0f;
     if (m == -INFINITY && sum == sum) sum = any ? 1.0f : 0.0f;
     float *own_sums = (float *)room[wave];
 #pragma unroll
@@ -331,33 +458,67 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     }
 }
 
-// Joins the parts of cut sequences: 16 queries a workgroup
-template <typename T>
-__global__ __launch_bounds__(kCacheThreads) void sig_cache_join_kernel(CacheAttentionArgs A)
+// Joins the parts of cut sequences.  `columns` x `turns` threads (powers of two) take a query, or one of its `slices` of columns: N columns and every
+// `turns`-th part each.
+template <typename T, int N>
+__global__ __launch_bounds__(kCacheThreads) void sig_cache_join_kernel(CacheAttentionArgs A, int columns, int turns, int slices)
 {
-    QueryPlace p;
-    const int64_t line = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    if (!query_place(A, line * A.splits, p)) return;
-    const int V = A.cache.V;
-    T *out = (T *)A.out;
-    for (int i = threadIdx.x; i < kQueries * V; i += kCacheThreads) {
-        const int query = i / V, c = i % V;
-        const int64_t number = (int64_t)p.tile * kQueries + query;
-        if (number >= A.T * A.group) continue;
-        const float *parts = A.parts + (line * A.splits * kQueries + query) * (V + 2);
-        const int64_t apart = (int64_t)kQueries * (V + 2);
-        float top = -INFINITY, total = 0.0f, value = 0.0f;
-        bool any = false;
-        for (int s = 0; s < A.splits; ++s) top = fmaxf(top, parts[s * apart + V]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        for (int s = 0; s < A.splits; ++s) {
-            const float sum = parts[s * apart + V + 1], share = __builtin_amdgcn_exp2f(parts[s * apart + V] - base);
-            any = any || sum != 0.0f;
-            total = fmaf(sum, share, total);
-            if (sum != 0.0f) value = fmaf(parts[s * apart + c], share, value);
+    __shared__ float shares[kMostSplits], numbers[kCacheThreads];
+    __shared__ Pack<float, N> joined[kCacheThreads];
+    const int team = columns * turns, of_team = threadIdx.x % team, first = threadIdx.x - of_team, V = A.cache.V, apart = kQueries * (V + 2);
+    const int64_t queries = A.T * A.group, all = A.B * A.cache.heads * queries;
+    const int64_t piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kCacheThreads / team) + threadIdx.x / team, id = piece / slices;
+    const bool there = id < all;
+    const int64_t number = there ? id % queries : 0, head = there ? id / queries : 0;
+    const float *parts = A.parts + ((head * A.tiles + number / kQueries) * A.splits * kQueries + number % kQueries) * (V + 2);
+    float *own_shares = shares + threadIdx.x / team * A.splits;
+    // f over what the team's threads hold
+    auto over_team = [&](float x, auto f) {
+        numbers[threadIdx.x] = x;
+        for (int i = team / 2; i > 0; i /= 2) {
+            __syncthreads();
+            if (of_team < i) numbers[threadIdx.x] = f(numbers[threadIdx.x], numbers[threadIdx.x + i]);
         }
-        out[((p.b * A.T + number / A.group) * A.heads + p.shared * A.group + number % A.group) * V + c] = from_float<T>(any ? value / total : 0.0f);
+        __syncthreads();
+        x = numbers[first];
+        __syncthreads();
+        return x;
+    };
+    float top = -INFINITY, total = 0.0f, any = 0.0f;
+    for (int s = of_team; s < A.splits; s += team) top = fmaxf(top, parts[(int64_t)s * apart + V]);
+    top = over_team(top, fmaxf);
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int s = of_team; s < A.splits; s += team) {
+        const float sum = parts[(int64_t)s * apart + V + 1], share = __builtin_amdgcn_exp2f(parts[(int64_t)s * apart + V] - base);
+        if (sum != 0.0f) any = 1.0f;
+        total = fmaf(sum, share, total);
+        own_shares[s] = sum != 0.0f ? share : -1.0f;      // (a part that has seen nothing is left out)
     }
+    total = over_team(total, [](float a, float b) { return a + b; });
+    any = over_team(any, fmaxf);
+    const int turn = of_team / columns;
+    const int c = ((int)(piece % slices) * columns + of_team % columns) * N;      // (V <= slices columns N)
+    float value[N] = {};
+    if (c < V) {
+#pragma unroll 8
+        for (int s = turn; s < A.splits; s += turns) {
+            const Pack<float, N> part = load_pack<float, N>(parts + (int64_t)s * apart + c);
+            const float share = own_shares[s];
+#pragma unroll
+            for (int j = 0; j < N; ++j) value[j] = share < 0.0f ? value[j] : fmaf(part.v[j], share, value[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) joined[threadIdx.x].v[j] = value[j];
+    __syncthreads();
+    if (turn > 0 || !there || c >= V) return;
+    for (int i = 1; i < turns; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) value[j] += joined[threadIdx.x + i * columns].v[j];
+    Pack<T, N> result;
+#pragma unroll
+    for (int j = 0; j < N; ++j) result.v[j] = from_float<T>(any != 0.0f ? value[j] / total : 0.0f);
+    store_pack((T *)A.out + ((head / A.cache.heads * A.T + number / A.group) * A.heads + head % A.cache.heads * A.group + number % A.group) * V + c, result);
 }
 
 hipError_t launch_cache_attention_f32(const CacheAttentionArgs &A, bool narrow, hipStream_t st);
@@ -377,8 +538,14 @@ hipError_t launch_cache_attention(const CacheAttentionArgs &A, bool narrow, hipS
     const dim3 grid = cache_grid(lines * A.splits);
     auto go = [&](auto d) {
         constexpr int D = decltype(d)::value;
-        if (narrow) sig_cache_attention_kernel<T, Narrow, SmallTiles<T>, D><<<grid, kCacheThreads, 0, st>>>(A);
-        else sig_cache_attention_kernel<T, T, SmallTiles<T>, D><<<grid, kCacheThreads, 0, st>>>(A);
+        auto launch = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value, WIDE = sizeof(T) == 4;
+            // values of 8 bits are bfloat16's, and a query is one, two or three of them
+            if (narrow) sig_cache_attention_kernel<T, Narrow, SmallTiles<bf16>, D, WIDE ? 3 : std::is_same_v<T, f16> ? 2 : 1, WIDE ? 3 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
+            else sig_cache_attention_kernel<T, T, SmallTiles<T>, D, 1, WIDE ? 1 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
+        };
+        if (A.cache.K == D && A.cache.V == D) launch(std::true_type());
+        else launch(std::false_type());
     };
     const int dim = A.cache.K > A.cache.V ? A.cache.K : A.cache.V;
     if (dim <= 64) go(std::integral_constant<int, 64>());
@@ -386,7 +553,19 @@ hipError_t launch_cache_attention(const CacheAttentionArgs &A, bool narrow, hipS
     else go(std::integral_constant<int, 256>());
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !A.parts) return e;
-    sig_cache_join_kernel<T><<<cache_grid(lines), kCacheThreads, 0, st>>>(A);
+    const int64_t queries = A.B * A.cache.heads * A.T * A.group;
+    auto join = [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        int columns = 1, turns = 1, slices = 1;
+        while (columns * N < A.cache.V) columns *= 2;
+        // (many parts of few queries: eight columns a workgroup, 256 parts of 16 queries 20 -> us)
+        for (; A.splits >= 64 && columns > 8; columns /= 2) slices *= 2;
+        while (turns < A.splits && columns * turns < kCacheThreads) turns *= 2;
+        const int at_once = kCacheThreads / (columns * turns);
+        sig_cache_join_kernel<T, N><<<cache_grid((queries * slices + at_once - 1) / at_once), kCacheThreads, 0, st>>>(A, columns, turns, slices);
+    };
+    if (A.cache.V % 4 == 0) join(std::integral_constant<int, 4>());
+    else join(std::integral_constant<int, 1>());
     return hipGetLastError();
 }
 

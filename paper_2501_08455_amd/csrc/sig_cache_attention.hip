@@ -51,6 +51,8 @@ extern "C" int sig_cache_attention(sig_ctx *ctx, const sig_cache_t *cache, const
     A.splits = 1;
     if (lines < 2 * ctx->num_cu) A.splits = (int)least((2 * ctx->num_cu + lines - 1) / lines, (most + 32 * kLeastBlocks - 1) / (32 * kLeastBlocks));
     if (A.splits < 1) A.splits = 1;
+    if (A.splits > kMostSplits) A.splits = kMostSplits;
+    A.quotient = Quotient(cache->page_tokens);
     const hipStream_t st = (hipStream_t)hip_stream;
     Scratch scratch;
     if (A.splits > 1) {

@@ -201,8 +201,7 @@ template <typename T, typename E, int D, int ROWS, int THREADS>
 struct TileMover {
     static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = ROWS * GROUPS / THREADS;
     static_assert(ROWS * GROUPS % THREADS == 0);
-    using Group = struct { E v[GROUP]; };
-    Pack<T, GROUP> held[COUNT];
+    Words<T, GROUP> held[COUNT];
 
     static __device__ int row_of(int i) { return (threadIdx.x + i * THREADS) / GROUPS; }
     static __device__ int place_of(int i) { return (threadIdx.x + i * THREADS) % GROUPS * GROUP; }
@@ -214,7 +213,7 @@ struct TileMover {
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const int place = place_of(i);
-                held[i] = load_pack<T, GROUP>(first + min(row_of(i), n - 1) * stride + (place + GROUP <= dim ? place : 0));
+                held[i] = load_words<T, GROUP>(first + min(row_of(i), n - 1) * stride + (place + GROUP <= dim ? place : 0));
             }
         }
         if (dim % GROUP) {
@@ -223,11 +222,13 @@ struct TileMover {
                 const int place = place_of(i);
                 if (place < dim && place + GROUP > dim) {
                     const T *p = first + min(row_of(i), n - 1) * stride;
+                    struct { T v[GROUP]; } rest;
 #pragma unroll
                     for (int j = 0; j < GROUP; ++j) {
-                        held[i].v[j] = (T)0.0f;
-                        if (place + j < dim) held[i].v[j] = p[place + j];
+                        rest.v[j] = (T)0.0f;
+                        if (place + j < dim) rest.v[j] = p[place + j];
                     }
+                    held[i] = __builtin_bit_cast(Words<T, GROUP>, rest);
                 }
             }
         }
@@ -237,19 +238,27 @@ struct TileMover {
     {
         bool any = false;
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i)
+        for (int i = 0; i < COUNT; ++i) {
+            bool bad = false;
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) any = any || (!__builtin_isfinite((float)held[i].v[j]) && row_of(i) < n && place_of(i) < dim);
+            for (int j = 0; j < (int)sizeof(held[i]) / 4; ++j) bad |= word_spoilt<T>(held[i][j]);
+            const bool there = row_of(i) < n, within = place_of(i) < dim;
+            any |= bad & there & within;
+        }
         return any;
     }
     __device__ void store(E *tile, int dim, int n) const
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            Group values;
+            f4 bits;
+            if constexpr (sizeof(T) == sizeof(E)) {
+                bits = __builtin_bit_cast(f4, held[i]);
+            } else {
+                const auto values = __builtin_bit_cast(__attribute__((ext_vector_type(GROUP))) T, held[i]);
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) values.v[j] = (E)held[i].v[j];
-            const f4 bits = __builtin_bit_cast(f4, values);
+                for (int j = 0; j < GROUP; ++j) bits[j] = (float)values[j];
+            }
             *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = row_of(i) < n && place_of(i) < dim ? bits : f4{};
         }
     }

@@ -57,6 +57,25 @@ __device__ inline Pack<T, N> load_pack(const T *from)
     else return __builtin_bit_cast(Pack<T, N>, ((const PackWords<T, N> *)from)->words);
 }
 
+// N values as the words that hold them (values of a struct of their own would take a register each while they wait), and back
+template <typename T, int N>
+using Words = __attribute__((ext_vector_type(N * sizeof(T) / 4))) unsigned;
+
+template <typename T, int N>
+__device__ inline Words<T, N> load_words(const T *from)
+{
+    return ((const PackWords<T, N> *)from)->words;
+}
+
+// whether one of the values in `word` is not finite
+template <typename T>
+__device__ inline bool word_spoilt(unsigned word)
+{
+    if constexpr (sizeof(T) == 4) return (word & 0x7f800000u) == 0x7f800000u;
+    constexpr unsigned exponent = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
+    return ((word & exponent) == exponent) | ((word & exponent << 16) == exponent << 16);
+}
+
 template <typename T, int N>
 __device__ inline void store_pack(T *to, const Pack<T, N> &values)
 {

@@ -89,7 +89,8 @@ struct KeyTiles {
 
 struct Seen {
     int window, sinks;
-    __device__ bool operator()(int query, int key) const { return key <= query && (query - key < window || key < sinks); }
+    // (all of it compared: branches for single pairs cost more than the comparisons)
+    __device__ bool operator()(int query, int key) const { return (key <= query) & ((query - key < window) | (key < sinks)); }
     // of queries q0 ... q1 and keys k0 ... k1
     __device__ bool all(int q0, int q1, int k0, int k1) const { return k1 <= q0 && (q1 - k0 < window || k1 < sinks); }
     __device__ bool none(int q0, int q1, int k0, int k1) const { return k0 > q1 || (k1 <= q0 - window && k0 >= sinks); }
@@ -180,7 +181,8 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) {
-                if (!whole && !seen(line, at + t * M + X::row_of(lane, i))) s[t][i] = -INFINITY;
+                const bool ok = whole | seen(line, at + t * M + X::row_of(lane, i));
+                s[t][i] = ok ? s[t][i] : -INFINITY;
                 most = fmaxf(most, s[t][i]);
             }
         most = over_column<M>(most, fmaxf);
@@ -290,7 +292,8 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 128 ? 
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) {
                 const float probability = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -stats.x)) * stats.y;
-                u[t][i] = whole || seen(line, at + t * M + X::row_of(lane, i)) ? probability * (u[t][i] - delta) : 0.0f;
+                const bool ok = whole | seen(line, at + t * M + X::row_of(lane, i));
+                u[t][i] = ok ? probability * (u[t][i] - delta) : 0.0f;
             }
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
@@ -379,7 +382,7 @@ __global__ __launch_bounds__(kWindowThreads, 1) void sig_window_key_gradient_ker
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) {
                 const int row = t * M + X::row_of(lane, i);
-                const bool ok = whole || (at + row < p.n && seen(at + row, line));
+                const bool ok = whole | ((at + row < p.n) & seen(at + row, line));
                 s[t][i] = ok ? __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -most[row])) * inverse[row] : 0.0f;
                 u[t][i] = ok ? s[t][i] * (u[t][i] - delta[row]) : 0.0f;
             }
