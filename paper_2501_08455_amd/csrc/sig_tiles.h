@@ -172,32 +172,39 @@ struct LdsTile {
     static constexpr int PITCH = D + (sizeof(E) == 4 ? 4 : BANK_GROUPS == 0 || BANK_GROUPS == 4 ? 24 : 8);
 };
 
-// The wavefront's own operand, one line a lane: fragments to match the rows form, zeros where `there` is false
-template <typename X, int STEPS, typename T>
-__device__ inline void fragments_of(typename X::Frag *f, int lane, const T *line, int dim, bool there, bool negated)
+// The wavefront's own operand, one line a lane: a fragment to match step number j of the rows form, zeros where `there` is false
+template <typename X, typename T>
+__device__ inline void fragment_of(typename X::Frag *f, int lane, int j, const T *line, int dim, bool there)
 {
     using E = typename X::E;
     constexpr int N = X::GROUP;
+    const int at = j * X::STEP + X::first_of(lane);
+    *f = typename X::Frag{};
+    if (there && at + N <= dim) {
+        const auto got = __builtin_bit_cast(__attribute__((ext_vector_type(N))) T, load_words<T, N>(line + at));
+#pragma unroll
+        for (int e = 0; e < N; ++e) (*f)[e] = (E)got[e];
+    } else if (there) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (at + e < dim) (*f)[e] = (E)line[at + e];
+    }
+}
+
+template <typename X, int STEPS, typename T>
+__device__ inline void fragments_of(typename X::Frag *f, int lane, const T *line, int dim, bool there, bool negated)
+{
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-        const int at = j * X::STEP + X::first_of(lane);
-        f[j] = typename X::Frag{};
-        if (there && at + N <= dim) {
-            const Pack<T, N> got = load_pack<T, N>(line + at);
-#pragma unroll
-            for (int e = 0; e < N; ++e) f[j][e] = (E)got.v[e];
-        } else if (there) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (at + e < dim) f[j][e] = (E)line[at + e];
-        }
+        fragment_of<X>(f + j, lane, j, line, dim, there);
         if (negated) f[j] = -f[j];
     }
 }
 
 // ROWS x D values, global memory -> registers -> LDS, by THREADS threads: zeros beyond the rows and values that are there.  Loads of whole groups are
 // unconditional (what is not there is read from a place that is, and dropped on the way to LDS), so that all are in flight at once.
-template <typename T, typename E, int D, int ROWS, int THREADS>
+// WHOLE: rows have D values.
+template <typename T, typename E, int D, int ROWS, int THREADS, bool WHOLE>
 struct TileMover {
     static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = ROWS * GROUPS / THREADS;
     static_assert(ROWS * GROUPS % THREADS == 0);
@@ -209,14 +216,14 @@ struct TileMover {
     // rows 0 ... n - 1 are there, n >= 1
     __device__ void load(const T *first, int64_t stride, int dim, int n)
     {
-        if (dim >= GROUP) {
+        if (WHOLE || dim >= GROUP) {
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const int place = place_of(i);
-                held[i] = load_words<T, GROUP>(first + min(row_of(i), n - 1) * stride + (place + GROUP <= dim ? place : 0));
+                held[i] = load_words<T, GROUP>(first + min(row_of(i), n - 1) * stride + (WHOLE || place + GROUP <= dim ? place : 0));
             }
         }
-        if (dim % GROUP) {
+        if (!WHOLE && dim % GROUP) {
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const int place = place_of(i);
@@ -242,7 +249,7 @@ struct TileMover {
             bool bad = false;
 #pragma unroll
             for (int j = 0; j < (int)sizeof(held[i]) / 4; ++j) bad |= word_spoilt<T>(held[i][j]);
-            const bool there = row_of(i) < n, within = place_of(i) < dim;
+            const bool there = row_of(i) < n, within = WHOLE || place_of(i) < dim;
             any |= bad & there & within;
         }
         return any;
@@ -259,7 +266,8 @@ struct TileMover {
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) bits[j] = (float)values[j];
             }
-            *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = row_of(i) < n && place_of(i) < dim ? bits : f4{};
+            const bool there = row_of(i) < n, within = WHOLE || place_of(i) < dim, ok = there & within;
+            *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = ok ? bits : f4{};
         }
     }
 };

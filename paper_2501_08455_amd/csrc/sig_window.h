@@ -24,6 +24,13 @@
 
 namespace sig {
 
+#ifndef WINDOW_WIDE
+#define WINDOW_WIDE 128
+#define WINDOW_QUERY_WIDE 128
+#define WINDOW_QUERY_BYTES 128
+#define WINDOW_KEY_BYTES 64
+#endif
+
 constexpr int kWindowThreads = 256, kWindowWaves = kWindowThreads / 64;
 
 struct WindowArgs {
@@ -36,6 +43,8 @@ struct WindowArgs {
     const void *grad_out;                 // as `out`
     void *grad_q, *grad_k, *grad_v;       // as q, k, v, contiguous
     float *delta;                         // [B][heads][T]: D
+    float *parts;                         // [B][shared heads][front tiles][parts][rows of a tile][K + V], for the keys that everyone sees
+    int front, front_parts;               // those keys' tiles, and the parts that their queries are cut into
     int64_t B;
     int T, heads, group, K, V;
     int window, sinks;                    // at most T
@@ -50,7 +59,7 @@ struct WindowPlace {
     int head, tile, n;      // n: tokens of the sequence
 };
 
-// Workgroups that follow one another take the last tiles of all heads first, which have the most to do where everything is seen.
+// Workgroups that follow one another take the last tiles first, which have the most to do where everything is seen.
 // Eight dies take workgroups in turn, each with a cache of its own: where heads are a multiple of eight, a head's workgroups stay on one.
 __device__ inline bool window_place(const WindowArgs &A, int heads, WindowPlace &p)
 {
@@ -124,15 +133,50 @@ __device__ inline void zero_rows(T *first, int64_t stride, int dim, int from, in
     for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * dim; i += kWindowThreads) first[(from + i / dim) * stride + i % dim] = from_float<T>(0.0f);
 }
 
+// What float16 holds is small: probabilities are scaled up by a power of two, so that those of a long row's tokens are not rounded as subnormal numbers.
+// (A maximum that stays behind by 2^8 lets them grow to 2^15.)
+template <typename E>
+constexpr int kLift = std::is_same_v<E, f16> ? 7 : 0;
+constexpr float kBehind = 8.0f;
+
+// Gradient terms in float16 have no scale that suits all of them: each lane (a line of the result) has a power of two of its own, `factor`, which
+// keeps its largest term so far within 2^15 and above 2^-7 of that when it is chosen.  Returns what the sums so far are to be multiplied with.
+struct TermScale {
+    float factor = 0.0f;      // none yet
+
+    template <int M, int COUNT, typename Result>
+    __device__ bool grown(const Result *u, float *shrink)
+    {
+        float most = 0.0f;
+#pragma unroll
+        for (int t = 0; t < COUNT; ++t)
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(Result) / 4); ++i) most = fmaxf(most, fabsf(u[t][i]));
+        most = over_column<M>(most, fmaxf);
+        const bool change = (most > 0.0f) & (most < INFINITY) & ((factor == 0.0f) | (most * factor > 32768.0f));
+        *shrink = 1.0f;
+        if (!__any(change)) return false;
+        if (change) {
+            int exponent = (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127;
+            exponent = min(max(8 - exponent, -120), 120);
+            const float next = __builtin_bit_cast(float, (unsigned)(exponent + 127) << 23);
+            *shrink = factor == 0.0f ? 1.0f : next / factor;
+            factor = next;
+        }
+        return true;
+    }
+    __device__ float back() const { return factor == 0.0f ? 1.0f : 1.0f / factor; }
+};
+
 // ---------------------------------------------------------------- forward
-template <typename T, typename X, int D, int N>
+template <typename T, typename X, int D, int N, bool WHOLE>
 __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 2 : 1) void sig_window_forward_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M;
-    __shared__ __attribute__((aligned(16))) E keys[N * LdsTile<E, D>::PITCH];
-    __shared__ __attribute__((aligned(16))) E values[N * LdsTile<E, D>::PITCH];
-    __shared__ int spoilt[2];
+    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    __shared__ __attribute__((aligned(16))) E keys[2 * SIZE];
+    __shared__ __attribute__((aligned(16))) E values[2 * SIZE];
+    __shared__ int spoilt[2];      // 1 + the number of a tile that is partly hidden and holds something that is not finite
     WindowPlace p;
     if (!window_place(A, A.heads, p)) return;
     const int lane = threadIdx.x % 64, lo = p.tile * ROWS, end = min(lo + ROWS, A.T);
@@ -144,51 +188,55 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
     }
     const int hi = min(end, p.n), shared = p.head / A.group;
     const T *k = (const T *)A.k + p.b * A.ks[0] + shared * A.ks[2], *v = (const T *)A.v + p.b * A.vs[0] + shared * A.vs[2];
-    const int own = lo + threadIdx.x / 64 * M, line = own + lane % M;
+    const int own = lo + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * M, line = own + lane % M;
     const bool there = line < p.n;
     typename X::Frag q[STEPS];
     fragments_of<X, STEPS>(q, lane, (const T *)A.q + p.b * A.qs[0] + (there ? line : lo) * A.qs[1] + p.head * A.qs[2], A.K, there, A.negated);
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
-    TileMover<T, E, D, N, kWindowThreads> key_tile, value_tile;
+    TileMover<T, E, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
         value_tile.load(v + at * A.vs[1], A.vs[1], A.V, p.n - at);
     };
+    auto store = [&](int j) {
+        const int at = tiles.at(j);
+        key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
+        value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
+        if (!seen.all(lo, hi - 1, at, at + N - 1) && value_tile.spoilt(A.V, p.n - at)) spoilt[j & 1] = j + 1;
+    };
     typename X::Result acc[OUT] = {};
     float m = -INFINITY, sum = 0.0f;      // of the lane's own part of its line
-    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    load(0);
-    for (int j = 0; j < tiles.count; ++j) {
-        const int at = tiles.at(j);
-        __syncthreads();
-        key_tile.store(keys, A.K, p.n - at);
-        value_tile.store(values, A.V, p.n - at);
-        // (a tile that is partly hidden from some wavefront)
-        if (!seen.all(lo, hi - 1, at, at + N - 1) && value_tile.spoilt(A.V, p.n - at)) spoilt[j & 1] = 1;
-        if (threadIdx.x == 0) spoilt[~j & 1] = 0;
-        __syncthreads();
-        if (j + 1 < tiles.count) load(j + 1);
-        const bool whole = seen.all(own, own + M - 1, at, at + N - 1), careful = spoilt[j & 1];
-        const bool none = seen.none(own, min(own + M, hi) - 1, at, at + N - 1);
-        typename X::Frag probabilities[N / X::STEP];
-        if (!none) {
+    typename X::Frag probabilities[N / X::STEP];
+    // the probabilities of tile j, and the running maximum and sum
+    auto weigh = [&](int at, const E *keys) {
         typename X::Result s[KEYS] = {};
         product_of_rows<X, D, KEYS>(lane, keys, q, s);
+        if (!seen.all(own, own + M - 1, at, at + N - 1)) {
+#pragma unroll
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) s[t][i] = seen(line, at + t * M + X::row_of(lane, i)) ? s[t][i] : -INFINITY;
+        }
         float most = -INFINITY;
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
-            for (int i = 0; i < X::REGS; ++i) {
-                const bool ok = whole | seen(line, at + t * M + X::row_of(lane, i));
-                s[t][i] = ok ? s[t][i] : -INFINITY;
-                most = fmaxf(most, s[t][i]);
-            }
+            for (int i = 0; i < X::REGS; ++i) most = fmaxf(most, s[t][i]);
         most = over_column<M>(most, fmaxf);
-        const float next = fmaxf(m, most * A.power), base = next == -INFINITY ? 0.0f : next;      // (nothing seen so far: all p are 0)
-        const float shrink = __builtin_amdgcn_exp2f(m - base);
-        m = next;
+        // The maximum that everything is scaled with may stay behind by a factor of 2^8: what is added up so far then need not be touched
+        const float next = fmaxf(m, most * A.power);
+        if (__any(next > m + kBehind)) {
+            const float shrink = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next));
+            m = next;
+            sum *= shrink;
+#pragma unroll
+            for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
+        }
+        const float base = (m == -INFINITY ? 0.0f : m) - kLift<E>;      // (nothing seen so far: all p are 0)
         float part = 0.0f;
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
@@ -197,35 +245,63 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
                 s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -base));
                 part += s[t][i];
             }
-        sum = fmaf(sum, shrink, part);
-#pragma unroll
-        for (int t = 0; t < OUT; ++t)
-#pragma unroll
-            for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
+        sum += part;
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) probabilities[step] = X::of_results(s, step);
+    };
+    auto none = [&](int at) { return own >= hi || seen.none(own, min(own + M, hi) - 1, at, at + N - 1); };
+    // Tile j is in LDS, tile j + 1 on its way to registers: it goes to LDS's other half in the middle of tile j's work.  Spoilt tiles are left out, and
+    // taken by themselves afterwards (a branch in the middle would cost every tile its registers)
+    bool left_out = false;
+    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
+    load(0);
+    __syncthreads();
+    store(0);
+    if (tiles.count > 1) load(1);
+    for (int j = 0; j < tiles.count; ++j) {
+        const int at = tiles.at(j), half = (j & 1) * SIZE;
+        __syncthreads();
+        const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
+        left_out |= bad;
+        if (!skip) weigh(at, keys + half);
+        if (j + 1 < tiles.count) store(j + 1);
+        if (j + 2 < tiles.count) load(j + 2);
+        if (!skip) product_along_rows<X, D, N / X::STEP>(lane, values + half, probabilities, acc);
+    }
+    if (left_out) {
+#pragma unroll 1
+        for (int j = 0; j < tiles.count; ++j) {
+            const int at = tiles.at(j);
+            E *tile = values + (j & 1) * SIZE;
+            __syncthreads();
+            load(j);
+            store(j);
+            __syncthreads();
+            if (spoilt[j & 1] != j + 1) continue;
+            const bool skip = none(at);
+            if (!skip) weigh(at, keys + (j & 1) * SIZE);
+            leave_finite<E, D, N, kWindowThreads>(tile);
+            if (!skip) product_along_rows<X, D, N / X::STEP>(lane, tile, probabilities, acc);
+            add_not_finite<X, D, N, kWindowThreads, false>(lane, tile, v + at * A.vs[1], A.vs[1], A.V, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
-        if (careful) leave_finite<E, D, N, kWindowThreads>(values);
-        if (!none) product_along_rows<X, D, N / X::STEP>(lane, values, probabilities, acc);
-        if (careful) add_not_finite<X, D, N, kWindowThreads, false>(lane, values, v + at * A.vs[1], A.vs[1], A.V, p.n - at, none, acc, [&](int r) { return seen(line, at + r); });
     }
     sum = over_column<M>(sum, [](float a, float b) { return a + b; });
     const float r = 1.0f / sum;
     if (there) {
         store_line<X, D>(out + line * out_stride, A.V, lane, acc, r);
-        if (A.stats && lane < M) A.stats[(p.b * A.heads + p.head) * A.T + line] = make_float2(m == -INFINITY ? 0.0f : m, r);
+        if (A.stats && lane < M) A.stats[(p.b * A.heads + p.head) * A.T + line] = make_float2((m == -INFINITY ? 0.0f : m) - kLift<E>, r);
     }
     if (hi < end) zero_rows(out, out_stride, A.V, hi, end);
 }
 
 // ---------------------------------------------------------------- gradient of the queries, and D
-template <typename T, typename X, int D, int N>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 128 ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
+template <typename T, typename X, int D, int N, bool WHOLE>
+__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW_QUERY_BYTES ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M;
-    __shared__ __attribute__((aligned(16))) E keys[N * LdsTile<E, D>::PITCH];
-    __shared__ __attribute__((aligned(16))) E values[N * LdsTile<E, D>::PITCH];
+    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    __shared__ __attribute__((aligned(16))) E keys[2 * SIZE];
+    __shared__ __attribute__((aligned(16))) E values[2 * SIZE];
     __shared__ int spoilt[2];
     WindowPlace p;
     if (!window_place(A, A.heads, p)) return;
@@ -238,7 +314,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 128 ? 
     }
     const int hi = min(end, p.n), shared = p.head / A.group;
     const T *k = (const T *)A.k + p.b * A.ks[0] + shared * A.ks[2], *v = (const T *)A.v + p.b * A.vs[0] + shared * A.vs[2];
-    const int own = lo + threadIdx.x / 64 * M, line = own + lane % M;
+    const int own = lo + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * M, line = own + lane % M;
     const bool there = line < p.n;
     typename X::Frag q[STEPS], g[STEPS];
     fragments_of<X, STEPS>(q, lane, (const T *)A.q + p.b * A.qs[0] + (there ? line : lo) * A.qs[1] + p.head * A.qs[2], A.K, there, A.negated);
@@ -247,12 +323,13 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 128 ? 
     float delta = 0.0f;
     {
         // (the output as the forward pass rounded it)
-        typename X::Frag o[STEPS];
-        fragments_of<X, STEPS>(o, lane, (const T *)A.out + upstream, A.V, there, false);
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j)
+        for (int j = 0; j < STEPS; ++j) {
+            typename X::Frag o;
+            fragment_of<X>(&o, lane, j, (const T *)A.out + upstream, A.V, there);
 #pragma unroll
-            for (int e = 0; e < X::GROUP; ++e) delta = fmaf((float)o[j][e], (float)g[j][e], delta);
+            for (int e = 0; e < X::GROUP; ++e) delta = fmaf((float)o[e], (float)g[j][e], delta);
+        }
         delta = over_column<M>(delta, [](float a, float b) { return a + b; });
     }
     float2 stats = make_float2(0.0f, 0.0f);
@@ -262,158 +339,305 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 128 ? 
     }
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
-    TileMover<T, E, D, N, kWindowThreads> key_tile, value_tile;
+    TileMover<T, E, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
         value_tile.load(v + at * A.vs[1], A.vs[1], A.V, p.n - at);
     };
-    typename X::Result acc[OUT] = {};
-    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    load(0);
-    for (int j = 0; j < tiles.count; ++j) {
+    auto store = [&](int j) {
         const int at = tiles.at(j);
-        __syncthreads();
-        key_tile.store(keys, A.K, p.n - at);
-        value_tile.store(values, A.V, p.n - at);
-        if (!seen.all(lo, hi - 1, at, at + N - 1) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = 1;
-        if (threadIdx.x == 0) spoilt[~j & 1] = 0;
-        __syncthreads();
-        if (j + 1 < tiles.count) load(j + 1);
-        const bool whole = seen.all(own, own + M - 1, at, at + N - 1), careful = spoilt[j & 1];
-        const bool none = seen.none(own, min(own + M, hi) - 1, at, at + N - 1);
-        typename X::Frag terms[N / X::STEP];
-        if (!none) {
+        key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
+        value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
+        if (!seen.all(lo, hi - 1, at, at + N - 1) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = j + 1;
+    };
+    typename X::Result acc[OUT] = {};
+    TermScale scale;
+    typename X::Frag terms[N / X::STEP];
+    auto weigh = [&](int at, const E *keys, const E *values) {
         typename X::Result s[KEYS] = {}, u[KEYS] = {};
         product_of_rows<X, D, KEYS>(lane, keys, q, s);
         product_of_rows<X, D, KEYS>(lane, values, g, u);
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
-            for (int i = 0; i < X::REGS; ++i) {
-                const float probability = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -stats.x)) * stats.y;
-                const bool ok = whole | seen(line, at + t * M + X::row_of(lane, i));
-                u[t][i] = ok ? probability * (u[t][i] - delta) : 0.0f;
+            for (int i = 0; i < X::REGS; ++i) u[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -stats.x)) * stats.y * (u[t][i] - delta);
+        if (!seen.all(own, own + M - 1, at, at + N - 1)) {
+#pragma unroll
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) u[t][i] = seen(line, at + t * M + X::row_of(lane, i)) ? u[t][i] : 0.0f;
+        }
+        if constexpr (std::is_same_v<E, f16>) {
+            float shrink;
+            if (scale.grown<M, KEYS>(u, &shrink)) {
+#pragma unroll
+                for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                    for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
             }
 #pragma unroll
-        for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) u[t][i] *= scale.factor;
         }
-        if (careful) leave_finite<E, D, N, kWindowThreads>(keys);
-        if (!none) product_along_rows<X, D, N / X::STEP>(lane, keys, terms, acc);
-        if (careful) add_not_finite<X, D, N, kWindowThreads, true>(lane, keys, k + at * A.ks[1], A.ks[1], A.K, p.n - at, none, acc, [&](int r) { return seen(line, at + r); });
+#pragma unroll
+        for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
+    };
+    auto none = [&](int at) { return own >= hi || seen.none(own, min(own + M, hi) - 1, at, at + N - 1); };
+    bool left_out = false;
+    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
+    load(0);
+    __syncthreads();
+    store(0);
+    if (tiles.count > 1) load(1);
+    for (int j = 0; j < tiles.count; ++j) {
+        const int at = tiles.at(j), half = (j & 1) * SIZE;
+        __syncthreads();
+        const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
+        left_out |= bad;
+        if (!skip) weigh(at, keys + half, values + half);
+        if (j + 1 < tiles.count) store(j + 1);
+        if (j + 2 < tiles.count) load(j + 2);
+        if (!skip) product_along_rows<X, D, N / X::STEP>(lane, keys + half, terms, acc);
     }
-    if (there) store_line<X, D>(out + line * out_stride, A.K, lane, acc, A.scale);
+    if (left_out) {
+#pragma unroll 1
+        for (int j = 0; j < tiles.count; ++j) {
+            const int at = tiles.at(j);
+            E *tile = keys + (j & 1) * SIZE;
+            __syncthreads();
+            load(j);
+            store(j);
+            __syncthreads();
+            if (spoilt[j & 1] != j + 1) continue;
+            const bool skip = none(at);
+            if (!skip) weigh(at, tile, values + (j & 1) * SIZE);
+            leave_finite<E, D, N, kWindowThreads>(tile);
+            if (!skip) product_along_rows<X, D, N / X::STEP>(lane, tile, terms, acc);
+            add_not_finite<X, D, N, kWindowThreads, true>(lane, tile, k + at * A.ks[1], A.ks[1], A.K, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
+        }
+    }
+    if (there) store_line<X, D>(out + line * out_stride, A.K, lane, acc, A.scale * scale.back());
     if (hi < end) zero_rows(out, out_stride, A.K, hi, end);
 }
 
 // ---------------------------------------------------------------- gradient of keys and values
 // A wavefront's own lines are keys; queries and upstream gradients of all heads that share them come as tiles, one head after the other, so
-// that the sum over these heads is one of registers.
-template <typename T, typename X, int D, int N>
-__global__ __launch_bounds__(kWindowThreads, 1) void sig_window_key_gradient_kernel(WindowArgs A)
+// that the sum over these heads is one of registers.  The first tokens' tiles, which every query sees, are cut into parts along the queries, and joined
+// from scratch.
+template <typename T, typename X, int D, int N, bool WHOLE>
+__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW_KEY_BYTES ? 2 : 1) void sig_window_key_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M;
-    __shared__ __attribute__((aligned(16))) E queries[N * LdsTile<E, D>::PITCH];
-    __shared__ __attribute__((aligned(16))) E upstream[N * LdsTile<E, D>::PITCH];
-    __shared__ __attribute__((aligned(16))) float most[N], inverse[N], delta[N];
+    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    constexpr float LIFT = std::is_same_v<E, f16> ? 32768.0f : 1.0f;      // of the probabilities, which are at most 1 (see kLift)
+    __shared__ __attribute__((aligned(16))) E queries[2 * SIZE];
+    __shared__ __attribute__((aligned(16))) E upstream[2 * SIZE];
+    __shared__ __attribute__((aligned(16))) float most[2 * N], inverse[2 * N], delta[2 * N];
     __shared__ int spoilt[2];
-    WindowPlace p;
-    const int shared_heads = A.heads / A.group;
-    if (!window_place(A, shared_heads, p)) return;
-    const int lane = threadIdx.x % 64, lo = p.tile * ROWS, end = min(lo + ROWS, A.T);
-    T *out_k = (T *)A.grad_k + ((p.b * A.T) * shared_heads + p.head) * A.K, *out_v = (T *)A.grad_v + ((p.b * A.T) * shared_heads + p.head) * A.V;
+    // which head and keys: the front tiles' parts first, then the other tiles
+    const int shared_heads = A.heads / A.group, pieces = A.front * A.front_parts + A.tiles - A.front;
+    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, lines = A.B * shared_heads;
+    if (id >= lines * pieces) return;
+    const bool by_eight = lines % 8 == 0;      // (see window_place)
+    const int64_t head_line = by_eight ? id / 8 / pieces * 8 + id % 8 : id % lines;
+    const int piece = (int)(by_eight ? id / 8 % pieces : id / lines);
+    const int64_t b = head_line / shared_heads;
+    const int shared = (int)(head_line % shared_heads), front_pieces = A.front * A.front_parts;
+    const int tile = piece < front_pieces ? piece / A.front_parts : piece - front_pieces + A.front, parts = piece < front_pieces ? A.front_parts : 1;
+    const int64_t counted = A.lengths ? A.lengths[b] : A.T;
+    const int n = counted < 0 ? 0 : counted > A.T ? A.T : (int)counted;
+
+    const int lane = threadIdx.x % 64, lo = tile * ROWS, end = min(lo + ROWS, A.T);
+    T *out_k = (T *)A.grad_k + ((b * A.T) * shared_heads + shared) * A.K, *out_v = (T *)A.grad_v + ((b * A.T) * shared_heads + shared) * A.V;
     const int64_t k_stride = (int64_t)shared_heads * A.K, v_stride = (int64_t)shared_heads * A.V, g_stride = (int64_t)A.heads * A.V;
-    if (lo >= p.n) {
+    const bool zeros = parts == 1 || piece % A.front_parts == 0;      // whether this workgroup clears what stands behind the sequence
+    if (lo >= n) {
+        if (!zeros) return;
         zero_rows(out_k, k_stride, A.K, lo, end);
         zero_rows(out_v, v_stride, A.V, lo, end);
         return;
     }
-    const int hi = min(end, p.n);
-    const int own = lo + threadIdx.x / 64 * M, line = own + lane % M;
-    const bool there = line < p.n;
+    const int hi = min(end, n);
+    const int own = lo + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * M, line = own + lane % M;
+    const bool there = line < n;
     typename X::Frag k[STEPS], v[STEPS];
-    fragments_of<X, STEPS>(k, lane, (const T *)A.k + p.b * A.ks[0] + (there ? line : lo) * A.ks[1] + p.head * A.ks[2], A.K, there, A.negated);
-    fragments_of<X, STEPS>(v, lane, (const T *)A.v + p.b * A.vs[0] + (there ? line : lo) * A.vs[1] + p.head * A.vs[2], A.V, there, false);
+    fragments_of<X, STEPS>(k, lane, (const T *)A.k + b * A.ks[0] + (there ? line : lo) * A.ks[1] + shared * A.ks[2], A.K, there, A.negated);
+    fragments_of<X, STEPS>(v, lane, (const T *)A.v + b * A.vs[0] + (there ? line : lo) * A.vs[1] + shared * A.vs[2], A.V, there, false);
     const Seen seen = {A.window, A.sinks};
     // queries from lo on; where no key is one of the first tokens, those that have the last one in their window
-    const int first = lo / N, last = (lo < A.sinks ? p.n : (int)min((int64_t)p.n, (int64_t)hi - 1 + A.window)) - 1, tiles = last / N - first + 1, count = tiles * A.group;
-    TileMover<T, E, D, N, kWindowThreads> query_tile, upstream_tile;
+    const int last = (lo < A.sinks ? n : (int)min((int64_t)n, (int64_t)hi - 1 + A.window)) - 1, all_tiles = last / N - lo / N + 1;
+    const int part = parts == 1 ? 0 : piece % A.front_parts;
+    const int first = lo / N + (int)((int64_t)all_tiles * part / parts), tiles = lo / N + (int)((int64_t)all_tiles * (part + 1) / parts) - first, count = tiles * A.group;
+    struct Place { int head, at; };      // of a tile of queries
+    auto next = [&](Place &w) {
+        w.at += N;
+        if (w.at >= (first + tiles) * N) {
+            w.at = first * N;
+            ++w.head;
+        }
+    };
+    TileMover<T, E, D, N, kWindowThreads, WHOLE> query_tile, upstream_tile;
     float2 stats_tile;
     float delta_tile;
-    auto load = [&](int j) {
-        const int head = p.head * A.group + j / tiles, at = (first + j % tiles) * N;
-        query_tile.load((const T *)A.q + p.b * A.qs[0] + head * A.qs[2] + at * A.qs[1], A.qs[1], A.K, p.n - at);
-        upstream_tile.load((const T *)A.grad_out + ((p.b * A.T + at) * A.heads + head) * A.V, g_stride, A.V, p.n - at);
+    auto load = [&](const Place &w) {
+        const int head = shared * A.group + w.head;
+        query_tile.load((const T *)A.q + b * A.qs[0] + head * A.qs[2] + w.at * A.qs[1], A.qs[1], A.K, n - w.at);
+        upstream_tile.load((const T *)A.grad_out + ((b * A.T + w.at) * A.heads + head) * A.V, g_stride, A.V, n - w.at);
         stats_tile = make_float2(0.0f, 0.0f);
         delta_tile = 0.0f;
-        if (threadIdx.x < N && at + (int)threadIdx.x < p.n) {
-            const int64_t place = (p.b * A.heads + head) * A.T + at + threadIdx.x;
+        if (threadIdx.x < N && w.at + (int)threadIdx.x < n) {
+            const int64_t place = (b * A.heads + head) * A.T + w.at + threadIdx.x;
             stats_tile = A.stats[place];
             delta_tile = A.delta[place];
         }
     };
-    typename X::Result acc_k[OUT] = {}, acc_v[OUT] = {};
-    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    load(0);
-    for (int j = 0; j < count; ++j) {
-        const int at = (first + j % tiles) * N;
-        __syncthreads();
-        query_tile.store(queries, A.K, p.n - at);
-        upstream_tile.store(upstream, A.V, p.n - at);
+    auto store = [&](const Place &w, int j) {
+        const int half = j & 1;
+        query_tile.store(queries + half * SIZE, A.K, n - w.at);
+        upstream_tile.store(upstream + half * SIZE, A.V, n - w.at);
         if (threadIdx.x < N) {
-            most[threadIdx.x] = stats_tile.x;
-            inverse[threadIdx.x] = stats_tile.y;
-            delta[threadIdx.x] = delta_tile;
+            most[half * N + threadIdx.x] = stats_tile.x;
+            inverse[half * N + threadIdx.x] = stats_tile.y;
+            delta[half * N + threadIdx.x] = delta_tile;
         }
-        if (!seen.all(at, at + N - 1, lo, lo + ROWS - 1) && (query_tile.spoilt(A.K, p.n - at) || upstream_tile.spoilt(A.V, p.n - at))) spoilt[j & 1] = 1;
-        if (threadIdx.x == 0) spoilt[~j & 1] = 0;
-        __syncthreads();
-        if (j + 1 < count) load(j + 1);
-        const bool whole = at + N <= p.n && seen.all(at, at + N - 1, own, own + M - 1);
-        const bool none = seen.none(at, min(at + N, p.n) - 1, own, min(own + M, hi) - 1), careful = spoilt[j & 1];
-        typename X::Frag weights[N / X::STEP], terms[N / X::STEP];
-        if (!none) {
+        if (!seen.all(w.at, w.at + N - 1, lo, lo + ROWS - 1) && (query_tile.spoilt(A.K, n - w.at) || upstream_tile.spoilt(A.V, n - w.at))) spoilt[half] = j + 1;
+    };
+    typename X::Result acc_k[OUT] = {}, acc_v[OUT] = {};
+    TermScale scale;
+    typename X::Frag weights[N / X::STEP], terms[N / X::STEP];
+    auto weigh = [&](int at, int half) {
         typename X::Result s[QUERIES] = {}, u[QUERIES] = {};
-        product_of_rows<X, D, QUERIES>(lane, queries, k, s);
-        product_of_rows<X, D, QUERIES>(lane, upstream, v, u);
+        product_of_rows<X, D, QUERIES>(lane, queries + half * SIZE, k, s);
+        product_of_rows<X, D, QUERIES>(lane, upstream + half * SIZE, v, u);
 #pragma unroll
         for (int t = 0; t < QUERIES; ++t)
 #pragma unroll
-            for (int i = 0; i < X::REGS; ++i) {
-                const int row = t * M + X::row_of(lane, i);
-                const bool ok = whole | ((at + row < p.n) & seen(at + row, line));
-                s[t][i] = ok ? __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -most[row])) * inverse[row] : 0.0f;
-                u[t][i] = ok ? s[t][i] * (u[t][i] - delta[row]) : 0.0f;
+            for (int i = 0; i < X::REGS; i += 4) {
+                const int row = half * N + t * M + X::row_of(lane, i);
+                const f4 x = *(const f4 *)(most + row), r = *(const f4 *)(inverse + row), d = *(const f4 *)(delta + row);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    s[t][i + c] = __builtin_amdgcn_exp2f(fmaf(s[t][i + c], A.power, -x[c])) * r[c];
+                    u[t][i + c] = s[t][i + c] * (u[t][i + c] - d[c]);
+                }
             }
+        if (at + N > n || !seen.all(at, at + N - 1, own, own + M - 1)) {
+#pragma unroll
+            for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) {
+                    const int query = at + t * M + X::row_of(lane, i);
+                    const bool ok = (query < n) & seen(query, line);
+                    s[t][i] = ok ? s[t][i] : 0.0f;
+                    u[t][i] = ok ? u[t][i] : 0.0f;
+                }
+        }
+        if constexpr (std::is_same_v<E, f16>) {
+            float shrink;
+            if (scale.grown<M, QUERIES>(u, &shrink)) {
+#pragma unroll
+                for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                    for (int i = 0; i < X::REGS; ++i) acc_k[t][i] *= shrink;
+            }
+#pragma unroll
+            for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) {
+                    u[t][i] *= scale.factor;
+                    s[t][i] *= LIFT;
+                }
+        }
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) {
             weights[step] = X::of_results(s, step);
             terms[step] = X::of_results(u, step);
         }
+    };
+    auto none = [&](int at) { return own >= hi || seen.none(at, min(at + N, n) - 1, own, min(own + M, hi) - 1); };
+    bool left_out = false;
+    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
+    Place now = {0, first * N}, ahead = now;
+    if (count > 0) load(ahead);
+    __syncthreads();
+    if (count > 0) store(ahead, 0);
+    next(ahead);
+    if (count > 1) load(ahead);
+    for (int j = 0; j < count; ++j) {
+        const int half = j & 1;
+        __syncthreads();
+        const bool bad = __builtin_amdgcn_readfirstlane(spoilt[half]) == j + 1, skip = bad || none(now.at);
+        left_out |= bad;
+        if (!skip) weigh(now.at, half);
+        if (j + 1 < count) store(ahead, j + 1);
+        next(ahead);
+        if (j + 2 < count) load(ahead);
+        if (!skip) {
+            product_along_rows<X, D, N / X::STEP>(lane, upstream + half * SIZE, weights, acc_v);
+            product_along_rows<X, D, N / X::STEP>(lane, queries + half * SIZE, terms, acc_k);
         }
-        if (careful) {
-            leave_finite<E, D, N, kWindowThreads>(queries);
-            leave_finite<E, D, N, kWindowThreads>(upstream);
-        }
-        if (!none) {
-            product_along_rows<X, D, N / X::STEP>(lane, upstream, weights, acc_v);
-            product_along_rows<X, D, N / X::STEP>(lane, queries, terms, acc_k);
-        }
-        if (careful) {
-            const int head = p.head * A.group + j / tiles, n = p.n - at;
-            auto sees = [&](int r) { return seen(at + r, line); };
-            add_not_finite<X, D, N, kWindowThreads, false>(lane, upstream, (const T *)A.grad_out + ((p.b * A.T + at) * A.heads + head) * A.V, g_stride, A.V, n, none, acc_v, sees);
-            add_not_finite<X, D, N, kWindowThreads, true>(lane, queries, (const T *)A.q + p.b * A.qs[0] + head * A.qs[2] + at * A.qs[1], A.qs[1], A.K, n, none, acc_k, sees);
+        next(now);
+    }
+    if (left_out) {
+        now = {0, first * N};
+#pragma unroll 1
+        for (int j = 0; j < count; ++j, next(now)) {
+            const int at = now.at, half = j & 1, head = shared * A.group + now.head;
+            __syncthreads();
+            load(now);
+            store(now, j);
+            __syncthreads();
+            if (spoilt[half] != j + 1) continue;
+            const bool skip = none(at);
+            if (!skip) weigh(at, half);
+            leave_finite<E, D, N, kWindowThreads>(queries + half * SIZE);
+            leave_finite<E, D, N, kWindowThreads>(upstream + half * SIZE);
+            if (!skip) {
+                product_along_rows<X, D, N / X::STEP>(lane, upstream + half * SIZE, weights, acc_v);
+                product_along_rows<X, D, N / X::STEP>(lane, queries + half * SIZE, terms, acc_k);
+            }
+            auto sees = [&](int r) { return (at + r < n) & seen(at + r, line); };
+            add_not_finite<X, D, N, kWindowThreads, false>(lane, upstream + half * SIZE, (const T *)A.grad_out + ((b * A.T + at) * A.heads + head) * A.V, g_stride, A.V,
+                                                           n - at, skip, acc_v, sees);
+            add_not_finite<X, D, N, kWindowThreads, true>(lane, queries + half * SIZE, (const T *)A.q + b * A.qs[0] + head * A.qs[2] + at * A.qs[1], A.qs[1], A.K,
+                                                          n - at, skip, acc_k, sees);
         }
     }
-    if (there) {
-        store_line<X, D>(out_k + line * k_stride, A.K, lane, acc_k, A.scale);
-        store_line<X, D>(out_v + line * v_stride, A.V, lane, acc_v, 1.0f);
+    const float k_scale = A.scale * scale.back(), v_scale = 1.0f / LIFT;
+    if (there && parts == 1) {
+        store_line<X, D>(out_k + line * k_stride, A.K, lane, acc_k, k_scale);
+        store_line<X, D>(out_v + line * v_stride, A.V, lane, acc_v, v_scale);
+    } else if (there) {
+        float *to = A.parts + (((head_line * A.front + tile) * parts + part) * ROWS + (line - lo)) * (A.K + A.V);
+        store_line<X, D>(to, A.K, lane, acc_k, k_scale);
+        store_line<X, D>(to + A.K, A.V, lane, acc_v, v_scale);
     }
-    if (hi < end) {
+    if (hi < end && zeros) {
         zero_rows(out_k, k_stride, A.K, hi, end);
         zero_rows(out_v, v_stride, A.V, hi, end);
+    }
+}
+
+// The sum of the front tiles' parts, in their order: a key a workgroup
+template <typename T, int ROWS>
+__global__ __launch_bounds__(kWindowThreads) void sig_window_join_kernel(WindowArgs A)
+{
+    const int shared_heads = A.heads / A.group, keys = A.front * ROWS;
+    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, head_line = id / keys;
+    const int key = (int)(id % keys);
+    if (head_line >= A.B * shared_heads) return;
+    const int64_t b = head_line / shared_heads, n = A.lengths ? A.lengths[b] : A.T;
+    if (key >= n || key >= A.T) return;      // (those are zero by now)
+    const float *parts = A.parts + ((head_line * A.front + key / ROWS) * A.front_parts * ROWS + key % ROWS) * (A.K + A.V);
+    for (int c = threadIdx.x; c < A.K + A.V; c += kWindowThreads) {
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < A.front_parts; ++i) sum += parts[(int64_t)i * ROWS * (A.K + A.V) + c];
+        const int64_t row = (b * A.T + key) * shared_heads + head_line % shared_heads;
+        if (c < A.K) ((T *)A.grad_k)[row * A.K + c] = from_float<T>(sum);
+        else ((T *)A.grad_v)[row * A.V + c - A.K] = from_float<T>(sum);
     }
 }
 
@@ -424,27 +648,43 @@ hipError_t launch_window_f32(const WindowArgs &A, WindowPass pass, hipStream_t s
 hipError_t launch_window_bf16(const WindowArgs &A, WindowPass pass, hipStream_t st);
 hipError_t launch_window_f16(const WindowArgs &A, WindowPass pass, hipStream_t st);
 
-// T: in memory; E: of the products
-template <typename T, typename E>
-hipError_t launch_window(WindowArgs A, WindowPass pass, hipStream_t st)
+// lines of a workgroup, for rows of up to `dim` values
+inline int window_rows(int type, int dim) { return type == SIG_F32 || dim > 128 ? kWindowWaves * 16 : kWindowWaves * 32; }
+
+inline dim3 window_grid(int64_t blocks)
+{
+    const int64_t across = ((int64_t)1 << 32) / kWindowThreads - 1;      // (a launch holds fewer than 2^32 threads along an axis)
+    return dim3((unsigned)(blocks < across ? blocks : across), (unsigned)((blocks + across - 1) / across));
+}
+
+template <typename T>
+hipError_t launch_window(const WindowArgs &A, WindowPass pass, hipStream_t st)
 {
     const int dim = A.K > A.V ? A.K : A.V;
-    auto go = [&](auto x, auto d) {
+    const int64_t shared = A.B * (A.heads / A.group);
+    auto go = [&](auto x, auto d, auto whole) {
         using X = typename decltype(x)::type;
-        constexpr int D = decltype(d)::value, ROWS = kWindowWaves * X::M, BYTES = D * (int)sizeof(E);
+        constexpr int D = decltype(d)::value, BYTES = D * (int)sizeof(T), ROWS = kWindowWaves * X::M;
+        constexpr bool WHOLE = decltype(whole)::value;
         // tokens of a tile
-        constexpr int N = BYTES > 512 ? 16 : BYTES > 128 ? 32 : 64, GRADIENT = BYTES > 512 ? 16 : 32;
-        A.tiles = (A.T + ROWS - 1) / ROWS;
-        const int64_t blocks = A.B * (pass == WINDOW_KEY_GRADIENT ? A.heads / A.group : A.heads) * A.tiles;
-        const int64_t across = ((int64_t)1 << 32) / kWindowThreads - 1;      // (a launch holds fewer than 2^32 threads along an axis)
-        const dim3 grid((unsigned)(blocks < across ? blocks : across), (unsigned)((blocks + across - 1) / across));
-        if (pass == WINDOW_FORWARD) sig_window_forward_kernel<T, X, D, N><<<grid, kWindowThreads, 0, st>>>(A);
-        else if (pass == WINDOW_QUERY_GRADIENT) sig_window_query_gradient_kernel<T, X, D, N><<<grid, kWindowThreads, 0, st>>>(A);
-        else sig_window_key_gradient_kernel<T, X, D, GRADIENT><<<grid, kWindowThreads, 0, st>>>(A);
+        constexpr int N = BYTES > 512 ? 16 : BYTES > WINDOW_WIDE ? 32 : 64, QUERY = BYTES > 512 ? 16 : BYTES > WINDOW_QUERY_WIDE ? 32 : 64, KEY = BYTES > 512 ? 16 : 32;
+        if (pass == WINDOW_FORWARD) {
+            sig_window_forward_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
+        } else if (pass == WINDOW_QUERY_GRADIENT) {
+            sig_window_query_gradient_kernel<T, X, D, QUERY, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
+        } else {
+            const int64_t pieces = A.front * A.front_parts + A.tiles - A.front;
+            sig_window_key_gradient_kernel<T, X, D, KEY, WHOLE><<<window_grid(shared * pieces), kWindowThreads, 0, st>>>(A);
+            if (A.front && A.front_parts > 1) sig_window_join_kernel<T, ROWS><<<window_grid(shared * A.front * ROWS), kWindowThreads, 0, st>>>(A);
+        }
     };
-    if (dim <= 64) go(Tag<Tiles<E>>(), std::integral_constant<int, 64>());
-    else if (dim <= 128) go(Tag<Tiles<E>>(), std::integral_constant<int, 128>());
-    else go(Tag<SmallTiles<E>>(), std::integral_constant<int, 256>());
+    auto with = [&](auto x, auto d) {
+        if (A.K == decltype(d)::value && A.V == A.K) go(x, d, std::true_type());
+        else go(x, d, std::false_type());
+    };
+    if (dim <= 64) with(Tag<Tiles<T>>(), std::integral_constant<int, 64>());
+    else if (dim <= 128) with(Tag<Tiles<T>>(), std::integral_constant<int, 128>());
+    else with(Tag<SmallTiles<T>>(), std::integral_constant<int, 256>());
     return hipGetLastError();
 }
 

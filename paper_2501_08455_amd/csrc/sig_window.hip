@@ -9,6 +9,7 @@ namespace {
 
 constexpr int kMostDim = 256;
 constexpr double kLog2E = 1.4426950408889634;
+constexpr int kMostParts = 64;      // of the first tokens' queries
 
 int check(const sig_ctx *ctx, const sig_window_t *s)
 {
@@ -45,6 +46,8 @@ WindowArgs arguments(const sig_window_t &s, const void *q, const void *k, const 
     // (a scale of 0 is taken as the smallest one, so that the scores of what is hidden stay minus infinity)
     A.power = fmaxf((float)(fabs((double)s.scale) * kLog2E), FLT_MIN);
     A.negated = s.scale < 0.0f;
+    const int rows = window_rows(s.type, A.K > A.V ? A.K : A.V);
+    A.tiles = (A.T + rows - 1) / rows;
     return A;
 }
 
@@ -85,9 +88,20 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
     A.grad_q = grad_q;
     A.grad_k = grad_k;
     A.grad_v = grad_v;
+    // The first tokens' tiles are cut where they have more than twice the queries of the others
+    const int rows = window_rows(shape->type, A.K > A.V ? A.K : A.V);
+    const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T;
+    A.front_parts = 1;
+    if (A.sinks > 0 && A.T > usual) {
+        A.front = (A.sinks + rows - 1) / rows;
+        const int64_t parts = (A.T + usual - 1) / usual;
+        A.front_parts = (int)(parts < kMostParts ? parts : kMostParts);
+    }
+    const int64_t joined = A.front * A.front_parts * (int64_t)rows * (A.K + A.V) * A.B * shape->shared_heads;
     Scratch scratch;
-    rc = scratch.get(ctx, (size_t)(A.B * A.heads) * A.T * sizeof(float), st, &A.delta);
+    rc = scratch.get(ctx, (size_t)(deltas + joined) * sizeof(float), st, &A.delta);
     if (rc != SIG_OK) return rc;
+    A.parts = A.delta + deltas;
     hipError_t e = launch(A, shape->type, WINDOW_QUERY_GRADIENT, st);
     if (e == hipSuccess) e = launch(A, shape->type, WINDOW_KEY_GRADIENT, st);
     return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;

@@ -1,3 +1,3 @@
 #include "sig_window.h"
 
-hipError_t sig::launch_window_bf16(const WindowArgs &A, WindowPass pass, hipStream_t st) { return launch_window<bf16, bf16>(A, pass, st); }
+hipError_t sig::launch_window_bf16(const WindowArgs &A, WindowPass pass, hipStream_t st) { return launch_window<bf16>(A, pass, st); }
