@@ -149,8 +149,8 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  *   grad_out     DEVICE, [B][T][heads][value_dim] of `type`, contiguous; what stands behind the lengths is not read
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
- * Context scratch of B * heads * T floats, and where sequences are much longer than the window, for the sinks' gradients in up to 64 parts: B * shared_heads
- * floats times the parts, the sinks rounded up to 128, and key_dim + value_dim.
+ * Context scratch of B * heads * T floats; and where sequences are much longer than the window, for the sinks' gradients in up to 64 parts, or where keys are few, for
+ * all of them in up to 64 parts (some four of 64 or 128 keys for each compute unit): key_dim + value_dim floats for each key and part.
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
                                   const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);

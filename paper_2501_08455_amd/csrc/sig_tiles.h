@@ -206,12 +206,14 @@ __device__ inline void fragments_of(typename X::Frag *f, int lane, const T *line
 // WHOLE: rows have D values.
 template <typename T, typename E, int D, int ROWS, int THREADS, bool WHOLE>
 struct TileMover {
-    static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = ROWS * GROUPS / THREADS;
-    static_assert(ROWS * GROUPS % THREADS == 0);
+    static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = (ROWS * GROUPS + THREADS - 1) / THREADS;
+    static constexpr bool EVEN = ROWS * GROUPS % THREADS == 0;      // else some threads have no last group (they load what is there, and drop it)
     Words<T, GROUP> held[COUNT];
 
     static __device__ int row_of(int i) { return (threadIdx.x + i * THREADS) / GROUPS; }
     static __device__ int place_of(int i) { return (threadIdx.x + i * THREADS) % GROUPS * GROUP; }
+
+    static __device__ bool here(int i) { return EVEN || (int)threadIdx.x + i * THREADS < ROWS * GROUPS; }
 
     // rows 0 ... n - 1 are there, n >= 1
     __device__ void load(const T *first, int64_t stride, int dim, int n)
@@ -250,7 +252,7 @@ struct TileMover {
 #pragma unroll
             for (int j = 0; j < (int)sizeof(held[i]) / 4; ++j) bad |= word_spoilt<T>(held[i][j]);
             const bool there = row_of(i) < n, within = WHOLE || place_of(i) < dim;
-            any |= bad & there & within;
+            any |= bad & there & within & here(i);
         }
         return any;
     }
@@ -267,21 +269,28 @@ struct TileMover {
                 for (int j = 0; j < GROUP; ++j) bits[j] = (float)values[j];
             }
             const bool there = row_of(i) < n, within = WHOLE || place_of(i) < dim, ok = there & within;
-            *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = ok ? bits : f4{};
+            if (EVEN || here(i)) *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = ok ? bits : f4{};
         }
     }
 };
 
-// acc[t] += columns(tile)' x p, tile by tile of D / M: `p` are STEPS fragments along the tile's rows
-template <typename X, int D, int STEPS>
-__device__ inline void product_along_rows(int lane, const typename X::E *tile, const typename X::Frag *p, typename X::Result *acc)
+// acc[t] += columns(tile)' x p, tile by tile of D / M: `p` are STEPS fragments along the tile's rows.  Unless WHOLE, only `dim` of the D columns are there,
+// and quarters of D that have none are left out.  Between APART steps nothing is moved: else all reads are moved to the front, and more registers
+// are asked for than there are.
+template <typename X, int D, int STEPS, bool WHOLE, int APART = 1>
+__device__ inline void product_along_rows(int lane, const typename X::E *tile, const typename X::Frag *p, typename X::Result *acc, int dim)
 {
     using E = typename X::E;
+    constexpr int PIECES = WHOLE ? 1 : 4, TILES = D / X::M / PIECES > 0 ? D / X::M / PIECES : 1;
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
+    for (int piece = 0; piece < D / X::M; piece += TILES) {
+        if (!WHOLE && piece * X::M >= dim) break;
 #pragma unroll
-        for (int t = 0; t < D / X::M; ++t) acc[t] = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j * X::STEP, t * X::M), p[j], acc[t]);
-        __builtin_amdgcn_sched_barrier(0);      // (else all reads are moved to the front, and more registers are asked for than there are)
+        for (int j = 0; j < STEPS; ++j) {
+#pragma unroll
+            for (int t = piece; t < piece + TILES; ++t) acc[t] = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j * X::STEP, t * X::M), p[j], acc[t]);
+            if (j % APART == APART - 1) __builtin_amdgcn_sched_barrier(0);
+        }
     }
 }
 
@@ -334,16 +343,21 @@ __device__ inline void add_not_finite(int lane, typename X::E *tile, const T *fi
     }
 }
 
-// s[t] += rows(tile) x own, tile by tile of COUNT M rows
-template <typename X, int D, int COUNT>
-__device__ inline void product_of_rows(int lane, const typename X::E *tile, const typename X::Frag *own, typename X::Result *s)
+// s[t] += rows(tile) x own, tile by tile of COUNT M rows (WHOLE, dim, APART: as above)
+template <typename X, int D, int COUNT, bool WHOLE, int APART = 2>
+__device__ inline void product_of_rows(int lane, const typename X::E *tile, const typename X::Frag *own, typename X::Result *s, int dim)
 {
     using E = typename X::E;
+    constexpr int PIECES = WHOLE ? 1 : 4, STEPS = D / X::STEP / PIECES > 0 ? D / X::STEP / PIECES : 1;
 #pragma unroll
-    for (int step = 0; step < D / X::STEP; ++step) {
+    for (int piece = 0; piece < D / X::STEP; piece += STEPS) {
+        if (!WHOLE && piece * X::STEP >= dim) break;
 #pragma unroll
-        for (int t = 0; t < COUNT; ++t) s[t] = X::multiply(X::template rows<LdsTile<E, D>>(lane, tile, t * X::M, step * X::STEP), own[step], s[t]);
-        if (step % 2) __builtin_amdgcn_sched_barrier(0);
+        for (int step = piece; step < piece + STEPS; ++step) {
+#pragma unroll
+            for (int t = 0; t < COUNT; ++t) s[t] = X::multiply(X::template rows<LdsTile<E, D>>(lane, tile, t * X::M, step * X::STEP), own[step], s[t]);
+            if (step % APART == APART - 1) __builtin_amdgcn_sched_barrier(0);
+        }
     }
 }
 

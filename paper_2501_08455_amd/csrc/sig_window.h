@@ -24,13 +24,6 @@
 
 namespace sig {
 
-#ifndef WINDOW_WIDE
-#define WINDOW_WIDE 128
-#define WINDOW_QUERY_WIDE 128
-#define WINDOW_QUERY_BYTES 128
-#define WINDOW_KEY_BYTES 64
-#endif
-
 constexpr int kWindowThreads = 256, kWindowWaves = kWindowThreads / 64;
 
 struct WindowArgs {
@@ -43,8 +36,10 @@ struct WindowArgs {
     const void *grad_out;                 // as `out`
     void *grad_q, *grad_k, *grad_v;       // as q, k, v, contiguous
     float *delta;                         // [B][heads][T]: D
-    float *parts;                         // [B][shared heads][front tiles][parts][rows of a tile][K + V], for the keys that everyone sees
-    int front, front_parts;               // those keys' tiles, and the parts that their queries are cut into
+    // Keys' gradients that are cut along the queries: `cut` tiles into `parts` each, whose sums for the first `joined` keys are added up from scratch,
+    // [B][shared heads][cut][parts][rows of a tile][K + V].  Either all tiles, evenly, where there are few, or those of the first tokens, which every query sees
+    float *sums;
+    int cut, parts, joined, even;
     int64_t B;
     int T, heads, group, K, V;
     int window, sinks;                    // at most T
@@ -127,10 +122,10 @@ __device__ inline void store_line(T *line, int dim, int lane, const typename X::
         }
 }
 
-template <typename T>
+template <int THREADS = kWindowThreads, typename T>
 __device__ inline void zero_rows(T *first, int64_t stride, int dim, int from, int to)
 {
-    for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * dim; i += kWindowThreads) first[(from + i / dim) * stride + i % dim] = from_float<T>(0.0f);
+    for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * dim; i += THREADS) first[(from + i / dim) * stride + i % dim] = from_float<T>(0.0f);
 }
 
 // What float16 holds is small: probabilities are scaled up by a power of two, so that those of a long row's tokens are not rounded as subnormal numbers.
@@ -212,7 +207,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
     // the probabilities of tile j, and the running maximum and sum
     auto weigh = [&](int at, const E *keys) {
         typename X::Result s[KEYS] = {};
-        product_of_rows<X, D, KEYS>(lane, keys, q, s);
+        product_of_rows<X, D, KEYS, WHOLE>(lane, keys, q, s, A.K);
         if (!seen.all(own, own + M - 1, at, at + N - 1)) {
 #pragma unroll
             for (int t = 0; t < KEYS; ++t)
@@ -266,7 +261,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
         if (!skip) weigh(at, keys + half);
         if (j + 1 < tiles.count) store(j + 1);
         if (j + 2 < tiles.count) load(j + 2);
-        if (!skip) product_along_rows<X, D, N / X::STEP>(lane, values + half, probabilities, acc);
+        if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, values + half, probabilities, acc, A.V);
     }
     if (left_out) {
 #pragma unroll 1
@@ -281,7 +276,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
             const bool skip = none(at);
             if (!skip) weigh(at, keys + (j & 1) * SIZE);
             leave_finite<E, D, N, kWindowThreads>(tile);
-            if (!skip) product_along_rows<X, D, N / X::STEP>(lane, tile, probabilities, acc);
+            if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, tile, probabilities, acc, A.V);
             add_not_finite<X, D, N, kWindowThreads, false>(lane, tile, v + at * A.vs[1], A.vs[1], A.V, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
     }
@@ -296,7 +291,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
 
 // ---------------------------------------------------------------- gradient of the queries, and D
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW_QUERY_BYTES ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE ? 256 : 128) ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
     constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
@@ -356,8 +351,8 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
     typename X::Frag terms[N / X::STEP];
     auto weigh = [&](int at, const E *keys, const E *values) {
         typename X::Result s[KEYS] = {}, u[KEYS] = {};
-        product_of_rows<X, D, KEYS>(lane, keys, q, s);
-        product_of_rows<X, D, KEYS>(lane, values, g, u);
+        product_of_rows<X, D, KEYS, WHOLE>(lane, keys, q, s, A.K);
+        product_of_rows<X, D, KEYS, WHOLE>(lane, values, g, u, A.V);
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
@@ -399,7 +394,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
         if (!skip) weigh(at, keys + half, values + half);
         if (j + 1 < tiles.count) store(j + 1);
         if (j + 2 < tiles.count) load(j + 2);
-        if (!skip) product_along_rows<X, D, N / X::STEP>(lane, keys + half, terms, acc);
+        if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, keys + half, terms, acc, A.K);
     }
     if (left_out) {
 #pragma unroll 1
@@ -414,7 +409,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
             const bool skip = none(at);
             if (!skip) weigh(at, tile, values + (j & 1) * SIZE);
             leave_finite<E, D, N, kWindowThreads>(tile);
-            if (!skip) product_along_rows<X, D, N / X::STEP>(lane, tile, terms, acc);
+            if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, tile, terms, acc, A.K);
             add_not_finite<X, D, N, kWindowThreads, true>(lane, tile, k + at * A.ks[1], A.ks[1], A.K, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
     }
@@ -423,53 +418,74 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
 }
 
 // ---------------------------------------------------------------- gradient of keys and values
-// A wavefront's own lines are keys; queries and upstream gradients of all heads that share them come as tiles, one head after the other, so
-// that the sum over these heads is one of registers.  The first tokens' tiles, which every query sees, are cut into parts along the queries, and joined
-// from scratch.
+// Own lines are keys; queries and upstream gradients of all heads that share them come as tiles, one head after the other, so that the sum over these
+// heads is one of registers.  Two wavefronts, on the same matrix unit, share M keys: the first holds the keys, works out p and adds up grad v; the second holds the
+// values, takes p from LDS a tile later, and adds up grad k.  Each has half of the registers' load, and one multiplies while the other one
+// does not (both gradients in one wavefront, one a unit: 1,510 us where this takes ; 8 x 4,096 tokens, 16 heads of 128 bfloat16, window 1,024).  Few
+// tiles, and those of the first tokens, which every query sees, are cut into parts along the queries, and joined from scratch.
+constexpr int kKeyThreads = 2 * kWindowThreads;
+
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW_KEY_BYTES ? 2 : 1) void sig_window_key_gradient_kernel(WindowArgs A)
+__global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH, NUMBERS = QUERIES * X::REGS;
     constexpr float LIFT = std::is_same_v<E, f16> ? 32768.0f : 1.0f;      // of the probabilities, which are at most 1 (see kLift)
-    __shared__ __attribute__((aligned(16))) E queries[2 * SIZE];
-    __shared__ __attribute__((aligned(16))) E upstream[2 * SIZE];
-    __shared__ __attribute__((aligned(16))) float most[2 * N], inverse[2 * N], delta[2 * N];
-    __shared__ int spoilt[2];
-    // which head and keys: the front tiles' parts first, then the other tiles
-    const int shared_heads = A.heads / A.group, pieces = A.front * A.front_parts + A.tiles - A.front;
+    __shared__ __attribute__((aligned(16))) E queries[3 * SIZE];
+    __shared__ __attribute__((aligned(16))) E upstream[3 * SIZE];
+    __shared__ __attribute__((aligned(16))) float most[3 * N], inverse[3 * N], delta[3 * N];
+    __shared__ __attribute__((aligned(16))) f4 passed[2][kWindowWaves][NUMBERS / 4][64];      // p, as the lanes hold it
+    __shared__ int spoilt[3];
+    // which head and keys: the cut tiles' parts first, then the other tiles
+    const int shared_heads = A.heads / A.group, pieces = A.cut * A.parts + A.tiles - A.cut;
     const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, lines = A.B * shared_heads;
     if (id >= lines * pieces) return;
     const bool by_eight = lines % 8 == 0;      // (see window_place)
     const int64_t head_line = by_eight ? id / 8 / pieces * 8 + id % 8 : id % lines;
     const int piece = (int)(by_eight ? id / 8 % pieces : id / lines);
     const int64_t b = head_line / shared_heads;
-    const int shared = (int)(head_line % shared_heads), front_pieces = A.front * A.front_parts;
-    const int tile = piece < front_pieces ? piece / A.front_parts : piece - front_pieces + A.front, parts = piece < front_pieces ? A.front_parts : 1;
+    const int shared = (int)(head_line % shared_heads), cut_pieces = A.cut * A.parts;
+    const int tile = piece < cut_pieces ? piece / A.parts : piece - cut_pieces + A.cut, parts = piece < cut_pieces ? A.parts : 1, part = parts == 1 ? 0 : piece % A.parts;
     const int64_t counted = A.lengths ? A.lengths[b] : A.T;
     const int n = counted < 0 ? 0 : counted > A.T ? A.T : (int)counted;
 
     const int lane = threadIdx.x % 64, lo = tile * ROWS, end = min(lo + ROWS, A.T);
     T *out_k = (T *)A.grad_k + ((b * A.T) * shared_heads + shared) * A.K, *out_v = (T *)A.grad_v + ((b * A.T) * shared_heads + shared) * A.V;
     const int64_t k_stride = (int64_t)shared_heads * A.K, v_stride = (int64_t)shared_heads * A.V, g_stride = (int64_t)A.heads * A.V;
-    const bool zeros = parts == 1 || piece % A.front_parts == 0;      // whether this workgroup clears what stands behind the sequence
+    const bool zeros = part == 0;      // whether this workgroup clears what stands behind the sequence
     if (lo >= n) {
         if (!zeros) return;
-        zero_rows(out_k, k_stride, A.K, lo, end);
-        zero_rows(out_v, v_stride, A.V, lo, end);
+        zero_rows<kKeyThreads>(out_k, k_stride, A.K, lo, end);
+        zero_rows<kKeyThreads>(out_v, v_stride, A.V, lo, end);
         return;
     }
-    const int hi = min(end, n);
-    const int own = lo + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * M, line = own + lane % M;
+    const int hi = min(end, n), wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64), pair = wave % kWindowWaves;
+    const bool second = wave >= kWindowWaves;
+    const int own = lo + pair * M, line = own + lane % M;
     const bool there = line < n;
-    typename X::Frag k[STEPS], v[STEPS];
-    fragments_of<X, STEPS>(k, lane, (const T *)A.k + b * A.ks[0] + (there ? line : lo) * A.ks[1] + shared * A.ks[2], A.K, there, A.negated);
-    fragments_of<X, STEPS>(v, lane, (const T *)A.v + b * A.vs[0] + (there ? line : lo) * A.vs[1] + shared * A.vs[2], A.V, there, false);
+    typename X::Frag held[STEPS];      // keys, or values
+    {
+        const int row = there ? line : lo;
+        if (second) fragments_of<X, STEPS>(held, lane, (const T *)A.v + b * A.vs[0] + row * A.vs[1] + shared * A.vs[2], A.V, there, false);
+        else fragments_of<X, STEPS>(held, lane, (const T *)A.k + b * A.ks[0] + row * A.ks[1] + shared * A.ks[2], A.K, there, A.negated);
+    }
     const Seen seen = {A.window, A.sinks};
     // queries from lo on; where no key is one of the first tokens, those that have the last one in their window
     const int last = (lo < A.sinks ? n : (int)min((int64_t)n, (int64_t)hi - 1 + A.window)) - 1, all_tiles = last / N - lo / N + 1;
-    const int part = parts == 1 ? 0 : piece % A.front_parts;
-    const int first = lo / N + (int)((int64_t)all_tiles * part / parts), tiles = lo / N + (int)((int64_t)all_tiles * (part + 1) / parts) - first, count = tiles * A.group;
+    // tiles of queries, of one head after the other: first ... first + tiles - 1, and of those numbers `from` to `until`
+    int first = lo / N, tiles = all_tiles, from = 0, until = tiles * A.group;
+    if (parts > 1 && A.even) {
+        from = (int)((int64_t)tiles * A.group * part / parts);
+        until = (int)((int64_t)tiles * A.group * (part + 1) / parts);
+    } else if (parts > 1) {
+        // (part 0 are the queries that have keys of this tile in their window, the others see the first tokens alone)
+        const int near = ((int)min((int64_t)n, (int64_t)hi - 1 + A.window) - 1) / N - lo / N + 1, far = all_tiles - near;
+        const int low = part == 0 ? 0 : near + (int)((int64_t)far * (part - 1) / (parts - 1)), high = part == 0 ? near : near + (int)((int64_t)far * part / (parts - 1));
+        first += low;
+        tiles = high - low;
+        until = tiles * A.group;
+    }
+    const int count = until - from;
     struct Place { int head, at; };      // of a tile of queries
     auto next = [&](Place &w) {
         w.at += N;
@@ -478,7 +494,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
             ++w.head;
         }
     };
-    TileMover<T, E, D, N, kWindowThreads, WHOLE> query_tile, upstream_tile;
+    TileMover<T, E, D, N, kKeyThreads, WHOLE> query_tile, upstream_tile;
     float2 stats_tile;
     float delta_tile;
     auto load = [&](const Place &w) {
@@ -493,46 +509,70 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
             delta_tile = A.delta[place];
         }
     };
-    auto store = [&](const Place &w, int j) {
-        const int half = j & 1;
-        query_tile.store(queries + half * SIZE, A.K, n - w.at);
-        upstream_tile.store(upstream + half * SIZE, A.V, n - w.at);
+    // `room`: of three, j % 3
+    auto store = [&](const Place &w, int j, int room) {
+        query_tile.store(queries + room * SIZE, A.K, n - w.at);
+        upstream_tile.store(upstream + room * SIZE, A.V, n - w.at);
         if (threadIdx.x < N) {
-            most[half * N + threadIdx.x] = stats_tile.x;
-            inverse[half * N + threadIdx.x] = stats_tile.y;
-            delta[half * N + threadIdx.x] = delta_tile;
+            most[room * N + threadIdx.x] = stats_tile.x;
+            inverse[room * N + threadIdx.x] = stats_tile.y;
+            delta[room * N + threadIdx.x] = delta_tile;
         }
-        if (!seen.all(w.at, w.at + N - 1, lo, lo + ROWS - 1) && (query_tile.spoilt(A.K, n - w.at) || upstream_tile.spoilt(A.V, n - w.at))) spoilt[half] = j + 1;
+        if (!seen.all(w.at, w.at + N - 1, lo, lo + ROWS - 1) && (query_tile.spoilt(A.K, n - w.at) || upstream_tile.spoilt(A.V, n - w.at))) spoilt[room] = j + 1;
     };
-    typename X::Result acc_k[OUT] = {}, acc_v[OUT] = {};
+    typename X::Result acc[OUT] = {};
     TermScale scale;
-    typename X::Frag weights[N / X::STEP], terms[N / X::STEP];
-    auto weigh = [&](int at, int half) {
-        typename X::Result s[QUERIES] = {}, u[QUERIES] = {};
-        product_of_rows<X, D, QUERIES>(lane, queries + half * SIZE, k, s);
-        product_of_rows<X, D, QUERIES>(lane, upstream + half * SIZE, v, u);
+    typename X::Frag weights[N / X::STEP];
+    auto hidden = [&](int at) { return at + N > n || !seen.all(at, at + N - 1, own, own + M - 1); };
+    auto sees = [&](int query) { return (query < n) & seen(query, line); };
+    // the probabilities of a tile, for the second wavefront too
+    auto weigh_values = [&](int at, int room, int half) {
+        typename X::Result s[QUERIES] = {};
+        product_of_rows<X, D, QUERIES, WHOLE, 4>(lane, queries + room * SIZE, held, s, A.K);
 #pragma unroll
         for (int t = 0; t < QUERIES; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; i += 4) {
-                const int row = half * N + t * M + X::row_of(lane, i);
-                const f4 x = *(const f4 *)(most + row), r = *(const f4 *)(inverse + row), d = *(const f4 *)(delta + row);
+                const int row = room * N + t * M + X::row_of(lane, i);
+                const f4 x = *(const f4 *)(most + row), r = *(const f4 *)(inverse + row);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    s[t][i + c] = __builtin_amdgcn_exp2f(fmaf(s[t][i + c], A.power, -x[c])) * r[c];
-                    u[t][i + c] = s[t][i + c] * (u[t][i + c] - d[c]);
-                }
+                for (int c = 0; c < 4; ++c) s[t][i + c] = __builtin_amdgcn_exp2f(fmaf(s[t][i + c], A.power, -x[c])) * r[c];
             }
-        if (at + N > n || !seen.all(at, at + N - 1, own, own + M - 1)) {
+        if (hidden(at)) {
 #pragma unroll
             for (int t = 0; t < QUERIES; ++t)
 #pragma unroll
-                for (int i = 0; i < X::REGS; ++i) {
-                    const int query = at + t * M + X::row_of(lane, i);
-                    const bool ok = (query < n) & seen(query, line);
-                    s[t][i] = ok ? s[t][i] : 0.0f;
-                    u[t][i] = ok ? u[t][i] : 0.0f;
-                }
+                for (int i = 0; i < X::REGS; ++i) s[t][i] = sees(at + t * M + X::row_of(lane, i)) ? s[t][i] : 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+            for (int i = 0; i < X::REGS; i += 4) passed[half][pair][(t * X::REGS + i) / 4][lane] = f4{s[t][i], s[t][i + 1], s[t][i + 2], s[t][i + 3]};
+        if constexpr (std::is_same_v<E, f16>) {
+#pragma unroll
+            for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) s[t][i] *= LIFT;
+        }
+#pragma unroll
+        for (int step = 0; step < N / X::STEP; ++step) weights[step] = X::of_results(s, step);
+    };
+    auto weigh_keys = [&](int at, int room, int half) {
+        typename X::Result u[QUERIES] = {};
+        product_of_rows<X, D, QUERIES, WHOLE, 4>(lane, upstream + room * SIZE, held, u, A.V);
+#pragma unroll
+        for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+            for (int i = 0; i < X::REGS; i += 4) {
+                const f4 p = passed[half][pair][(t * X::REGS + i) / 4][lane], d = *(const f4 *)(delta + room * N + t * M + X::row_of(lane, i));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) u[t][i + c] = p[c] * (u[t][i + c] - d[c]);
+            }
+        if (hidden(at)) {
+#pragma unroll
+            for (int t = 0; t < QUERIES; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) u[t][i] = sees(at + t * M + X::row_of(lane, i)) ? u[t][i] : 0.0f;
         }
         if constexpr (std::is_same_v<E, f16>) {
             float shrink;
@@ -540,101 +580,104 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= WINDOW
 #pragma unroll
                 for (int t = 0; t < OUT; ++t)
 #pragma unroll
-                    for (int i = 0; i < X::REGS; ++i) acc_k[t][i] *= shrink;
+                    for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
             }
 #pragma unroll
             for (int t = 0; t < QUERIES; ++t)
 #pragma unroll
-                for (int i = 0; i < X::REGS; ++i) {
-                    u[t][i] *= scale.factor;
-                    s[t][i] *= LIFT;
-                }
+                for (int i = 0; i < X::REGS; ++i) u[t][i] *= scale.factor;
         }
 #pragma unroll
-        for (int step = 0; step < N / X::STEP; ++step) {
-            weights[step] = X::of_results(s, step);
-            terms[step] = X::of_results(u, step);
-        }
+        for (int step = 0; step < N / X::STEP; ++step) weights[step] = X::of_results(u, step);
     };
     auto none = [&](int at) { return own >= hi || seen.none(at, min(at + N, n) - 1, own, min(own + M, hi) - 1); };
-    bool left_out = false;
-    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    Place now = {0, first * N}, ahead = now;
+    // Tile j is the first wavefronts' and tile j - 1 the second ones', tile j + 1 goes to LDS, j + 2 is on its way
+    bool left_out = false, skipped = true;      // skipped: the tile before
+    if (threadIdx.x < 3) spoilt[threadIdx.x] = 0;
+    const Place begin = {tiles > 0 ? from / tiles : 0, (first + (tiles > 0 ? from % tiles : 0)) * N};
+    Place now = begin, before = now, ahead = now;
     if (count > 0) load(ahead);
     __syncthreads();
-    if (count > 0) store(ahead, 0);
+    if (count > 0) store(ahead, 0, 0);
     next(ahead);
     if (count > 1) load(ahead);
-    for (int j = 0; j < count; ++j) {
-        const int half = j & 1;
+    int room = 0, behind = 2;
+    for (int j = 0; j <= count; ++j) {
+        const int following = room == 2 ? 0 : room + 1;
         __syncthreads();
-        const bool bad = __builtin_amdgcn_readfirstlane(spoilt[half]) == j + 1, skip = bad || none(now.at);
+        const bool bad = j < count && __builtin_amdgcn_readfirstlane(spoilt[room]) == j + 1, skip = bad || j == count || none(now.at);
         left_out |= bad;
-        if (!skip) weigh(now.at, half);
-        if (j + 1 < count) store(ahead, j + 1);
+        if (!second && !skip) {
+            weigh_values(now.at, room, j & 1);
+            product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, upstream + room * SIZE, weights, acc, A.V);
+        }
+        if (second && !skipped) {
+            weigh_keys(before.at, behind, ~j & 1);
+            product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, queries + behind * SIZE, weights, acc, A.K);
+        }
+        if (j + 1 < count) store(ahead, j + 1, following);
         next(ahead);
         if (j + 2 < count) load(ahead);
-        if (!skip) {
-            product_along_rows<X, D, N / X::STEP>(lane, upstream + half * SIZE, weights, acc_v);
-            product_along_rows<X, D, N / X::STEP>(lane, queries + half * SIZE, terms, acc_k);
-        }
+        skipped = skip;
+        before = now;
         next(now);
+        behind = room;
+        room = following;
     }
     if (left_out) {
-        now = {0, first * N};
+        now = begin;
 #pragma unroll 1
         for (int j = 0; j < count; ++j, next(now)) {
-            const int at = now.at, half = j & 1, head = shared * A.group + now.head;
+            const int at = now.at, head = shared * A.group + now.head;
             __syncthreads();
             load(now);
-            store(now, j);
+            store(now, j, 0);
             __syncthreads();
-            if (spoilt[half] != j + 1) continue;
+            if (spoilt[0] != j + 1) continue;
             const bool skip = none(at);
-            if (!skip) weigh(at, half);
-            leave_finite<E, D, N, kWindowThreads>(queries + half * SIZE);
-            leave_finite<E, D, N, kWindowThreads>(upstream + half * SIZE);
-            if (!skip) {
-                product_along_rows<X, D, N / X::STEP>(lane, upstream + half * SIZE, weights, acc_v);
-                product_along_rows<X, D, N / X::STEP>(lane, queries + half * SIZE, terms, acc_k);
-            }
-            auto sees = [&](int r) { return (at + r < n) & seen(at + r, line); };
-            add_not_finite<X, D, N, kWindowThreads, false>(lane, upstream + half * SIZE, (const T *)A.grad_out + ((b * A.T + at) * A.heads + head) * A.V, g_stride, A.V,
-                                                           n - at, skip, acc_v, sees);
-            add_not_finite<X, D, N, kWindowThreads, true>(lane, queries + half * SIZE, (const T *)A.q + b * A.qs[0] + head * A.qs[2] + at * A.qs[1], A.qs[1], A.K,
-                                                          n - at, skip, acc_k, sees);
+            if (!second && !skip) weigh_values(at, 0, 0);
+            __syncthreads();
+            if (second && !skip) weigh_keys(at, 0, 0);
+            leave_finite<E, D, N, kKeyThreads>(queries);
+            leave_finite<E, D, N, kKeyThreads>(upstream);
+            if (!second && !skip) product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, upstream, weights, acc, A.V);
+            if (second && !skip) product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, queries, weights, acc, A.K);
+            add_not_finite<X, D, N, kKeyThreads, false>(lane, upstream, (const T *)A.grad_out + ((b * A.T + at) * A.heads + head) * A.V, g_stride, A.V, n - at,
+                                                        skip || second, acc, [&](int r) { return sees(at + r); });
+            add_not_finite<X, D, N, kKeyThreads, true>(lane, queries, (const T *)A.q + b * A.qs[0] + head * A.qs[2] + at * A.qs[1], A.qs[1], A.K, n - at,
+                                                       skip || !second, acc, [&](int r) { return sees(at + r); });
         }
     }
-    const float k_scale = A.scale * scale.back(), v_scale = 1.0f / LIFT;
-    if (there && parts == 1) {
-        store_line<X, D>(out_k + line * k_stride, A.K, lane, acc_k, k_scale);
-        store_line<X, D>(out_v + line * v_stride, A.V, lane, acc_v, v_scale);
-    } else if (there) {
-        float *to = A.parts + (((head_line * A.front + tile) * parts + part) * ROWS + (line - lo)) * (A.K + A.V);
-        store_line<X, D>(to, A.K, lane, acc_k, k_scale);
-        store_line<X, D>(to + A.K, A.V, lane, acc_v, v_scale);
+    const float own_scale = second ? A.scale * scale.back() : 1.0f / LIFT;
+    if (there && (parts == 1 || (part == 0 && line >= A.joined))) {
+        if (second) store_line<X, D>(out_k + line * k_stride, A.K, lane, acc, own_scale);
+        else store_line<X, D>(out_v + line * v_stride, A.V, lane, acc, own_scale);
+    } else if (there && line < A.joined) {
+        float *to = A.sums + (((head_line * A.cut + tile) * parts + part) * ROWS + (line - lo)) * (A.K + A.V);
+        if (second) store_line<X, D>(to, A.K, lane, acc, own_scale);
+        else store_line<X, D>(to + A.K, A.V, lane, acc, own_scale);
     }
     if (hi < end && zeros) {
-        zero_rows(out_k, k_stride, A.K, hi, end);
-        zero_rows(out_v, v_stride, A.V, hi, end);
+        zero_rows<kKeyThreads>(out_k, k_stride, A.K, hi, end);
+        zero_rows<kKeyThreads>(out_v, v_stride, A.V, hi, end);
     }
 }
 
-// The sum of the front tiles' parts, in their order: a key a workgroup
+// The sums of cut tiles' parts, in their order: some tokens a workgroup, `lanes` threads (a power of two) each
 template <typename T, int ROWS>
-__global__ __launch_bounds__(kWindowThreads) void sig_window_join_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads) void sig_window_join_kernel(WindowArgs A, int lanes)
 {
-    const int shared_heads = A.heads / A.group, keys = A.front * ROWS;
-    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, head_line = id / keys;
-    const int key = (int)(id % keys);
+    const int shared_heads = A.heads / A.group, width = A.K + A.V;
+    const int64_t id = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kWindowThreads / lanes) + threadIdx.x / lanes, head_line = id / A.joined;
+    const int key = (int)(id % A.joined);
     if (head_line >= A.B * shared_heads) return;
     const int64_t b = head_line / shared_heads, n = A.lengths ? A.lengths[b] : A.T;
     if (key >= n || key >= A.T) return;      // (those are zero by now)
-    const float *parts = A.parts + ((head_line * A.front + key / ROWS) * A.front_parts * ROWS + key % ROWS) * (A.K + A.V);
-    for (int c = threadIdx.x; c < A.K + A.V; c += kWindowThreads) {
+    const float *sums = A.sums + ((head_line * A.cut + key / ROWS) * A.parts * ROWS + key % ROWS) * width;
+    for (int c = threadIdx.x % lanes; c < width; c += lanes) {
         float sum = 0.0f;
 #pragma unroll 8
-        for (int i = 0; i < A.front_parts; ++i) sum += parts[(int64_t)i * ROWS * (A.K + A.V) + c];
+        for (int i = 0; i < A.parts; ++i) sum += sums[(int64_t)i * ROWS * width + c];
         const int64_t row = (b * A.T + key) * shared_heads + head_line % shared_heads;
         if (c < A.K) ((T *)A.grad_k)[row * A.K + c] = from_float<T>(sum);
         else ((T *)A.grad_v)[row * A.V + c - A.K] = from_float<T>(sum);
@@ -653,7 +696,7 @@ inline int window_rows(int type, int dim) { return type == SIG_F32 || dim > 128 
 
 inline dim3 window_grid(int64_t blocks)
 {
-    const int64_t across = ((int64_t)1 << 32) / kWindowThreads - 1;      // (a launch holds fewer than 2^32 threads along an axis)
+    const int64_t across = ((int64_t)1 << 32) / (2 * kWindowThreads) - 1;      // (a launch holds fewer than 2^32 threads along an axis)
     return dim3((unsigned)(blocks < across ? blocks : across), (unsigned)((blocks + across - 1) / across));
 }
 
@@ -667,22 +710,29 @@ hipError_t launch_window(const WindowArgs &A, WindowPass pass, hipStream_t st)
         constexpr int D = decltype(d)::value, BYTES = D * (int)sizeof(T), ROWS = kWindowWaves * X::M;
         constexpr bool WHOLE = decltype(whole)::value;
         // tokens of a tile
-        constexpr int N = BYTES > 512 ? 16 : BYTES > WINDOW_WIDE ? 32 : 64, QUERY = BYTES > 512 ? 16 : BYTES > WINDOW_QUERY_WIDE ? 32 : 64, KEY = BYTES > 512 ? 16 : 32;
+        constexpr int N = BYTES > 512 ? 16 : sizeof(T) == 4 || BYTES > (WHOLE ? 256 : 128) ? 32 : 64, QUERY = BYTES > 512 ? 16 : BYTES > 128 ? 32 : 64, KEY = BYTES > 512 ? 16 : BYTES > 128 ? 32 : 64;
         if (pass == WINDOW_FORWARD) {
             sig_window_forward_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
         } else if (pass == WINDOW_QUERY_GRADIENT) {
             sig_window_query_gradient_kernel<T, X, D, QUERY, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
         } else {
-            const int64_t pieces = A.front * A.front_parts + A.tiles - A.front;
-            sig_window_key_gradient_kernel<T, X, D, KEY, WHOLE><<<window_grid(shared * pieces), kWindowThreads, 0, st>>>(A);
-            if (A.front && A.front_parts > 1) sig_window_join_kernel<T, ROWS><<<window_grid(shared * A.front * ROWS), kWindowThreads, 0, st>>>(A);
+            const int64_t pieces = A.cut * A.parts + A.tiles - A.cut;
+            sig_window_key_gradient_kernel<T, X, D, KEY, WHOLE><<<window_grid(shared * pieces), kKeyThreads, 0, st>>>(A);
+            if (A.parts > 1) {
+                int lanes = 64;
+                while (lanes < A.K + A.V && lanes < kWindowThreads) lanes *= 2;
+                const int at_once = kWindowThreads / lanes;
+                sig_window_join_kernel<T, ROWS><<<window_grid((shared * A.joined + at_once - 1) / at_once), kWindowThreads, 0, st>>>(A, lanes);
+            }
         }
     };
     auto with = [&](auto x, auto d) {
         if (A.K == decltype(d)::value && A.V == A.K) go(x, d, std::true_type());
         else go(x, d, std::false_type());
     };
-    if (dim <= 64) with(Tag<Tiles<T>>(), std::integral_constant<int, 64>());
+    if (dim <= 32) with(Tag<Tiles<T>>(), std::integral_constant<int, 32>());
+    else if (dim <= 64) with(Tag<Tiles<T>>(), std::integral_constant<int, 64>());
+    else if (dim <= 96) with(Tag<Tiles<T>>(), std::integral_constant<int, 96>());
     else if (dim <= 128) with(Tag<Tiles<T>>(), std::integral_constant<int, 128>());
     else with(Tag<SmallTiles<T>>(), std::integral_constant<int, 256>());
     return hipGetLastError();

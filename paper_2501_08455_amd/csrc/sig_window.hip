@@ -9,7 +9,9 @@ namespace {
 
 constexpr int kMostDim = 256;
 constexpr double kLog2E = 1.4426950408889634;
-constexpr int kMostParts = 64;      // of the first tokens' queries
+constexpr int kMostParts = 64;      // of a tile's queries
+
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 int check(const sig_ctx *ctx, const sig_window_t *s)
 {
@@ -88,20 +90,28 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
     A.grad_q = grad_q;
     A.grad_k = grad_k;
     A.grad_v = grad_v;
-    // The first tokens' tiles are cut where they have more than twice the queries of the others
+    // The first tokens' tiles are cut where they have more than twice the queries of the others; else all tiles, where they are fewer than two a unit,
+    // into as many parts as give four, of 128 queries or more
     const int rows = window_rows(shape->type, A.K > A.V ? A.K : A.V);
-    const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T;
-    A.front_parts = 1;
+    const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T, all = A.B * shape->shared_heads * A.tiles;
+    A.parts = 1;
     if (A.sinks > 0 && A.T > usual) {
-        A.front = (A.sinks + rows - 1) / rows;
-        const int64_t parts = (A.T + usual - 1) / usual;
-        A.front_parts = (int)(parts < kMostParts ? parts : kMostParts);
+        A.cut = (A.sinks + rows - 1) / rows;
+        A.joined = A.sinks;
+        A.parts = (int)least(1 + (A.T + usual - 1) / usual, kMostParts);
+    } else if (all < 2 * ctx->num_cu) {
+        A.parts = (int)least((4 * ctx->num_cu + all - 1) / all, least(kMostParts, (least(A.T, (int64_t)A.window + rows) * A.group + 127) / 128));
+        if (A.parts > 1) {
+            A.cut = A.tiles;
+            A.joined = A.T;
+            A.even = 1;
+        }
     }
-    const int64_t joined = A.front * A.front_parts * (int64_t)rows * (A.K + A.V) * A.B * shape->shared_heads;
+    const int64_t joined = A.cut * A.parts * (int64_t)rows * (A.K + A.V) * A.B * shape->shared_heads;
     Scratch scratch;
     rc = scratch.get(ctx, (size_t)(deltas + joined) * sizeof(float), st, &A.delta);
     if (rc != SIG_OK) return rc;
-    A.parts = A.delta + deltas;
+    A.sums = A.delta + deltas;
     hipError_t e = launch(A, shape->type, WINDOW_QUERY_GRADIENT, st);
     if (e == hipSuccess) e = launch(A, shape->type, WINDOW_KEY_GRADIENT, st);
     return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;
