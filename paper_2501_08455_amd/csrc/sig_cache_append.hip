@@ -2,7 +2,8 @@
 //
 // Bound by memory: each value is read and written once.  A workgroup takes a few tokens, works out their cosines and sines once for all
 // heads, in LDS, and walks over the lines (a token's head of q, k or v), several loads in flight a thread.  Into pages of 8 bits: a workgroup
-// takes a page's tokens of one head, since they share a scale, which is known when all of them have been read; they are read twice.
+// takes a page's tokens of one head, since they share a scale, which is known when all of them have been read; more than a thread's worth each are
+// read twice.
 #include <type_traits>
 
 #include "sig_cache.h"
@@ -91,24 +92,61 @@ __device__ void turn_unit(float *low, float *high, const float2 *angles, int at)
     }
 }
 
+// N values on their way, as the words that hold them where they are whole words
+template <typename T, int N>
+using Held = std::conditional_t<(N * sizeof(T) >= 4), Words<T, (N * sizeof(T) >= 4 ? N : 4)>, Pack<T, N>>;
+
+template <typename T, int N>
+__device__ inline Held<T, N> load_held(const T *from)
+{
+    return __builtin_bit_cast(Held<T, N>, load_pack<T, N>(from));
+}
+
+template <typename T, int N>
+__device__ inline void floats_of(const Held<T, N> &held, float *x)
+{
+    const auto values = __builtin_bit_cast(Pack<T, N>, held);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = to_float(values.v[j]);
+}
+
+template <typename T, int N>
+__device__ inline void store_floats(T *to, const float *x)
+{
+    Pack<T, N> values;
+#pragma unroll
+    for (int j = 0; j < N; ++j) values.v[j] = from_float<T>(x[j]);
+    store_pack(to, values);
+}
+
 // Whole tokens: all lines of q, and those of k and v where the cache has their type
 template <typename T, int N, bool INTERLEAVED, bool WIDE>
 __device__ void append_tokens(const AppendArgs &A, int64_t block, float2 *table)
 {
     constexpr int AT_ONCE = 4;
     constexpr int M = kGroup<T>;
-    __shared__ int64_t key_at[kMostTokens], value_at[kMostTokens];      // -1: not there
-    __shared__ int live[kMostTokens];
+    struct Token {
+        int64_t from[3], to[3];      // of q, k and v: in values, the first head's
+        int live, written;           // whether the token is there, and its place has a page
+    };
+    __shared__ Token of[kMostTokens];
     const int half = A.turned / 2, G = WIDE ? A.cache.heads : 0, lines = A.heads + 2 * G;
     const int64_t first = block * A.tokens, all = A.B * A.T;
     const int tokens = all - first < A.tokens ? (int)(all - first) : A.tokens;
     for (int i = threadIdx.x; i < tokens * half || i < tokens; i += kThreads) {
         if (i < tokens) {
             const int64_t b = (first + i) / A.T, t = (first + i) % A.T, place = held_by(A, b) + t;
-            live[i] = t < new_of(A, b);
-            const int64_t page = live[i] ? A.cache.page_of(b, place / A.cache.page_tokens) : -1, slot = place % A.cache.page_tokens;
-            key_at[i] = page < 0 ? -1 : page * A.cache.keys.page + slot * A.cache.keys.slot;
-            value_at[i] = page < 0 ? -1 : page * A.cache.values.page + slot * A.cache.values.slot;
+            Token token;
+            token.live = t < new_of(A, b);
+            const int64_t page = WIDE && token.live ? A.cache.page_of(b, place / A.cache.page_tokens) : -1, slot = place % A.cache.page_tokens;
+            token.written = page >= 0;
+            token.from[0] = b * A.qs[0] + t * A.qs[1];
+            token.from[1] = b * A.ks[0] + t * A.ks[1];
+            token.from[2] = b * A.vs[0] + t * A.vs[1];
+            token.to[0] = (first + i) * A.heads * A.cache.K;
+            token.to[1] = page * A.cache.keys.page + slot * A.cache.keys.slot;
+            token.to[2] = page * A.cache.values.page + slot * A.cache.values.slot;
+            of[i] = token;
         }
         if (i < tokens * half) {
             const int64_t b = (first + i / half) / A.T, t = (first + i / half) % A.T;
@@ -119,74 +157,73 @@ __device__ void append_tokens(const AppendArgs &A, int64_t block, float2 *table)
     }
     __syncthreads();
     const Line<T, N, INTERLEAVED> turned_line = {A.cache.K, A.turned}, copied_line = {A.cache.V, 0};
-    const int most = max(turned_line.units(), G ? copied_line.units() : 0), apart = kThreads / A.places, count = tokens * lines;
+    const int turned_units = turned_line.units(), copied_units = copied_line.units(), most = max(turned_units, G ? copied_units : 0);
+    const int apart = kThreads / A.places, token_step = apart / lines, line_step = apart % lines;
     for (int unit = threadIdx.x % A.places; unit < most; unit += A.places) {
-        for (int from = threadIdx.x / A.places; from < count; from += AT_ONCE * apart) {
-            Pack<T, M> same[AT_ONCE];
-            Pack<T, N> low[AT_ONCE], high[AT_ONCE];
+        const int turned_at = turned_line.at(unit), copied_at = copied_line.at(unit);
+        // what the unit is in lines of q and k: 1 turned, 2 copied, 3 fewer than a unit, 0 nothing; and of v: 2, 3, 0
+        const int turned_what = unit >= turned_units ? 0 : !turned_line.copied(unit) ? 1 : turned_line.few() ? 3 : 2;
+        const int copied_what = unit >= copied_units ? 0 : copied_line.few() ? 3 : 2;
+        int token = threadIdx.x / A.places / lines, line = threadIdx.x / A.places % lines;
+        while (token < tokens) {
+            Held<T, M> same[AT_ONCE];
+            Held<T, N> low[AT_ONCE], high[AT_ONCE];
             const T *source[AT_ONCE];
             T *to[AT_ONCE];
-            int token[AT_ONCE], what[AT_ONCE];      // 0: zeros, 1: turned, 2: copied, 3: copied, fewer than a unit, -1: nothing
+            int tokens_of[AT_ONCE], what[AT_ONCE], widths[AT_ONCE];
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
-                what[i] = -1;
-                const int line = from + i * apart;
-                if (line >= count) continue;
-                token[i] = line / lines;
-                int head = line % lines;
-                const int64_t b = (first + token[i]) / A.T, t = (first + token[i]) % A.T;
-                const bool is_value = head >= A.heads + G;
-                const Line<T, N, INTERLEAVED> &shape = is_value ? copied_line : turned_line;
-                if (unit >= shape.units()) continue;
-                const int at = shape.at(unit);
-                if (head < A.heads) {
-                    source[i] = (const T *)A.q + b * A.qs[0] + t * A.qs[1] + head * A.qs[2] + at;
-                    to[i] = (T *)A.q_out + ((first + token[i]) * A.heads + head) * A.cache.K + at;
-                } else {
-                    head -= A.heads;
-                    if (is_value) head -= G;
-                    const int64_t place = is_value ? value_at[token[i]] : key_at[token[i]];
-                    if (place < 0) continue;
-                    source[i] = is_value ? (const T *)A.v + b * A.vs[0] + t * A.vs[1] + head * A.vs[2] + at
-                                         : (const T *)A.k + b * A.ks[0] + t * A.ks[1] + head * A.ks[2] + at;
-                    to[i] = is_value ? (T *)A.cache.values.values + place + head * A.cache.values.head + at
-                                     : (T *)A.cache.keys.values + place + head * A.cache.keys.head + at;
+                what[i] = 0;
+                tokens_of[i] = token;
+                if (token < tokens) {
+                    const Token &its = of[token];
+                    const bool is_query = line < A.heads, is_value = line >= A.heads + G;
+                    const int head = is_query ? line : is_value ? line - A.heads - G : line - A.heads;
+                    what[i] = is_value ? copied_what : turned_what;
+                    if (!is_query && !its.written) what[i] = 0;
+                    const int at = is_value ? copied_at : turned_at;
+                    widths[i] = is_value ? A.cache.V : A.cache.K - A.turned;
+                    source[i] = (is_query ? (const T *)A.q + its.from[0] + head * A.qs[2] : is_value ? (const T *)A.v + its.from[2] + head * A.vs[2]
+                                                                                                    : (const T *)A.k + its.from[1] + head * A.ks[2]) + at;
+                    to[i] = (is_query ? (T *)A.q_out + its.to[0] + (int64_t)head * A.cache.K : is_value ? (T *)A.cache.values.values + its.to[2] + head * A.cache.values.head
+                                                                                                      : (T *)A.cache.keys.values + its.to[1] + head * A.cache.keys.head) + at;
+                    if (its.live) {
+                        if (what[i] == 2) same[i] = load_held<T, M>(source[i]);
+                        if (what[i] == 1) {
+                            low[i] = load_held<T, N>(source[i]);
+                            if (!INTERLEAVED) high[i] = load_held<T, N>(source[i] + half);
+                        }
+                    } else {
+                        what[i] = -what[i];      // (zeros)
+                    }
                 }
-                const bool copied = shape.copied(unit), few = copied && shape.few();
-                what[i] = few ? 3 : copied ? 2 : 1;
-                if (!live[token[i]]) continue;
-                if (copied && !few) same[i] = load_pack<T, M>(source[i]);
-                if (!copied) {
-                    low[i] = load_pack<T, N>(source[i]);
-                    if (!INTERLEAVED) high[i] = load_pack<T, N>(source[i] + half);
+                token += token_step;
+                line += line_step;
+                if (line >= lines) {
+                    line -= lines;
+                    ++token;
                 }
             }
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
-                if (what[i] < 0) continue;
-                const bool there = live[token[i]];
                 if (what[i] == 1) {
                     float a[N], b[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        a[j] = there ? to_float(low[i].v[j]) : 0.0f;
-                        b[j] = there && !INTERLEAVED ? to_float(high[i].v[j]) : 0.0f;
-                    }
-                    turn_unit<T, N, INTERLEAVED>(a, b, table + token[i] * half, turned_line.at(unit));
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        low[i].v[j] = from_float<T>(there ? a[j] : 0.0f);
-                        high[i].v[j] = from_float<T>(there ? b[j] : 0.0f);
-                    }
-                    store_pack(to[i], low[i]);
-                    if (!INTERLEAVED) store_pack(to[i] + half, high[i]);
+                    floats_of<T, N>(low[i], a);
+                    if (!INTERLEAVED) floats_of<T, N>(high[i], b);
+                    turn_unit<T, N, INTERLEAVED>(a, b, table + tokens_of[i] * half, turned_at);
+                    store_floats<T, N>(to[i], a);
+                    if (!INTERLEAVED) store_floats<T, N>(to[i] + half, b);
                 } else if (what[i] == 2) {
-#pragma unroll
-                    for (int j = 0; j < M; ++j) same[i].v[j] = there ? same[i].v[j] : from_float<T>(0.0f);
-                    store_pack(to[i], same[i]);
-                } else {
-                    const int line = (from + i * apart) % lines, n = line >= A.heads + G ? A.cache.V : A.cache.K - A.turned;
-                    for (int j = 0; j < n; ++j) to[i][j] = there ? source[i][j] : from_float<T>(0.0f);
+                    store_pack(to[i], __builtin_bit_cast(Pack<T, M>, same[i]));
+                } else if (what[i] == -1) {
+                    const float none[N] = {};
+                    store_floats<T, N>(to[i], none);
+                    if (!INTERLEAVED) store_floats<T, N>(to[i] + half, none);
+                } else if (what[i] == -2) {
+                    const float none[M] = {};
+                    store_floats<T, M>(to[i], none);
+                } else if (what[i] != 0) {
+                    for (int j = 0; j < widths[i]; ++j) to[i][j] = what[i] > 0 ? source[i][j] : from_float<T>(0.0f);
                 }
             }
         }
@@ -224,20 +261,23 @@ __device__ void append_page(const AppendArgs &A, int64_t block, float2 *table)
     const int64_t source_stride = is_value ? A.vs[1] : A.ks[1];
     Narrow *to = (Narrow *)pages.values + page * pages.page + head * pages.head;
     const int at_once = half ? min(tokens, kTable / half) : tokens;      // tokens whose angles the table holds
+    // the cosines and sines of n tokens
+    auto angles = [&](int first, int n) {
+        if (!half) return;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n * half; i += kThreads) {
+            const int64_t t = t0 + first + i / half;
+            float c, s;
+            turn(position_of(A, b, t, held + t), A.frequencies[i % half], &c, &s);
+            table[i] = make_float2(A.scale * c, A.scale * s);
+        }
+        __syncthreads();
+    };
     // f(token, component, values, count) of all values as they are before they are rounded
     auto each = [&](auto f, bool again) {
         for (int first = 0; first < tokens; first += at_once) {
             const int n = min(at_once, tokens - first);
-            if (half && !(again && at_once == tokens)) {
-                __syncthreads();
-                for (int i = threadIdx.x; i < n * half; i += kThreads) {
-                    const int64_t t = t0 + first + i / half;
-                    float c, s;
-                    turn(position_of(A, b, t, held + t), A.frequencies[i % half], &c, &s);
-                    table[i] = make_float2(A.scale * c, A.scale * s);
-                }
-                __syncthreads();
-            }
+            if (!(again && at_once == tokens)) angles(first, n);
             for (int i = threadIdx.x; i < n * units; i += kThreads) {
                 const int token = first + i / units, unit = i % units, at = shape.at(unit);
                 const T *p = source + token * source_stride + at;
@@ -269,18 +309,47 @@ __device__ void append_page(const AppendArgs &A, int64_t block, float2 *table)
             }
         }
     };
+    // (a value of each thread: it stays where it is until the scale is known)
+    const bool one = tokens * units <= kThreads && at_once == tokens;
+    const int own_token = threadIdx.x / units, own_unit = threadIdx.x % units, own_at = shape.at(own_unit);
+    const int own = !one || own_token >= tokens ? 0 : !shape.copied(own_unit) ? 1 : shape.few() ? 3 : 2;
+    float x[M > N ? M : N] = {}, y[N] = {};
     float most = 0.0f;
-    each([&](int, int, const float *x, auto n) {
+    auto larger = [&](const float *values, int n) {
 #pragma unroll
-        for (int j = 0; j < decltype(n)::value; ++j) {
-            const float size = fabsf(x[j]);
+        for (int j = 0; j < n; ++j) {
+            const float size = fabsf(values[j]);
             most = size <= 3.4028234663852886e38f ? fmaxf(most, size) : most;
         }
-    }, false);
+    };
+    const float before = pages.scales[page * A.cache.heads + head];
+    if (one) {
+        const T *p = source + own_token * source_stride + own_at;
+        Held<T, N> low, high;
+        if (own == 1) {
+            low = load_held<T, N>(p);
+            if (!INTERLEAVED) high = load_held<T, N>(p + half);
+        } else if (own == 2) {
+            floats_of<T, M>(load_held<T, M>(p), x);
+        } else if (own == 3) {
+            for (int j = 0; j < shape.dim - shape.turned; ++j) most = fabsf(to_float(p[j])) <= 3.4028234663852886e38f ? fmaxf(most, fabsf(to_float(p[j]))) : most;
+        }
+        angles(0, tokens);
+        if (own == 1) {
+            floats_of<T, N>(low, x);
+            if (!INTERLEAVED) floats_of<T, N>(high, y);
+            turn_unit<T, N, INTERLEAVED>(x, y, table + own_token * half, own_at);
+            larger(x, N);
+            if (!INTERLEAVED) larger(y, N);
+        } else if (own == 2) {
+            larger(x, M);
+        }
+    } else {
+        each([&](int, int, const float *values, auto n) { larger(values, decltype(n)::value); }, false);
+    }
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) most = fmaxf(most, __shfl_xor(most, i));
     if (threadIdx.x % 64 == 0) mosts[threadIdx.x / 64] = most;
-    const float before = pages.scales[page * A.cache.heads + head];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) most = fmaxf(most, mosts[i]);
@@ -294,13 +363,27 @@ __device__ void append_page(const AppendArgs &A, int64_t block, float2 *table)
         }
     }
     if (threadIdx.x == 0) pages.scales[page * A.cache.heads + head] = scale;
-    each([&](int token, int at, const float *x, auto n) {
+    auto put = [&](int token, int at, const float *values, auto n) {
         constexpr int COUNT = decltype(n)::value;
-        Pack<Narrow, COUNT> values;
+        Pack<Narrow, COUNT> narrow;
 #pragma unroll
-        for (int j = 0; j < COUNT; ++j) values.v[j] = to_narrow(x[j] * inverse);
-        store_pack(to + (slot + token) * pages.slot + at, values);
-    }, true);
+        for (int j = 0; j < COUNT; ++j) narrow.v[j] = to_narrow(values[j] * inverse);
+        store_pack(to + (slot + token) * pages.slot + at, narrow);
+    };
+    if (!one) {
+        each(put, true);
+    } else if (own == 1) {
+        put(own_token, own_at, x, std::integral_constant<int, N>());
+        if (!INTERLEAVED) put(own_token, own_at + half, y, std::integral_constant<int, N>());
+    } else if (own == 2) {
+        put(own_token, own_at, x, std::integral_constant<int, M>());
+    } else if (own == 3) {
+        const T *p = source + own_token * source_stride + own_at;
+        for (int j = 0; j < shape.dim - shape.turned; ++j) {
+            const float value = to_float(p[j]);
+            put(own_token, own_at + j, &value, std::integral_constant<int, 1>());
+        }
+    }
 }
 
 template <typename T, int N, bool INTERLEAVED, bool NARROW>

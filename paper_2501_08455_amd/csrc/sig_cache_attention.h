@@ -99,6 +99,7 @@ __device__ inline Row row_values(Row got, int at, int dim)
 {
     constexpr int COUNT = 16 / sizeof(C), BITS = 8 * sizeof(C);
     if constexpr (WHOLE) return got;
+    asm volatile("" : "+s"(dim));      // (compared anew: the answers would be kept in registers)
     const int over = at + COUNT - dim;
     if (dim % COUNT && over > 0 && over < COUNT) got = __builtin_bit_cast(Row, __builtin_bit_cast(unsigned __int128, got) >> (over * BITS));
     return over >= COUNT ? Row{} : got;
@@ -225,6 +226,7 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? C
             const C *row = (const C *)A.cache.keys.values + __shfl(key_row, t * M + column);
 #pragma unroll
             for (int i = 0; i < KEY_LOADS; ++i) keys[t][i] = row_load<C, WHOLE>(row, i * 4 * LOAD + lane / 16 * LOAD, K);
+            if (!WHOLE) __builtin_amdgcn_sched_barrier(0);
         }
     };
     auto load_values = [&] {
@@ -232,6 +234,7 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? C
         for (int i = 0; i < VALUE_LOADS; ++i) {
             const C *row = (const C *)A.cache.values.values + __shfl(value_row, (lane + i * 64) / ROW_LOADS);
             held[i] = row_load<C, WHOLE>(row, (lane + i * 64) % ROW_LOADS * LOAD, V);
+            if (!WHOLE && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -266,6 +269,7 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? C
 #pragma unroll
                     for (int part = 0; part < QUERY_PARTS; ++part) s[t] = X::multiply(more, q[part][i * OPERANDS + 1], s[t]);
                 }
+                if (!WHOLE) __builtin_amdgcn_sched_barrier(0);      // (else all operands are made first, and more registers asked for than there are)
             }
         // (the next block's loads go out as soon as there is room for them, so that some are always on their way)
         const uint64_t existed = existing;
