@@ -129,7 +129,8 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
  * 16-bit operands are multiplied as they are, and the probabilities (before they are divided by their sum) rounded to that type for their product
  * with v; sums are float32's.  What a token does not see may be anything, NaN and infinities too; what is not finite spoils the tokens that see it.
  * Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); a scale that is not finite is SIG_ERR_INVALID; 2^31 - 1024 tokens or more, 2^31 heads
- * (B * heads) or more, or 2^39 tokens of heads, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  No context scratch.
+ * (B * heads) or more, 2^39 tokens of heads, or 2^30 groups of 16 tokens in the heads that
+ * share one, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  No context scratch.
  */
 typedef struct sig_window_t {
     int64_t B, T;
@@ -149,8 +150,8 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  *   grad_out     DEVICE, [B][T][heads][value_dim] of `type`, contiguous; what stands behind the lengths is not read
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
- * Context scratch of B * heads * T floats; and where sequences are much longer than the window, for the sinks' gradients in up to 64 parts, or where keys are few, for
- * all of them in up to 64 parts (some four of 64 or 128 keys for each compute unit): key_dim + value_dim floats for each key and part.
+ * Context scratch of B * heads * T floats; and where sequences are much longer than the window, for the sinks' gradients in up to 64 parts (16 of 64 or 128 keys for each
+ * compute unit at most), or where keys are few, for all of them (some four for each unit): key_dim + value_dim floats for each key and part.
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
                                   const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
@@ -186,7 +187,7 @@ typedef struct sig_cache_t {
  *   counts       DEVICE, int64 [B], new tokens of each sequence (taken into 0 ... T); NULL: T.  Those behind them are not read; their queries
  *                give zeros
  *   positions    DEVICE, of `position_type`, position_strides[2] values apart between sequences and tokens; NULL: the places
- *   frequencies  DEVICE, float64 [turned / 2]; turned, interleaved, scale: see sig_rotary.  turned == 0 and scale == 1 leave keys as they are
+ *   frequencies  DEVICE, float64 [turned / 2]; turned, interleaved, scale: see sig_rotary.  turned == 0 leaves keys as they are
  * The cache's type is `type`, or SIG_E4M3.  Then a page's scale is the smallest power of two (2^-126 or more) that is at least the largest
  * magnitude / 448 of what it holds of a head (1 for zeros), and never less than it was while the page keeps earlier tokens: a page
  * whose slot 0 is written by the call keeps none, what another one holds is rounded anew when its scale grows (which changes only values below 2^-6 of

@@ -230,12 +230,14 @@ __device__ void append_tokens(const AppendArgs &A, int64_t block, float2 *table)
     }
 }
 
+constexpr float kLeastScale = 0x1p-126f;
+
 // the smallest power of two, 2^-126 at least, that is no less than most / 448
 __device__ inline float narrow_scale(float most)
 {
     const float ratio = most / kMostNarrow;
     const unsigned bits = __builtin_bit_cast(unsigned, ratio);
-    if (ratio <= 1.1754943508222875e-38f) return 1.1754943508222875e-38f;
+    if (ratio <= kLeastScale) return kLeastScale;
     return __builtin_bit_cast(float, (bits + 0x7fffffu) & 0x7f800000u);
 }
 
@@ -354,7 +356,7 @@ __device__ void append_page(const AppendArgs &A, int64_t block, float2 *table)
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) most = fmaxf(most, mosts[i]);
     // (slot 0: the page keeps nothing from before)
-    const float need = most > 0.0f ? narrow_scale(most) : slot == 0 ? 1.0f : 0.0f, scale = slot == 0 ? need : fmaxf(need, before), inverse = 1.0f / scale;
+    const float need = most > 0.0f ? narrow_scale(most) : slot == 0 ? 1.0f : kLeastScale, scale = slot == 0 ? need : fmaxf(need, before), inverse = 1.0f / scale;
     if (slot > 0 && scale > before) {
         const float shrink = before * inverse;
         for (int i = threadIdx.x; i < slot * shape.dim; i += kThreads) {

@@ -20,9 +20,6 @@ namespace sig {
 constexpr int kCacheThreads = 256, kCacheWaves = kCacheThreads / 64;
 constexpr int kQueries = 16;      // of a workgroup
 constexpr int kMostSplits = 1024;      // (a workgroup's queries times their parts are at most that)
-#ifndef CACHE_WAVES
-#define CACHE_WAVES 2
-#endif
 
 // 0 ... 2^31 - 1 over a divisor, as a product
 struct Quotient {
@@ -127,7 +124,7 @@ __device__ inline typename X::Frag operand(Row got)
 // T: of q and out; C: of the cache in memory (Narrow: 8 bits); X: of the products; PARTS: of X's type that hold one of q's or a probability; WHOLE: keys
 // and values have D components
 template <typename T, typename C, typename X, int D, int QUERY_PARTS, int PARTS, bool WHOLE>
-__global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? CACHE_WAVES : 1) void sig_cache_attention_kernel(CacheAttentionArgs A)
+__global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2 : 1) void sig_cache_attention_kernel(CacheAttentionArgs A)
 {
     using E = typename X::E;
     using Tile = LdsTile<E, D>;
@@ -562,7 +559,7 @@ hipError_t launch_cache_attention(const CacheAttentionArgs &A, bool narrow, hipS
         constexpr int N = decltype(n)::value;
         int columns = 1, turns = 1, slices = 1;
         while (columns * N < A.cache.V) columns *= 2;
-        // (many parts of few queries: eight columns a workgroup, 256 parts of 16 queries 20 -> us)
+        // (many parts of few queries: eight columns a workgroup, 256 parts of 16 queries 20 -> 10 us)
         for (; A.splits >= 64 && columns > 8; columns /= 2) slices *= 2;
         while (turns < A.splits && columns * turns < kCacheThreads) turns *= 2;
         const int at_once = kCacheThreads / (columns * turns);

@@ -602,6 +602,12 @@ at::Tensor cache_append(const at::Tensor &k_, const at::Tensor &v_, const at::Te
     }
     shape.interleaved = interleaved;
     shape.scale = scale;
+    for (const at::Tensor &written : {keys, values, cache.key_scales, cache.value_scales})
+        for (const auto &[t, name] : {std::pair<const at::Tensor &, const char *>{k, "k"}, {v, "v"}, {q, "q"}}) {
+            if (!written.defined() || !t.defined() || written.numel() == 0 || t.numel() == 0) continue;
+            const auto x = span_of(t), y = span_of(written);
+            if (x.first < y.second && y.first < x.second) refuse(std::string(name) + " must lie apart from the cache");
+        }
     std::optional<RotaryPlace> place;
     if (frequencies_.defined()) {
         // (places, where positions are not given, are not a tensor of the call)

@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
 // Own lines are keys; queries and upstream gradients of all heads that share them come as tiles, one head after the other, so that the sum over these
 // heads is one of registers.  Two wavefronts, on the same matrix unit, share M keys: the first holds the keys, works out p and adds up grad v; the second holds the
 // values, takes p from LDS a tile later, and adds up grad k.  Each has half of the registers' load, and one multiplies while the other one
-// does not (both gradients in one wavefront, one a unit: 1,510 us where this takes ; 8 x 4,096 tokens, 16 heads of 128 bfloat16, window 1,024).  Few
+// does not (both gradients in one wavefront, one a unit: 1,510 us where this takes 1,190; 8 x 4,096 tokens, 16 heads of 128 bfloat16, window 1,024).  Few
 // tiles, and those of the first tokens, which every query sees, are cut into parts along the queries, and joined from scratch.
 constexpr int kKeyThreads = 2 * kWindowThreads;
 

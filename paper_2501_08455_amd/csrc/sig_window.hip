@@ -10,6 +10,7 @@ namespace {
 constexpr int kMostDim = 256;
 constexpr double kLog2E = 1.4426950408889634;
 constexpr int kMostParts = 64;      // of a tile's queries
+constexpr int kMostCut = 16;        // workgroups a unit that the first tokens' tiles are cut into
 
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
@@ -21,6 +22,8 @@ int check(const sig_ctx *ctx, const sig_window_t *s)
     if (s->key_dim > kMostDim || s->value_dim > kMostDim) return SIG_ERR_UNSUPPORTED;
     // (a grid of 2^24 x 2^15 workgroups of 64 tokens or more)
     if (s->T >= INT32_MAX - 1023 || s->B > INT32_MAX / s->heads || (s->T > 0 && s->B * s->heads > ((int64_t)1 << 39) / (s->T + 127))) return SIG_ERR_TOO_LARGE;
+    // (tiles of 16 queries or more, of all heads that share a key, are counted in 32 bits)
+    if ((s->T + 15) / 16 * (s->heads / s->shared_heads) >= INT32_MAX / 2) return SIG_ERR_TOO_LARGE;
     return SIG_OK;
 }
 
@@ -90,15 +93,19 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
     A.grad_q = grad_q;
     A.grad_k = grad_k;
     A.grad_v = grad_v;
-    // The first tokens' tiles are cut where they have more than twice the queries of the others; else all tiles, where they are fewer than two a unit,
-    // into as many parts as give four, of 128 queries or more
+    // The first tokens' tiles are cut where they have more than twice the queries of the others, unless they are so many that they balance by themselves and the parts'
+    // sums would take much memory; else all tiles, where they are fewer than two a unit, into as many parts as give four, of 128 queries or more
     const int rows = window_rows(shape->type, A.K > A.V ? A.K : A.V);
-    const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T, all = A.B * shape->shared_heads * A.tiles;
+    const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T, lines = A.B * shape->shared_heads, all = lines * A.tiles;
     A.parts = 1;
     if (A.sinks > 0 && A.T > usual) {
-        A.cut = (A.sinks + rows - 1) / rows;
-        A.joined = A.sinks;
-        A.parts = (int)least(1 + (A.T + usual - 1) / usual, kMostParts);
+        const int64_t tiles = (A.sinks + rows - 1) / rows;
+        A.parts = (int)least(least(1 + (A.T + usual - 1) / usual, kMostParts), kMostCut * (int64_t)ctx->num_cu / (lines * tiles));
+        if (A.parts < 2) A.parts = 1;
+        if (A.parts > 1) {
+            A.cut = (int)tiles;
+            A.joined = A.sinks;
+        }
     } else if (all < 2 * ctx->num_cu) {
         A.parts = (int)least((4 * ctx->num_cu + all - 1) / all, least(kMostParts, (least(A.T, (int64_t)A.window + rows) * A.group + 127) / 128));
         if (A.parts > 1) {
@@ -107,7 +114,7 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
             A.even = 1;
         }
     }
-    const int64_t joined = A.cut * A.parts * (int64_t)rows * (A.K + A.V) * A.B * shape->shared_heads;
+    const int64_t joined = A.cut * A.parts * (int64_t)rows * (A.K + A.V) * lines;
     Scratch scratch;
     rc = scratch.get(ctx, (size_t)(deltas + joined) * sizeof(float), st, &A.delta);
     if (rc != SIG_OK) return rc;

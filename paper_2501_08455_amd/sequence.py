@@ -58,6 +58,8 @@ class SequenceModel(torch.nn.Module):
 
     A model whose parameters are converted (`model.bfloat16()`, `.half()`) mixes and attends in that type; paths, signatures and states are float32."""
 
+    mixer, window, sinks = "linear", None, 0      # (of models that were pickled without)
+
     def __init__(self, inputs, channels, depth, outputs, heads=4, head_dim=64, turned=None, decays=(0.125, 0.002), device="cuda",
                  mixer="linear", window=None, sinks=0, **positions):
         super().__init__()

@@ -26,7 +26,7 @@ def launches(linked):   # noqa: F811
 
 
 HUGE = [(way, *shape) for way in ("forward", "backward")
-        for shape in (((1 << 31) - 1, 1, 1, 1, 4, 4, BF16, 0, 0), (1, 1 << 30, 1, 1, 8, 8, F32, 100, 0), (1 << 22, 500, 8, 2, 8, 8, F16, 16, 3), (1, 1, (1 << 31) - 1, 1, 4, 4, F32, 0, 0))]
+        for shape in (((1 << 31) - 1, 1, 1, 1, 4, 4, BF16, 0, 0), (1, 1 << 30, 1, 1, 8, 8, F32, 100, 0), (1 << 22, 500, 8, 2, 8, 8, F16, 16, 3), (1, 1, 1 << 29, 1, 4, 4, F32, 0, 0))]
 HUGE += [("append", 1 << 15, (1 << 16) - 1, 1, 1, 2, 2, BF16, cache, 16, 2) for cache in (BF16, E4M3)]
 HUGE += [("append", (1 << 31) - 1, 1, 0, 1, 2, 2, F32, cache, 1, 0) for cache in (F32, E4M3)]
 HUGE += [("attend", (1 << 31) - 1, 1, 1, 1, 4, 4, F32, F32, 16, 100, 0, 0), ("attend", 1, (1 << 31) - 1025, 1, 1, 4, 4, BF16, E4M3, 1 << 30, 2, 0, 0),
@@ -41,7 +41,9 @@ def test_no_launch_is_larger_than_launches_are(launches):
 
 
 def test_what_no_launch_can_hold_is_refused(launches):
-    calls = [("forward", 1 << 20, 1 << 25, 1, 1, 4, 4, F32, 0, 0), ("backward", 1, (1 << 31) - 1024, 1, 1, 4, 4, BF16, 0, 0), ("append", 1 << 16, 1 << 15, 1, 1, 2, 2, F32, F32, 16, 2),
+    calls = [("forward", 1 << 20, 1 << 25, 1, 1, 4, 4, F32, 0, 0), ("backward", 1, (1 << 31) - 1024, 1, 1, 4, 4, BF16, 0, 0),
+             ("forward", 1, 1, (1 << 31) - 1, 1, 4, 4, F32, 0, 0), ("backward", 1, 1 << 20, 1 << 15, 1, 4, 4, F32, 0, 0),
+             ("append", 1 << 16, 1 << 15, 1, 1, 2, 2, F32, F32, 16, 2),
              ("attend", 1 << 16, 1 << 20, 1, 1, 4, 4, F32, F32, 16, 100, 0, 0), ("attend", 1, 1, 1, 1, 4, 4, F32, F32, 1 << 32, 1, 0, 0)]
     for call, (rc, _, got) in zip(calls, launches(calls)):
         assert rc == LARGE and not got, (call, rc)
@@ -61,6 +63,7 @@ CUT = [((4, 2048, 16, 4, 0, 0), (16, 4)),        # fewer than two a unit: four
        ((64, 2048, 16, 4, 0, 0), (0, 1)), ((8, 4096, 16, 16, 1024, 0), (0, 1)),
        ((8, 4096, 16, 16, 1024, 4), (1, 3)),     # the first tokens', whose queries are more than 2 (1,024 + 128)
        ((8, 4096, 16, 16, 1024, 129), (2, 3)), ((8, 2000, 16, 16, 1024, 4), (0, 1)), ((1, 65536, 16, 4, 1024, 4), (1, 30)), ((1, 1 << 20, 16, 4, 1024, 4), (1, 64)),
+       ((256, 4096, 4, 4, 64, 1000), (0, 1)), ((256, 4096, 4, 1, 64, 1000), (8, 2)),      # 16 workgroups a unit at most, for the parts
        ((1, 100, 1, 1, 0, 0), (0, 1)),           # a part has 128 queries or more
        ((1, 300, 2, 2, 20, 0), (3, 2))]
 
