@@ -126,6 +126,8 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
  *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous
  *   stats        DEVICE, float32 [B][heads][T][2], what sig_window_attention_backward needs (the largest z, as a power of two, and one over the
  *                sum of exp(z - largest)); may be NULL.  Nothing is written for the tokens behind the lengths
+ *   rest         DEVICE, a byte for each value of out, which the backward pass needs too: what out's rounding to 16 bits left (8 bits, 5 of exponent,
+ *                times 2^14).  Not used, and may be NULL, with float32 and where stats is NULL
  * 16-bit operands are multiplied as they are, and the probabilities (before they are divided by their sum) rounded to that type for their product
  * with v; sums are float32's.  What a token does not see may be anything, NaN and infinities too; what is not finite spoils the tokens that see it.
  * Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); a scale that is not finite is SIG_ERR_INVALID; 2^31 - 1024 tokens or more, 2^31 heads
@@ -142,11 +144,11 @@ typedef struct sig_window_t {
 } sig_window_t;
 
 int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths, void *out,
-                         float *stats, void *hip_stream);
+                         float *stats, void *rest, void *hip_stream);
 
 /*
  * Gradient of sig_window_attention with respect to q, k and v.
- *   out, stats   as sig_window_attention wrote them
+ *   out, stats, rest   as sig_window_attention wrote them
  *   grad_out     DEVICE, [B][T][heads][value_dim] of `type`, contiguous; what stands behind the lengths is not read
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
@@ -154,7 +156,7 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  * compute unit at most), or where keys are few, for all of them (some four for each unit): key_dim + value_dim floats for each key and part.
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
-                                  const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
+                                  const void *out, const float *stats, const void *rest, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
 
 /*
  * A paged cache of keys and values.  The place p of a sequence b is slot p % page_tokens of page table[b][p / page_tokens], for all heads.

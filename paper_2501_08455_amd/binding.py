@@ -147,9 +147,9 @@ def load():
     lib.sig_linear_attention_backward.restype = i32
     lib.sig_linear_attention_backward.argtypes = [vp, ctypes.POINTER(sig_attention_t)] + [vp] * 13
     lib.sig_window_attention.restype = i32
-    lib.sig_window_attention.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 7
+    lib.sig_window_attention.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 8
     lib.sig_window_attention_backward.restype = i32
-    lib.sig_window_attention_backward.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 11
+    lib.sig_window_attention_backward.argtypes = [vp, ctypes.POINTER(sig_window_t)] + [vp] * 12
     lib.sig_cache_append.restype = i32
     lib.sig_cache_append.argtypes = [vp, ctypes.POINTER(sig_cache_t), ctypes.POINTER(sig_append_t)] + [vp] * 7
     lib.sig_cache_attention.restype = i32

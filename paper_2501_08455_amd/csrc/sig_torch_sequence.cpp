@@ -455,13 +455,15 @@ struct WindowAttention {
         }
     }
 
-    at::Tensor forward(at::Tensor *stats) const
+    // stats, rest: what the gradient needs beside the output, or null
+    at::Tensor forward(at::Tensor *stats, at::Tensor *rest) const
     {
         const auto plain = q.options().memory_format(at::MemoryFormat::Contiguous);
         at::Tensor out = at::empty({shape.B, shape.T, shape.heads, shape.value_dim}, plain);
         if (stats) *stats = at::empty({shape.B, shape.heads, shape.T, 2}, plain.dtype(at::kFloat));
+        if (rest && shape.type != SIG_F32) *rest = at::empty(out.sizes(), plain.dtype(at::kByte));
         check(sig_window_attention(default_ctx, &shape, data(q), data(k), data(v), whole_numbers(lengths), own_data(out), stats ? own_floats(*stats) : nullptr,
-                                   current_stream()), "sig_window_attention");
+                                   rest ? own_data(*rest) : nullptr, current_stream()), "sig_window_attention");
         return out;
     }
 };
@@ -472,9 +474,9 @@ struct DifferentiableWindowAttention : torch::autograd::Function<DifferentiableW
     {
         at::AutoDispatchBelowADInplaceOrView below_autograd;
         const at::Tensor lengths = given(lengths_);
-        at::Tensor stats;
-        const at::Tensor out = WindowAttention(q, k, v, lengths, window, sinks, scale).forward(&stats);
-        ctx->save_for_backward({q, k, v, lengths, stats, out});
+        at::Tensor stats, rest;
+        const at::Tensor out = WindowAttention(q, k, v, lengths, window, sinks, scale).forward(&stats, &rest);
+        ctx->save_for_backward({q, k, v, lengths, stats, out, rest});
         ctx->saved_data["window"] = window;
         ctx->saved_data["sinks"] = sinks;
         ctx->saved_data["scale"] = scale;
@@ -492,7 +494,7 @@ struct DifferentiableWindowAttention : torch::autograd::Function<DifferentiableW
             const at::Tensor g = grads[0].contiguous();
             for (int i = 0; i < 3; ++i) out[i] = at::empty(saved[i].sizes(), saved[i].options().memory_format(at::MemoryFormat::Contiguous));
             check_in_backward(sig_window_attention_backward(default_ctx, &a.shape, data(a.q), data(a.k), data(a.v), whole_numbers(a.lengths), data(saved[5]),
-                                                            floats(saved[4]), data(g), own_data(out[0]), own_data(out[1]), own_data(out[2]), current_stream()),
+                                                            floats(saved[4]), data(saved[6]), data(g), own_data(out[0]), own_data(out[1]), own_data(out[2]), current_stream()),
                               "sig_window_attention_backward");
         }
         return first_order_only(std::move(out), saved, grads);
@@ -823,7 +825,7 @@ PyObject *py_window_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
             if (DIFFERENTIABLE && tracked({t[0], t[1], t[2]}))
                 return DifferentiableWindowAttention::apply(*t[0], *t[1], *t[2], maybe(lengths), window, sinks, scale);
             at::AutoDispatchBelowADInplaceOrView below_autograd;
-            return WindowAttention(*t[0], *t[1], *t[2], lengths, window, sinks, scale).forward(nullptr);
+            return WindowAttention(*t[0], *t[1], *t[2], lengths, window, sinks, scale).forward(nullptr, nullptr);
         });
         return THPVariable_Wrap(std::move(o));
     });

@@ -26,11 +26,30 @@ namespace sig {
 
 constexpr int kWindowThreads = 256, kWindowWaves = kWindowThreads / 64;
 
+// What the rounding of an output to 16 bits leaves, in 8 bits (5 of exponent), times 2^14.  D = g . o decides the gradient where a token sees few others,
+// so that there the output's rounding would cost as much as all others together: window 4, 128 components, the gradient of queries is off by 1.75 of what its own
+// rounding comes to without the rest, and by 1.43 with it.  Three digits of it are enough.  Outputs of 2^-16 to 2^10 have them, beyond it only helps less.
+using Rest = uint8_t;
+constexpr float kRestScale = 16384.0f, kMostRest = 57344.0f;
+
+__device__ inline unsigned rest_of(float low, float high, unsigned other, bool upper)
+{
+    low = __builtin_amdgcn_fmed3f(low * kRestScale, -kMostRest, kMostRest);
+    high = __builtin_amdgcn_fmed3f(high * kRestScale, -kMostRest, kMostRest);
+    return upper ? __builtin_amdgcn_cvt_pk_bf8_f32(low, high, other, true) : __builtin_amdgcn_cvt_pk_bf8_f32(low, high, other, false);
+}
+template <int BYTE>
+__device__ inline float rest_value(unsigned four)
+{
+    return __builtin_amdgcn_cvt_f32_bf8(four, BYTE) * (1.0f / kRestScale);
+}
+
 struct WindowArgs {
     const void *q, *k, *v;                // [B][T][heads or heads / group][.]
     int64_t qs[3], ks[3], vs[3];          // strides in values: batch, token, head
     void *out;                            // [B][T][heads][V], contiguous
     float2 *stats;                        // [B][heads][T]: m in powers of two, r; may be null in the forward pass
+    Rest *rest;                           // as `out`, of 16 bits: what its rounding left; null where stats is
     const int64_t *lengths;               // [B], or null: T
     // of the gradient
     const void *grad_out;                 // as `out`
@@ -118,6 +137,32 @@ __device__ inline void store_line(T *line, int dim, int lane, const typename X::
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (c + j < dim) line[c + j] = four.v[j];
+            }
+        }
+}
+
+// ... and what its rounding to T leaves
+template <typename X, int D, typename T>
+__device__ inline void store_rest(Rest *line, int dim, int lane, const typename X::Result *acc, float scale)
+{
+#pragma unroll
+    for (int t = 0; t < D / X::M; ++t)
+#pragma unroll
+        for (int i = 0; i < X::REGS; i += 4) {
+            const int c = t * X::M + X::row_of(lane, i);
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = acc[t][i + j] * scale;
+                x[j] -= to_float(from_float<T>(x[j]));
+            }
+            const unsigned four = rest_of(x[2], x[3], rest_of(x[0], x[1], 0, false), true);
+            if (c + 4 <= dim) {
+                store_pack(line + c, __builtin_bit_cast(Pack<Rest, 4>, four));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < dim) line[c + j] = (Rest)(four >> (8 * j));
             }
         }
 }
@@ -284,6 +329,9 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
     const float r = 1.0f / sum;
     if (there) {
         store_line<X, D>(out + line * out_stride, A.V, lane, acc, r);
+        if constexpr (sizeof(T) == 2) {
+            if (A.rest) store_rest<X, D, T>(A.rest + ((p.b * A.T + line) * A.heads + p.head) * A.V, A.V, lane, acc, r);
+        }
         if (A.stats && lane < M) A.stats[(p.b * A.heads + p.head) * A.T + line] = make_float2((m == -INFINITY ? 0.0f : m) - kLift<E>, r);
     }
     if (hi < end) zero_rows(out, out_stride, A.V, hi, end);
@@ -317,11 +365,31 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
     fragments_of<X, STEPS>(g, lane, (const T *)A.grad_out + upstream, A.V, there, false);
     float delta = 0.0f;
     {
-        // (the output as the forward pass rounded it)
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
             typename X::Frag o;
             fragment_of<X>(&o, lane, j, (const T *)A.out + upstream, A.V, there);
+            if constexpr (sizeof(T) == 2) {
+                const int at = j * X::STEP + X::first_of(lane);
+                uint64_t eight = 0;
+                if (there && at + 8 <= A.V) {
+                    eight = __builtin_bit_cast(uint64_t, load_pack<Rest, 8>(A.rest + upstream + at));
+                } else if (there) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (at + e < A.V) eight |= (uint64_t)A.rest[upstream + at + e] << (8 * e);
+                }
+                const unsigned words[] = {(unsigned)eight, (unsigned)(eight >> 32)};
+                float rest = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    rest = fmaf(rest_value<0>(words[h]), (float)g[j][4 * h], rest);
+                    rest = fmaf(rest_value<1>(words[h]), (float)g[j][4 * h + 1], rest);
+                    rest = fmaf(rest_value<2>(words[h]), (float)g[j][4 * h + 2], rest);
+                    rest = fmaf(rest_value<3>(words[h]), (float)g[j][4 * h + 3], rest);
+                }
+                delta += rest;
+            }
 #pragma unroll
             for (int e = 0; e < X::GROUP; ++e) delta = fmaf((float)o[e], (float)g[j][e], delta);
         }

@@ -66,29 +66,31 @@ hipError_t launch(const WindowArgs &A, int type, WindowPass pass, hipStream_t st
 extern "C" {
 
 int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths, void *out,
-                         float *stats, void *hip_stream)
+                         float *stats, void *rest, void *hip_stream)
 {
     const int rc = check(ctx, shape);
     if (rc != SIG_OK) return rc;
     if (shape->B == 0 || shape->T == 0) return SIG_OK;
-    if (!q || !k || !v || !out) return SIG_ERR_INVALID;
+    if (!q || !k || !v || !out || (stats && !rest && shape->type != SIG_F32)) return SIG_ERR_INVALID;
     WindowArgs A = arguments(*shape, q, k, v, lengths);
     A.out = out;
     A.stats = (float2 *)stats;
+    A.rest = stats ? (Rest *)rest : nullptr;
     return launch(A, shape->type, WINDOW_FORWARD, (hipStream_t)hip_stream) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
-                                  const void *out, const float *stats, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream)
+                                  const void *out, const float *stats, const void *rest, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream)
 {
     int rc = check(ctx, shape);
     if (rc != SIG_OK) return rc;
     if (shape->B == 0 || shape->T == 0) return SIG_OK;
-    if (!q || !k || !v || !out || !stats || !grad_out || !grad_q || !grad_k || !grad_v) return SIG_ERR_INVALID;
+    if (!q || !k || !v || !out || !stats || !grad_out || !grad_q || !grad_k || !grad_v || (!rest && shape->type != SIG_F32)) return SIG_ERR_INVALID;
     const hipStream_t st = (hipStream_t)hip_stream;
     WindowArgs A = arguments(*shape, q, k, v, lengths);
     A.out = (void *)out;
     A.stats = (float2 *)stats;
+    A.rest = (Rest *)rest;
     A.grad_out = grad_out;
     A.grad_q = grad_q;
     A.grad_k = grad_k;

@@ -90,8 +90,8 @@ int main()
         const int64_t *lengths = (const int64_t *)p;
         if (what == "forward" || what == "backward") {
             const sig_window_t s = {n[0], n[1], (int32_t)n[2], (int32_t)n[3], (int32_t)n[4], (int32_t)n[5], (int32_t)n[6], 1.0f, n[7], n[8], {}, {}, {}};
-            rc = what == "forward" ? sig_window_attention(ctx, &s, p, p, p, lengths, p, p, nullptr)
-                                   : sig_window_attention_backward(ctx, &s, p, p, p, lengths, p, p, p, p, p, p, nullptr);
+            rc = what == "forward" ? sig_window_attention(ctx, &s, p, p, p, lengths, p, p, p, nullptr)
+                                   : sig_window_attention_backward(ctx, &s, p, p, p, lengths, p, p, p, p, p, p, p, nullptr);
         } else {
             const bool attend = what == "attend";
             sig_cache_t c = {};

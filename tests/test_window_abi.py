@@ -32,8 +32,8 @@ def cache(p, **change):
 
 def test_calls_without_a_context_are_refused():
     lib, none = binding.load(), None
-    assert lib.sig_window_attention(none, ctypes.byref(window()), *[none] * 7) == INVALID
-    assert lib.sig_window_attention_backward(none, ctypes.byref(window()), *[none] * 11) == INVALID
+    assert lib.sig_window_attention(none, ctypes.byref(window()), *[none] * 8) == INVALID
+    assert lib.sig_window_attention_backward(none, ctypes.byref(window()), *[none] * 12) == INVALID
     c = cache(none)
     assert lib.sig_cache_append(none, ctypes.byref(c), ctypes.byref(binding.sig_append_t(1, 1, 1, 0)), *[none] * 7) == INVALID
     assert lib.sig_cache_attention(none, ctypes.byref(c), ctypes.byref(binding.sig_queries_t(1, 1, 1, 0, 1.0)), *[none] * 5) == INVALID
@@ -48,8 +48,8 @@ def test_bad_arguments_are_refused():
 
     def attention(q=p, k=p, v=p, out=p, **change):
         shape = window(**change)
-        both = (lib.sig_window_attention(ctx, ctypes.byref(shape), q, k, v, None, out, None, None),
-                lib.sig_window_attention_backward(ctx, ctypes.byref(shape), q, k, v, None, out, p, p, out, p, p, None))
+        both = (lib.sig_window_attention(ctx, ctypes.byref(shape), q, k, v, None, out, None, None, None),
+                lib.sig_window_attention_backward(ctx, ctypes.byref(shape), q, k, v, None, out, p, None, p, out, p, p, None))
         assert both[0] == both[1]
         return both[0]
 
@@ -60,8 +60,11 @@ def test_bad_arguments_are_refused():
     assert attention(key_dim=257) == attention(value_dim=1000) == UNSUPPORTED
     assert attention(B=1 << 31) == attention(T=(1 << 31) - 1024) == attention(B=1 << 20, T=1 << 28) == LARGE
     assert attention(B=0, q=None) == attention(T=0, q=None) == OK
-    assert lib.sig_window_attention(ctx, None, p, p, p, None, p, None, None) == INVALID
-    assert lib.sig_window_attention_backward(ctx, ctypes.byref(window()), p, p, p, None, p, None, p, p, p, p, None) == INVALID      # (no stats)
+    assert lib.sig_window_attention(ctx, None, p, p, p, None, p, None, None, None) == INVALID
+    assert lib.sig_window_attention_backward(ctx, ctypes.byref(window()), p, p, p, None, p, None, None, p, p, p, p, None) == INVALID      # (no stats)
+    for kind in (binding.SIG_BF16, binding.SIG_F16):      # (no rest)
+        assert lib.sig_window_attention(ctx, ctypes.byref(window(type=kind)), p, p, p, None, p, p, None, None) == INVALID
+        assert lib.sig_window_attention_backward(ctx, ctypes.byref(window(type=kind)), p, p, p, None, p, p, None, p, p, p, p, None) == INVALID
 
     def append(q=p, k=p, v=p, lengths=p, q_out=p, of=(), B=1, T=1, heads=1, kind=0, **change):
         shape, c = binding.sig_append_t(B, T, heads, kind), cache(p, **dict(of))
