@@ -23,12 +23,17 @@ namespace sig {
 using f4 = __attribute__((ext_vector_type(4))) float;
 using f16v = __attribute__((ext_vector_type(16))) float;
 
+template <typename E, int D>
+struct LdsTile;
+
 // What bfloat16 and float16 share
 template <typename E_>
 struct NarrowTiles {
     using E = E_;
-    static constexpr int M = 32, STEP = 16, REGS = 16;
-    static constexpr int GROUP = 8;                 // values of 16 bytes
+    static constexpr int M = 32, STEP = 16, REGS = 16, PLANES = 1;      // planes: of a value in LDS, side by side
+    static constexpr int GROUP = 8;                 // values of a fragment's lane
+    template <int D>
+    using Tile = LdsTile<E, D>;
     using Frag = __attribute__((ext_vector_type(8))) E;
     using Result = f16v;
 
@@ -69,8 +74,10 @@ struct NarrowTiles {
 template <typename E_>
 struct SmallNarrowTiles {
     using E = E_;
-    static constexpr int M = 16, STEP = 32, REGS = 4;
+    static constexpr int M = 16, STEP = 32, REGS = 4, PLANES = 1;
     static constexpr int GROUP = 8;
+    template <int D>
+    using Tile = LdsTile<E, D>;
     using Frag = __attribute__((ext_vector_type(8))) E;
     using Result = f4;
 
@@ -132,8 +139,10 @@ struct SmallTiles<f16> : SmallNarrowTiles<f16> {
 template <>
 struct Tiles<float> {
     using E = float;
-    static constexpr int M = 16, STEP = 16, REGS = 4;
+    static constexpr int M = 16, STEP = 16, REGS = 4, PLANES = 1;
     static constexpr int GROUP = 4;
+    template <int D>
+    using Tile = LdsTile<E, D>;
     using Frag = f4;
     using Result = f4;
 
@@ -164,31 +173,133 @@ struct Tiles<float> {
 template <>
 struct SmallTiles<float> : Tiles<float> {};
 
+// Float32 as three bfloat16 numbers that add up to it, 24 digits in all, multiplied in 32 x 32 tiles: six of the nine products of parts, the others being
+// 2^-23 of a product at most and 2^-26 on average, with either sign.  That is 2.7 times the rate that float32 products have, with twice the lines for each read.
+// The first part is cut off rather than rounded (so that it does not overflow), the second is rounded, the third is what is left.
+struct SplitTiles : NarrowTiles<bf16> {
+    using Base = NarrowTiles<bf16>;
+    static constexpr int PLANES = 3;
+    struct Frag {
+        Base::Frag part[PLANES];
+    };
+    template <int D>
+    using Tile = LdsTile<bf16, PLANES * D>;
+
+    // FINITE: x is known not to be infinite (an infinity is its first part)
+    template <bool FINITE, int N, typename V>
+    static __device__ void split(const float *x, V *parts)
+    {
+        using b2 = __attribute__((ext_vector_type(2))) bf16;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const unsigned low = __builtin_bit_cast(unsigned, x[e]), high = __builtin_bit_cast(unsigned, x[e + 1]);
+            float a = x[e] - __builtin_bit_cast(float, low & 0xffff0000u), b = x[e + 1] - __builtin_bit_cast(float, high & 0xffff0000u);
+            if (!FINITE) {
+                a = fabsf(x[e]) == INFINITY ? 0.0f : a;
+                b = fabsf(x[e + 1]) == INFINITY ? 0.0f : b;
+            }
+            const b2 first = __builtin_bit_cast(b2, __builtin_amdgcn_perm(high, low, 0x07060302u));
+            unsigned bits = __builtin_bit_cast(unsigned, b2{(bf16)a, (bf16)b});
+            asm("" : "+v"(bits));      // (or the conversion is done anew for each half)
+            const b2 second = __builtin_bit_cast(b2, bits);
+            a -= __builtin_bit_cast(float, bits << 16);
+            b -= __builtin_bit_cast(float, bits & 0xffff0000u);
+            const b2 third = __builtin_bit_cast(b2, __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                parts[0][e + i] = first[i];
+                parts[1][e + i] = second[i];
+                parts[2][e + i] = third[i];
+            }
+        }
+    }
+    template <typename Tile>
+    static __device__ Frag rows(int lane, const bf16 *tile, int line, int at)
+    {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i) f.part[i] = Base::rows<Tile>(lane, tile, line, at + i * (Tile::WIDTH / PLANES));
+        return f;
+    }
+    template <typename Tile>
+    static __device__ Frag columns(int lane, const bf16 *tile, int at, int line)
+    {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i) f.part[i] = Base::columns<Tile>(lane, tile, at, line + i * (Tile::WIDTH / PLANES));
+        return f;
+    }
+    static __device__ Frag of_results(const Result *tiles, int step)
+    {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = tiles[step / 2][step % 2 * 8 + e];
+        Frag f;
+        split<true, 8>(x, f.part);
+        return f;
+    }
+    static __device__ Result multiply(const Frag &left, const Frag &right, Result sum)
+    {
+#pragma unroll
+        for (int both = PLANES - 1; both >= 0; --both)      // (the smallest first)
+#pragma unroll
+            for (int i = 0; i <= both; ++i) sum = multiply_parts(left, i, right, both - i, sum);
+        return sum;
+    }
+    static __device__ Result multiply_parts(const Frag &left, int i, const Frag &right, int j, Result sum)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(left.part[i], right.part[j], sum, 0, 0, 0);
+    }
+};
+
+// Fragments as numbers: value e, and setting it
+template <typename F>
+__device__ inline float fragment_value(const F &f, int e) { return (float)f[e]; }
+__device__ inline float fragment_value(const SplitTiles::Frag &f, int e) { return (float)f.part[0][e] + ((float)f.part[1][e] + (float)f.part[2][e]); }
+template <typename F, typename V>
+__device__ inline void set_fragment(F &f, const V &values)
+{
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(F) / sizeof(f[0])); ++e) f[e] = (std::remove_reference_t<decltype(f[0])>)values[e];
+}
+template <typename V>
+__device__ inline void set_fragment(SplitTiles::Frag &f, const V &values)
+{
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = values[e];
+    SplitTiles::split<false, 8>(x, f.part);
+}
+
 // Rows of D values in LDS, PITCH apart: an odd number of 16 bytes, so that the 16 rows of a 16-byte read (rows) find all 64 banks, and
 // one that keeps the 32-byte pieces of four rows of a transposing read in different ones.
 template <typename E, int D>
 struct LdsTile {
-    static constexpr int BANK_GROUPS = D * (int)sizeof(E) / 16 % 16;
+    static constexpr int WIDTH = D, BANK_GROUPS = D * (int)sizeof(E) / 16 % 16;
     static constexpr int PITCH = D + (sizeof(E) == 4 ? 4 : BANK_GROUPS == 0 || BANK_GROUPS == 4 ? 24 : 8);
 };
 
 // The wavefront's own operand, one line a lane: a fragment to match step number j of the rows form, zeros where `there` is false
 template <typename X, typename T>
-__device__ inline void fragment_of(typename X::Frag *f, int lane, int j, const T *line, int dim, bool there)
+__device__ inline void fragment_of(typename X::Frag *f, int lane, int j, const T *line, int dim, bool there, bool negated = false)
 {
-    using E = typename X::E;
-    constexpr int N = X::GROUP;
+    constexpr int N = X::GROUP, LOAD = 16 / (int)sizeof(T);
     const int at = j * X::STEP + X::first_of(lane);
-    *f = typename X::Frag{};
+    __attribute__((ext_vector_type(N))) T got = {};
     if (there && at + N <= dim) {
-        const auto got = __builtin_bit_cast(__attribute__((ext_vector_type(N))) T, load_words<T, N>(line + at));
 #pragma unroll
-        for (int e = 0; e < N; ++e) (*f)[e] = (E)got[e];
+        for (int first = 0; first < N; first += LOAD) {
+            const auto some = __builtin_bit_cast(__attribute__((ext_vector_type(LOAD))) T, load_words<T, LOAD>(line + at + first));
+#pragma unroll
+            for (int e = 0; e < LOAD; ++e) got[first + e] = some[e];
+        }
     } else if (there) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (at + e < dim) (*f)[e] = (E)line[at + e];
+            if (at + e < dim) got[e] = line[at + e];
     }
+    if (negated) got = -got;
+    set_fragment(*f, got);
 }
 
 template <typename X, int STEPS, typename T>
@@ -196,22 +307,28 @@ __device__ inline void fragments_of(typename X::Frag *f, int lane, const T *line
 {
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-        fragment_of<X>(f + j, lane, j, line, dim, there);
-        if (negated) f[j] = -f[j];
+        fragment_of<X>(f + j, lane, j, line, dim, there, negated);
     }
 }
 
 // ROWS x D values, global memory -> registers -> LDS, by THREADS threads: zeros beyond the rows and values that are there.  Loads of whole groups are
 // unconditional (what is not there is read from a place that is, and dropped on the way to LDS), so that all are in flight at once.
-// WHOLE: rows have D values.
-template <typename T, typename E, int D, int ROWS, int THREADS, bool WHOLE>
+// WHOLE: rows have D values.  ANEW: addresses are worked out anew each time, where keeping them asks for more registers than there are.
+template <typename T, typename X, int D, int ROWS, int THREADS, bool WHOLE, bool ANEW = false>
 struct TileMover {
-    static constexpr int GROUP = Tiles<E>::GROUP, GROUPS = D / GROUP, COUNT = (ROWS * GROUPS + THREADS - 1) / THREADS;
+    using E = typename X::E;
+    static constexpr int GROUP = 16 / (int)sizeof(T), GROUPS = D / GROUP, COUNT = (ROWS * GROUPS + THREADS - 1) / THREADS;
     static constexpr bool EVEN = ROWS * GROUPS % THREADS == 0;      // else some threads have no last group (they load what is there, and drop it)
     Words<T, GROUP> held[COUNT];
 
-    static __device__ int row_of(int i) { return (threadIdx.x + i * THREADS) / GROUPS; }
-    static __device__ int place_of(int i) { return (threadIdx.x + i * THREADS) % GROUPS * GROUP; }
+    static __device__ int thread()
+    {
+        int number = threadIdx.x;
+        if (ANEW) asm volatile("" : "+v"(number));
+        return number;
+    }
+    static __device__ int row_of(int i) { return (thread() + i * THREADS) / GROUPS; }
+    static __device__ int place_of(int i) { return (thread() + i * THREADS) % GROUPS * GROUP; }
 
     static __device__ bool here(int i) { return EVEN || (int)threadIdx.x + i * THREADS < ROWS * GROUPS; }
 
@@ -258,18 +375,23 @@ struct TileMover {
     }
     __device__ void store(E *tile, int dim, int n) const
     {
+        using Tile = typename X::template Tile<D>;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            f4 bits;
-            if constexpr (sizeof(T) == sizeof(E)) {
-                bits = __builtin_bit_cast(f4, held[i]);
-            } else {
-                const auto values = __builtin_bit_cast(__attribute__((ext_vector_type(GROUP))) T, held[i]);
-#pragma unroll
-                for (int j = 0; j < GROUP; ++j) bits[j] = (float)values[j];
-            }
             const bool there = row_of(i) < n, within = WHOLE || place_of(i) < dim, ok = there & within;
-            if (EVEN || here(i)) *(f4 *)(tile + row_of(i) * LdsTile<E, D>::PITCH + place_of(i)) = ok ? bits : f4{};
+            E *to = tile + row_of(i) * Tile::PITCH + place_of(i);
+            const f4 bits = ok ? __builtin_bit_cast(f4, held[i]) : f4{};
+            if constexpr (X::PLANES == 1) {
+                if (EVEN || here(i)) *(f4 *)to = bits;
+            } else {
+                using b4 = __attribute__((ext_vector_type(4))) bf16;
+                const float x[] = {bits[0], bits[1], bits[2], bits[3]};
+                b4 parts[X::PLANES];
+                X::template split<false, 4>(x, parts);
+#pragma unroll
+                for (int p = 0; p < X::PLANES; ++p)
+                    if (EVEN || here(i)) *(b4 *)(to + p * D) = parts[p];
+            }
         }
     }
 };
@@ -280,7 +402,6 @@ struct TileMover {
 template <typename X, int D, int STEPS, bool WHOLE, int APART = 1>
 __device__ inline void product_along_rows(int lane, const typename X::E *tile, const typename X::Frag *p, typename X::Result *acc, int dim)
 {
-    using E = typename X::E;
     constexpr int PIECES = WHOLE ? 1 : 4, TILES = D / X::M / PIECES > 0 ? D / X::M / PIECES : 1;
 #pragma unroll
     for (int piece = 0; piece < D / X::M; piece += TILES) {
@@ -288,20 +409,22 @@ __device__ inline void product_along_rows(int lane, const typename X::E *tile, c
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
 #pragma unroll
-            for (int t = piece; t < piece + TILES; ++t) acc[t] = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j * X::STEP, t * X::M), p[j], acc[t]);
+            for (int t = piece; t < piece + TILES; ++t) acc[t] = X::multiply(X::template columns<typename X::template Tile<D>>(lane, tile, j * X::STEP, t * X::M), p[j], acc[t]);
             if (j % APART == APART - 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
 
 // Tiles that are partly hidden and hold something that is not finite: that is set to 0 in LDS before the product along the rows, by all threads ...
-template <typename E, int D, int ROWS, int THREADS>
-__device__ inline void leave_finite(E *tile)
+template <typename X, int D, int ROWS, int THREADS>
+__device__ inline void leave_finite(typename X::E *tile)
 {
+    using E = typename X::E;
+    constexpr int WIDTH = D * X::PLANES;
     __syncthreads();
 #pragma unroll 1
-    for (int i = threadIdx.x; i < ROWS * D; i += THREADS) {
-        E *x = tile + i / D * LdsTile<E, D>::PITCH + i % D;
+    for (int i = threadIdx.x; i < ROWS * WIDTH; i += THREADS) {
+        E *x = tile + i / WIDTH * X::template Tile<D>::PITCH + i % WIDTH;
         if (!__builtin_isfinite((float)*x)) *x = (E)0.0f;
     }
     __syncthreads();
@@ -322,7 +445,8 @@ __device__ inline void add_not_finite(int lane, typename X::E *tile, const T *fi
             const int row = i / D, c = i % D;
             const float x = row < n && c < dim ? (float)first[row * stride + c] : 0.0f;
             const bool is = NANS ? !__builtin_isfinite(x) : kind == 0 ? x != x : kind == 1 ? x == INFINITY : x == -INFINITY;
-            tile[row * LdsTile<E, D>::PITCH + c] = (E)(is ? 1.0f : 0.0f);
+#pragma unroll
+            for (int p = 0; p < X::PLANES; ++p) tile[row * X::template Tile<D>::PITCH + c + p * D] = (E)(is && p == 0 ? 1.0f : 0.0f);
         }
         __syncthreads();
         if (idle) continue;
@@ -332,10 +456,12 @@ __device__ inline void add_not_finite(int lane, typename X::E *tile, const T *fi
             typename X::Result counts = {};
 #pragma unroll 1
             for (int j = 0; j < ROWS; j += X::STEP) {
-                typename X::Frag sees;
+                float visible[X::GROUP];
 #pragma unroll
-                for (int e = 0; e < X::GROUP; ++e) sees[e] = (E)(seen(j + X::place_of(lane, e)) ? 1.0f : 0.0f);
-                counts = X::multiply(X::template columns<LdsTile<E, D>>(lane, tile, j, t * X::M), sees, counts);
+                for (int e = 0; e < X::GROUP; ++e) visible[e] = seen(j + X::place_of(lane, e)) ? 1.0f : 0.0f;
+                typename X::Frag sees;
+                set_fragment(sees, visible);
+                counts = X::multiply(X::template columns<typename X::template Tile<D>>(lane, tile, j, t * X::M), sees, counts);
             }
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) acc[t][i] += counts[i] > 0.0f ? what : 0.0f;
@@ -344,10 +470,9 @@ __device__ inline void add_not_finite(int lane, typename X::E *tile, const T *fi
 }
 
 // s[t] += rows(tile) x own, tile by tile of COUNT M rows (WHOLE, dim, APART: as above)
-template <typename X, int D, int COUNT, bool WHOLE, int APART = 2>
+template <typename X, int D, int COUNT, bool WHOLE, int APART = X::PLANES == 1 ? 2 : 1>
 __device__ inline void product_of_rows(int lane, const typename X::E *tile, const typename X::Frag *own, typename X::Result *s, int dim)
 {
-    using E = typename X::E;
     constexpr int PIECES = WHOLE ? 1 : 4, STEPS = D / X::STEP / PIECES > 0 ? D / X::STEP / PIECES : 1;
 #pragma unroll
     for (int piece = 0; piece < D / X::STEP; piece += STEPS) {
@@ -355,10 +480,43 @@ __device__ inline void product_of_rows(int lane, const typename X::E *tile, cons
 #pragma unroll
         for (int step = piece; step < piece + STEPS; ++step) {
 #pragma unroll
-            for (int t = 0; t < COUNT; ++t) s[t] = X::multiply(X::template rows<LdsTile<E, D>>(lane, tile, t * X::M, step * X::STEP), own[step], s[t]);
+            for (int t = 0; t < COUNT; ++t) s[t] = X::multiply(X::template rows<typename X::template Tile<D>>(lane, tile, t * X::M, step * X::STEP), own[step], s[t]);
             if (step % APART == APART - 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
+
+// An infinity times parts of either sign is no number: where the product of the first parts alone is not finite, that is what the whole product is
+template <typename X, int D, int COUNT>
+__device__ inline void settle_infinities(int lane, const typename X::E *tile, const typename X::Frag *own, typename X::Result *s)
+{
+    if constexpr (X::PLANES > 1) {
+#pragma unroll
+        for (int t = 0; t < COUNT; ++t) {
+            typename X::Result first = {};
+#pragma unroll
+            for (int step = 0; step < D / X::STEP; ++step) {
+                first = X::multiply_parts(X::template rows<typename X::template Tile<D>>(lane, tile, t * X::M, step * X::STEP), 0, own[step], 0, first);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < X::REGS; ++i) s[t][i] = __builtin_isfinite(first[i]) ? s[t][i] : first[i];
+        }
+    }
+}
+
+// whether a lane of the wavefront holds something that is not finite
+template <int STEPS>
+__device__ inline bool any_infinite(const SplitTiles::Frag *f)
+{
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const auto words = __builtin_bit_cast(Words<bf16, 8>, f[j].part[0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bad |= word_spoilt<bf16>(words[i]);
+    }
+    return __any(bad);
 }
 
 // over the lanes that hold one column of a result tile

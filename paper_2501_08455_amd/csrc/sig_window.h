@@ -210,10 +210,10 @@ struct TermScale {
 
 // ---------------------------------------------------------------- forward
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 2 : 1) void sig_window_forward_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::E) <= 384 ? 2 : 1) void sig_window_forward_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * X::template Tile<D>::PITCH;
     __shared__ __attribute__((aligned(16))) E keys[2 * SIZE];
     __shared__ __attribute__((aligned(16))) E values[2 * SIZE];
     __shared__ int spoilt[2];      // 1 + the number of a tile that is partly hidden and holds something that is not finite
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
     fragments_of<X, STEPS>(q, lane, (const T *)A.q + p.b * A.qs[0] + (there ? line : lo) * A.qs[1] + p.head * A.qs[2], A.K, there, A.negated);
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
-    TileMover<T, E, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
+    TileMover<T, X, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
@@ -244,15 +244,21 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
         const int at = tiles.at(j);
         key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
         value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
-        if (!seen.all(lo, hi - 1, at, at + N - 1) && value_tile.spoilt(A.V, p.n - at)) spoilt[j & 1] = j + 1;
+        // (float32's parts: infinities that all see as well, which are no products of theirs)
+        if constexpr (X::PLANES > 1) {
+            if (key_tile.spoilt(A.K, p.n - at) || value_tile.spoilt(A.V, p.n - at)) spoilt[j & 1] = j + 1;
+        } else {
+            if (!seen.all(lo, hi - 1, at, at + N - 1) && value_tile.spoilt(A.V, p.n - at)) spoilt[j & 1] = j + 1;
+        }
     };
     typename X::Result acc[OUT] = {};
     float m = -INFINITY, sum = 0.0f;      // of the lane's own part of its line
     typename X::Frag probabilities[N / X::STEP];
     // the probabilities of tile j, and the running maximum and sum
-    auto weigh = [&](int at, const E *keys) {
+    auto weigh = [&](int at, const E *keys, auto careful) {
         typename X::Result s[KEYS] = {};
         product_of_rows<X, D, KEYS, WHOLE>(lane, keys, q, s, A.K);
+        if constexpr (decltype(careful)::value) settle_infinities<X, D, KEYS>(lane, keys, q, s);
         if (!seen.all(own, own + M - 1, at, at + N - 1)) {
 #pragma unroll
             for (int t = 0; t < KEYS; ++t)
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
         __syncthreads();
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
-        if (!skip) weigh(at, keys + half);
+        if (!skip) weigh(at, keys + half, std::false_type());
         if (j + 1 < tiles.count) store(j + 1);
         if (j + 2 < tiles.count) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, values + half, probabilities, acc, A.V);
@@ -319,8 +325,8 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
             __syncthreads();
             if (spoilt[j & 1] != j + 1) continue;
             const bool skip = none(at);
-            if (!skip) weigh(at, keys + (j & 1) * SIZE);
-            leave_finite<E, D, N, kWindowThreads>(tile);
+            if (!skip) weigh(at, keys + (j & 1) * SIZE, std::true_type());
+            leave_finite<X, D, N, kWindowThreads>(tile);
             if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, tile, probabilities, acc, A.V);
             add_not_finite<X, D, N, kWindowThreads, false>(lane, tile, v + at * A.vs[1], A.vs[1], A.V, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
@@ -339,10 +345,10 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= 256 ? 
 
 // ---------------------------------------------------------------- gradient of the queries, and D
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE ? 256 : 128) ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE && X::PLANES == 1 ? 256 : 128) ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH;
+    constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * X::template Tile<D>::PITCH;
     __shared__ __attribute__((aligned(16))) E keys[2 * SIZE];
     __shared__ __attribute__((aligned(16))) E values[2 * SIZE];
     __shared__ int spoilt[2];
@@ -391,7 +397,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
                 delta += rest;
             }
 #pragma unroll
-            for (int e = 0; e < X::GROUP; ++e) delta = fmaf((float)o[e], (float)g[j][e], delta);
+            for (int e = 0; e < X::GROUP; ++e) delta = fmaf(fragment_value(o, e), fragment_value(g[j], e), delta);
         }
         delta = over_column<M>(delta, [](float a, float b) { return a + b; });
     }
@@ -402,7 +408,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
     }
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
-    TileMover<T, E, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
+    TileMover<T, X, D, N, kWindowThreads, WHOLE, (X::PLANES > 1 && !WHOLE)> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
@@ -412,14 +418,15 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         const int at = tiles.at(j);
         key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
         value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
-        if (!seen.all(lo, hi - 1, at, at + N - 1) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = j + 1;
+        if ((X::PLANES > 1 || !seen.all(lo, hi - 1, at, at + N - 1)) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = j + 1;
     };
     typename X::Result acc[OUT] = {};
     TermScale scale;
     typename X::Frag terms[N / X::STEP];
-    auto weigh = [&](int at, const E *keys, const E *values) {
+    auto weigh = [&](int at, const E *keys, const E *values, auto careful) {
         typename X::Result s[KEYS] = {}, u[KEYS] = {};
         product_of_rows<X, D, KEYS, WHOLE>(lane, keys, q, s, A.K);
+        if constexpr (decltype(careful)::value) settle_infinities<X, D, KEYS>(lane, keys, q, s);
         product_of_rows<X, D, KEYS, WHOLE>(lane, values, g, u, A.V);
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
@@ -459,7 +466,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         __syncthreads();
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
-        if (!skip) weigh(at, keys + half, values + half);
+        if (!skip) weigh(at, keys + half, values + half, std::false_type());
         if (j + 1 < tiles.count) store(j + 1);
         if (j + 2 < tiles.count) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, keys + half, terms, acc, A.K);
@@ -475,8 +482,8 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
             __syncthreads();
             if (spoilt[j & 1] != j + 1) continue;
             const bool skip = none(at);
-            if (!skip) weigh(at, tile, values + (j & 1) * SIZE);
-            leave_finite<E, D, N, kWindowThreads>(tile);
+            if (!skip) weigh(at, tile, values + (j & 1) * SIZE, std::true_type());
+            leave_finite<X, D, N, kWindowThreads>(tile);
             if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, tile, terms, acc, A.K);
             add_not_finite<X, D, N, kWindowThreads, true>(lane, tile, k + at * A.ks[1], A.ks[1], A.K, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
@@ -497,7 +504,7 @@ template <typename T, typename X, int D, int N, bool WHOLE>
 __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
-    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * LdsTile<E, D>::PITCH, NUMBERS = QUERIES * X::REGS;
+    constexpr int M = X::M, ROWS = kWindowWaves * M, QUERIES = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * X::template Tile<D>::PITCH, NUMBERS = QUERIES * X::REGS;
     constexpr float LIFT = std::is_same_v<E, f16> ? 32768.0f : 1.0f;      // of the probabilities, which are at most 1 (see kLift)
     __shared__ __attribute__((aligned(16))) E queries[3 * SIZE];
     __shared__ __attribute__((aligned(16))) E upstream[3 * SIZE];
@@ -562,7 +569,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
             ++w.head;
         }
     };
-    TileMover<T, E, D, N, kKeyThreads, WHOLE> query_tile, upstream_tile;
+    TileMover<T, X, D, N, kKeyThreads, WHOLE> query_tile, upstream_tile;
     float2 stats_tile;
     float delta_tile;
     auto load = [&](const Place &w) {
@@ -594,9 +601,10 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
     auto hidden = [&](int at) { return at + N > n || !seen.all(at, at + N - 1, own, own + M - 1); };
     auto sees = [&](int query) { return (query < n) & seen(query, line); };
     // the probabilities of a tile, for the second wavefront too
-    auto weigh_values = [&](int at, int room, int half) {
+    auto weigh_values = [&](int at, int room, int half, auto careful) {
         typename X::Result s[QUERIES] = {};
         product_of_rows<X, D, QUERIES, WHOLE, 4>(lane, queries + room * SIZE, held, s, A.K);
+        if constexpr (decltype(careful)::value) settle_infinities<X, D, QUERIES>(lane, queries + room * SIZE, held, s);
 #pragma unroll
         for (int t = 0; t < QUERIES; ++t)
 #pragma unroll
@@ -659,6 +667,8 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
         for (int step = 0; step < N / X::STEP; ++step) weights[step] = X::of_results(u, step);
     };
     auto none = [&](int at) { return own >= hi || seen.none(at, min(at + N, n) - 1, own, min(own + M, hi) - 1); };
+    bool all_bad = false;      // (infinite keys, whose products with parts are no numbers)
+    if constexpr (X::PLANES > 1) all_bad = __syncthreads_or(!second && any_infinite<STEPS>(held));
     // Tile j is the first wavefronts' and tile j - 1 the second ones', tile j + 1 goes to LDS, j + 2 is on its way
     bool left_out = false, skipped = true;      // skipped: the tile before
     if (threadIdx.x < 3) spoilt[threadIdx.x] = 0;
@@ -673,10 +683,10 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
     for (int j = 0; j <= count; ++j) {
         const int following = room == 2 ? 0 : room + 1;
         __syncthreads();
-        const bool bad = j < count && __builtin_amdgcn_readfirstlane(spoilt[room]) == j + 1, skip = bad || j == count || none(now.at);
+        const bool bad = j < count && (all_bad || __builtin_amdgcn_readfirstlane(spoilt[room]) == j + 1), skip = bad || j == count || none(now.at);
         left_out |= bad;
         if (!second && !skip) {
-            weigh_values(now.at, room, j & 1);
+            weigh_values(now.at, room, j & 1, std::false_type());
             product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, upstream + room * SIZE, weights, acc, A.V);
         }
         if (second && !skipped) {
@@ -701,13 +711,13 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
             load(now);
             store(now, j, 0);
             __syncthreads();
-            if (spoilt[0] != j + 1) continue;
+            if (!all_bad && spoilt[0] != j + 1) continue;
             const bool skip = none(at);
-            if (!second && !skip) weigh_values(at, 0, 0);
+            if (!second && !skip) weigh_values(at, 0, 0, std::true_type());
             __syncthreads();
             if (second && !skip) weigh_keys(at, 0, 0);
-            leave_finite<E, D, N, kKeyThreads>(queries);
-            leave_finite<E, D, N, kKeyThreads>(upstream);
+            leave_finite<X, D, N, kKeyThreads>(queries);
+            leave_finite<X, D, N, kKeyThreads>(upstream);
             if (!second && !skip) product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, upstream, weights, acc, A.V);
             if (second && !skip) product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, queries, weights, acc, A.K);
             add_not_finite<X, D, N, kKeyThreads, false>(lane, upstream, (const T *)A.grad_out + ((b * A.T + at) * A.heads + head) * A.V, g_stride, A.V, n - at,
@@ -759,8 +769,11 @@ hipError_t launch_window_f32(const WindowArgs &A, WindowPass pass, hipStream_t s
 hipError_t launch_window_bf16(const WindowArgs &A, WindowPass pass, hipStream_t st);
 hipError_t launch_window_f16(const WindowArgs &A, WindowPass pass, hipStream_t st);
 
-// lines of a workgroup, for rows of up to `dim` values
-inline int window_rows(int type, int dim) { return type == SIG_F32 || dim > 128 ? kWindowWaves * 16 : kWindowWaves * 32; }
+// Whether float32 is multiplied as three parts (SplitTiles), with rows of up to 64 components or of 96 that are all there
+constexpr bool window_splits(int K, int V) { return (K > V ? K : V) <= 64 || (K == 96 && V == 96); }
+
+// lines of a workgroup
+inline int window_rows(int type, int K, int V) { return kWindowWaves * ((type == SIG_F32 ? !window_splits(K, V) : (K > V ? K : V) > 128) ? 16 : 32); }
 
 inline dim3 window_grid(int64_t blocks)
 {
@@ -769,23 +782,26 @@ inline dim3 window_grid(int64_t blocks)
 }
 
 template <typename T>
-hipError_t launch_window(const WindowArgs &A, WindowPass pass, hipStream_t st)
+hipError_t launch_window(const WindowArgs &A, WindowPass given, hipStream_t st)
 {
     const int dim = A.K > A.V ? A.K : A.V;
     const int64_t shared = A.B * (A.heads / A.group);
-    auto go = [&](auto x, auto d, auto whole) {
-        using X = typename decltype(x)::type;
-        constexpr int D = decltype(d)::value, BYTES = D * (int)sizeof(T), ROWS = kWindowWaves * X::M;
+    auto go = [&](auto d, auto whole, auto pass) {
+        constexpr int D = decltype(d)::value;
         constexpr bool WHOLE = decltype(whole)::value;
+        constexpr WindowPass PASS = decltype(pass)::value;
+        constexpr bool SPLIT = sizeof(T) == 4 && (WHOLE ? window_splits(D, D) : D <= 64);
+        using X = std::conditional_t<SPLIT, SplitTiles, std::conditional_t<(D > 128), SmallTiles<T>, Tiles<T>>>;
         // tokens of a tile
-        constexpr int N = BYTES > 512 ? 16 : sizeof(T) == 4 || BYTES > (WHOLE ? 256 : 128) ? 32 : 64, QUERY = BYTES > 512 ? 16 : BYTES > 128 ? 32 : 64, KEY = BYTES > 512 ? 16 : BYTES > 128 ? 32 : 64;
-        if (pass == WINDOW_FORWARD) {
+        constexpr int BYTES = D * (int)sizeof(T), ROWS = kWindowWaves * X::M;
+        constexpr int N = BYTES > 512 ? 16 : sizeof(T) == 4 || BYTES > (PASS == WINDOW_FORWARD && WHOLE ? 256 : 128) ? 32 : 64;
+        if constexpr (PASS == WINDOW_FORWARD) {
             sig_window_forward_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
-        } else if (pass == WINDOW_QUERY_GRADIENT) {
-            sig_window_query_gradient_kernel<T, X, D, QUERY, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
+        } else if constexpr (PASS == WINDOW_QUERY_GRADIENT) {
+            sig_window_query_gradient_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
         } else {
             const int64_t pieces = A.cut * A.parts + A.tiles - A.cut;
-            sig_window_key_gradient_kernel<T, X, D, KEY, WHOLE><<<window_grid(shared * pieces), kKeyThreads, 0, st>>>(A);
+            sig_window_key_gradient_kernel<T, X, D, N, WHOLE><<<window_grid(shared * pieces), kKeyThreads, 0, st>>>(A);
             if (A.parts > 1) {
                 int lanes = 64;
                 while (lanes < A.K + A.V && lanes < kWindowThreads) lanes *= 2;
@@ -794,15 +810,20 @@ hipError_t launch_window(const WindowArgs &A, WindowPass pass, hipStream_t st)
             }
         }
     };
-    auto with = [&](auto x, auto d) {
-        if (A.K == decltype(d)::value && A.V == A.K) go(x, d, std::true_type());
-        else go(x, d, std::false_type());
+    auto of = [&](auto d, auto whole) {
+        if (given == WINDOW_FORWARD) go(d, whole, std::integral_constant<WindowPass, WINDOW_FORWARD>());
+        else if (given == WINDOW_QUERY_GRADIENT) go(d, whole, std::integral_constant<WindowPass, WINDOW_QUERY_GRADIENT>());
+        else go(d, whole, std::integral_constant<WindowPass, WINDOW_KEY_GRADIENT>());
     };
-    if (dim <= 32) with(Tag<Tiles<T>>(), std::integral_constant<int, 32>());
-    else if (dim <= 64) with(Tag<Tiles<T>>(), std::integral_constant<int, 64>());
-    else if (dim <= 96) with(Tag<Tiles<T>>(), std::integral_constant<int, 96>());
-    else if (dim <= 128) with(Tag<Tiles<T>>(), std::integral_constant<int, 128>());
-    else with(Tag<SmallTiles<T>>(), std::integral_constant<int, 256>());
+    auto with = [&](auto d) {
+        if (A.K == decltype(d)::value && A.V == A.K) of(d, std::true_type());
+        else of(d, std::false_type());
+    };
+    if (dim <= 32) with(std::integral_constant<int, 32>());
+    else if (dim <= 64) with(std::integral_constant<int, 64>());
+    else if (dim <= 96) with(std::integral_constant<int, 96>());
+    else if (dim <= 128) with(std::integral_constant<int, 128>());
+    else with(std::integral_constant<int, 256>());
     return hipGetLastError();
 }
 

@@ -51,7 +51,7 @@ WindowArgs arguments(const sig_window_t &s, const void *q, const void *k, const 
     // (a scale of 0 is taken as the smallest one, so that the scores of what is hidden stay minus infinity)
     A.power = fmaxf((float)(fabs((double)s.scale) * kLog2E), FLT_MIN);
     A.negated = s.scale < 0.0f;
-    const int rows = window_rows(s.type, A.K > A.V ? A.K : A.V);
+    const int rows = window_rows(s.type, A.K, A.V);
     A.tiles = (A.T + rows - 1) / rows;
     return A;
 }
@@ -97,7 +97,7 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
     A.grad_v = grad_v;
     // The first tokens' tiles are cut where they have more than twice the queries of the others, unless they are so many that they balance by themselves and the parts'
     // sums would take much memory; else all tiles, where they are fewer than two a unit, into as many parts as give four, of 128 queries or more
-    const int rows = window_rows(shape->type, A.K > A.V ? A.K : A.V);
+    const int rows = window_rows(shape->type, A.K, A.V);
     const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T, lines = A.B * shape->shared_heads, all = lines * A.tiles;
     A.parts = 1;
     if (A.sinks > 0 && A.T > usual) {

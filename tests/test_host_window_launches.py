@@ -50,8 +50,8 @@ def test_what_no_launch_can_hold_is_refused(launches):
 
 
 def test_every_query_and_key_has_a_workgroup(launches):
-    """Queries: 128 of 16 bits a workgroup, 64 of more than 128 components or float32.  Keys: as many, cut along the queries or not."""
-    for (B, T, H, G, K, V, kind), rows in (((3, 1000, 4, 2, 64, 64, BF16), 128), ((3, 1000, 4, 2, 64, 64, F32), 64), ((2, 129, 3, 3, 200, 16, F16), 64), ((700, 65, 2, 1, 30, 40, F16), 128)):
+    """Queries: 128 a workgroup, 64 of more than 128 components, and of float32 from 65 on but for 96.  Keys: as many, cut along the queries or not."""
+    for (B, T, H, G, K, V, kind), rows in (((3, 1000, 4, 2, 64, 64, BF16), 128), ((3, 1000, 4, 2, 64, 64, F32), 128), ((3, 1000, 4, 2, 96, 96, F32), 128), ((3, 1000, 4, 2, 96, 90, F32), 64), ((3, 1000, 4, 2, 128, 128, F32), 64), ((2, 129, 3, 3, 200, 16, F16), 64), ((700, 65, 2, 1, 30, 40, F16), 128)):
         ((rc, _, (forward,)), (rc2, _, backward)) = launches([("forward", B, T, H, G, K, V, kind, 10, 0), ("backward", B, T, H, G, K, V, kind, 10, 0)])
         tiles = -(-T // rows)
         assert rc == rc2 == OK and forward.workgroups == backward[0].workgroups == B * H * tiles
