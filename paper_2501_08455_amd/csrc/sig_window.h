@@ -178,6 +178,7 @@ __device__ inline void zero_rows(T *first, int64_t stride, int dim, int from, in
 template <typename E>
 constexpr int kLift = std::is_same_v<E, f16> ? 7 : 0;
 constexpr float kBehind = 8.0f;
+constexpr int kFewTokens = 16;
 
 // Gradient terms in float16 have no scale that suits all of them: each lane (a line of the result) has a power of two of its own, `factor`, which
 // keeps its largest term so far within 2^15 and above 2^-7 of that when it is chosen.  Returns what the sums so far are to be multiplied with.
@@ -402,10 +403,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         delta = over_column<M>(delta, [](float a, float b) { return a + b; });
     }
     float2 stats = make_float2(0.0f, 0.0f);
-    if (there) {
-        stats = A.stats[place];
-        if (lane < M) A.delta[place] = delta;
-    }
+    if (there) stats = A.stats[place];
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
     TileMover<T, X, D, N, kWindowThreads, WHOLE, (X::PLANES > 1 && !WHOLE)> key_tile, value_tile;
@@ -420,11 +418,10 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
         if ((X::PLANES > 1 || !seen.all(lo, hi - 1, at, at + N - 1)) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = j + 1;
     };
-    typename X::Result acc[OUT] = {};
-    TermScale scale;
-    typename X::Frag terms[N / X::STEP];
-    auto weigh = [&](int at, const E *keys, const E *values, auto careful) {
-        typename X::Result s[KEYS] = {}, u[KEYS] = {};
+    auto none = [&](int at) { return own >= hi || seen.none(own, min(own + M, hi) - 1, at, at + N - 1); };
+    // p (g . v - D) of a tile
+    auto find_terms = [&](int at, const E *keys, const E *values, typename X::Result *u, auto careful) {
+        typename X::Result s[KEYS] = {};
         product_of_rows<X, D, KEYS, WHOLE>(lane, keys, q, s, A.K);
         if constexpr (decltype(careful)::value) settle_infinities<X, D, KEYS>(lane, keys, q, s);
         product_of_rows<X, D, KEYS, WHOLE>(lane, values, g, u, A.V);
@@ -438,6 +435,40 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
 #pragma unroll
                 for (int i = 0; i < X::REGS; ++i) u[t][i] = seen(line, at + t * M + X::row_of(lane, i)) ? u[t][i] : 0.0f;
         }
+    };
+    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
+    // Where no query sees more than a few tokens, D is also off by what the rounded probabilities made of the output, by as much as its own rounding would be.
+    // The terms' sum, which should be 0, is that error, so it is found first (window 3 of 24 components, bfloat16: gradients of queries and keys 1.50 of their
+    // rounding off without it, 1.42 with it; it costs two of the three products once more, where there are few of them: 16 x 2,048 tokens, 16 heads of 64, both
+    // passes 543 us with a window of 8, 493 without this with one of 17)
+    if (sizeof(T) == 2 && min((int64_t)hi, (int64_t)A.window + A.sinks) <= kFewTokens) {
+        float off = 0.0f;
+#pragma unroll 1
+        for (int j = 0; j < tiles.count; ++j) {
+            if (!WHOLE) asm volatile("" : "+s"(A.K), "+s"(A.V));      // (else what depends on them is kept over the loop, in more registers than there are)
+            __syncthreads();
+            load(j);
+            store(j);
+            __syncthreads();
+            if (none(tiles.at(j))) continue;
+            typename X::Result u[KEYS] = {};
+            find_terms(tiles.at(j), keys + (j & 1) * SIZE, values + (j & 1) * SIZE, u, std::false_type());
+#pragma unroll
+            for (int t = 0; t < KEYS; ++t)
+#pragma unroll
+                for (int i = 0; i < X::REGS; ++i) off += u[t][i];
+        }
+        delta += over_column<M>(off, [](float a, float b) { return a + b; });
+        __syncthreads();
+        if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
+    }
+    if (there && lane < M) A.delta[place] = delta;
+    typename X::Result acc[OUT] = {};
+    TermScale scale;
+    typename X::Frag terms[N / X::STEP];
+    auto weigh = [&](int at, const E *keys, const E *values, auto careful) {
+        typename X::Result u[KEYS] = {};
+        find_terms(at, keys, values, u, careful);
         if constexpr (std::is_same_v<E, f16>) {
             float shrink;
             if (scale.grown<M, KEYS>(u, &shrink)) {
@@ -454,9 +485,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
     };
-    auto none = [&](int at) { return own >= hi || seen.none(own, min(own + M, hi) - 1, at, at + N - 1); };
     bool left_out = false;
-    if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
     load(0);
     __syncthreads();
     store(0);
