@@ -150,30 +150,32 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     const int window = (int)(A.window == 0 || A.window > INT32_MAX ? INT32_MAX : A.window), sinks = (int)(A.sinks > INT32_MAX ? INT32_MAX : A.sinks);
     // (all of it compared, here and below: branches for single values cost more than the comparisons)
     auto seen = [&](int place) { return (place <= own) & ((own - place < window) | (place < sinks)); };
+    // The queries, in parts.  A short call is one chain of loads that wait for one another (lengths, table, keys): the queries' go out between the table's and the keys', and
+    // are used when those are on their way, but for rows that are not whole, which would ask for more registers than there are (128 sequences of up to 255 places, 4 heads of 64 float32: 16.4 -> 15.2 us, 48 ragged ones in 8 bits with a window 143 -> 136)
+    constexpr int QUERY_COUNT = 16 / (int)sizeof(T), QUERY_LOADS = GROUP / QUERY_COUNT;
+    // (where the keys' loads have the components of this step)
+    auto query_at = [&](int step, int i) { return step / OPERANDS * 4 * LOAD + lane / 16 * LOAD + step % OPERANDS * GROUP + i * QUERY_COUNT; };
     typename X::Frag q[QUERY_PARTS][STEPS];
-    {
-        const T *line = (const T *)A.q + p.b * A.qs[0] + (there ? token : 0) * A.qs[1] + (p.shared * A.group + (there ? number % A.group : 0)) * A.qs[2];
+    auto take_query = [&](int step, int i, Row row) {
+        const auto got = __builtin_bit_cast(__attribute__((ext_vector_type(QUERY_COUNT))) T, row_values<T, WHOLE>(row, query_at(step, i), K));
 #pragma unroll
-        for (int step = 0; step < STEPS; ++step) {
-            // (where the keys' loads have the components of this step)
-            const int at = step / OPERANDS * 4 * LOAD + lane / 16 * LOAD + step % OPERANDS * GROUP;
-            constexpr int COUNT = 16 / (int)sizeof(T);
+        for (int e = 0; e < QUERY_COUNT; ++e) {
+            float x = there ? to_float(got[e]) : 0.0f;
+            if (A.negated) x = -x;
 #pragma unroll
-            for (int first = 0; first < GROUP; first += COUNT) {
-                const auto got = __builtin_bit_cast(__attribute__((ext_vector_type(COUNT))) T, row_values<T, false>(row_load<T, false>(line, at + first, K), at + first, K));
-#pragma unroll
-                for (int e = 0; e < COUNT; ++e) {
-                    float x = there ? to_float(got[e]) : 0.0f;
-                    if (A.negated) x = -x;
-#pragma unroll
-                    for (int part = 0; part < QUERY_PARTS; ++part) {
-                        q[part][step][first + e] = (E)x;
-                        x -= (float)q[part][step][first + e];
-                        if (x != x) x = 0.0f;      // (infinity less infinity)
-                    }
-                }
+            for (int part = 0; part < QUERY_PARTS; ++part) {
+                q[part][step][i * QUERY_COUNT + e] = (E)x;
+                x -= (float)q[part][step][i * QUERY_COUNT + e];
+                if (x != x) x = 0.0f;      // (infinity less infinity)
             }
         }
+    };
+    const T *query_line = (const T *)A.q + p.b * A.qs[0] + (there ? token : 0) * A.qs[1] + (p.shared * A.group + (there ? number % A.group : 0)) * A.qs[2];
+    if constexpr (!WHOLE) {
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+            for (int i = 0; i < QUERY_LOADS; ++i) take_query(step, i, row_load<T, false>(query_line, query_at(step, i), K));
     }
 
     // blocks of places that some query of the tile sees
@@ -241,10 +243,23 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     int j = first_block + wave;
     if (j < last_block) {
         look_up(j);
+        Row rows[STEPS][QUERY_LOADS];
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+                for (int i = 0; i < QUERY_LOADS; ++i) rows[step][i] = row_load<T, true>(query_line, query_at(step, i), K);
+        }
         find(j);
         load_keys();
         load_values();
         if (j + kCacheWaves < last_block) look_up(j + kCacheWaves);
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int step = 0; step < STEPS; ++step)
+#pragma unroll
+                for (int i = 0; i < QUERY_LOADS; ++i) take_query(step, i, rows[step][i]);
+        }
     }
     // Something that is not finite and not seen by all queries: such blocks are left out, and taken by themselves afterwards (CAREFUL; a branch in
     // the middle would cost every block its registers)
@@ -464,8 +479,9 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
 template <typename T, int N>
 __global__ __launch_bounds__(kCacheThreads) void sig_cache_join_kernel(CacheAttentionArgs A, int columns, int turns, int slices)
 {
-    __shared__ float shares[kMostSplits], numbers[kCacheThreads];
+    __shared__ float shares[kMostSplits], numbers[kCacheThreads / 64];
     __shared__ Pack<float, N> joined[kCacheThreads];
+    constexpr int AHEAD = 8, OWN = kMostSplits / kCacheThreads;      // loads on their way; parts whose numbers a thread holds, at most
     const int team = columns * turns, of_team = threadIdx.x % team, first = threadIdx.x - of_team, V = A.cache.V, apart = kQueries * (V + 2);
     const int64_t queries = A.T * A.group, all = A.B * A.cache.heads * queries;
     const int64_t piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kCacheThreads / team) + threadIdx.x / team, id = piece / slices;
@@ -475,39 +491,57 @@ __global__ __launch_bounds__(kCacheThreads) void sig_cache_join_kernel(CacheAtte
     float *own_shares = shares + threadIdx.x / team * A.splits;
     // f over what the team's threads hold
     auto over_team = [&](float x, auto f) {
-        numbers[threadIdx.x] = x;
-        for (int i = team / 2; i > 0; i /= 2) {
-            __syncthreads();
-            if (of_team < i) numbers[threadIdx.x] = f(numbers[threadIdx.x], numbers[threadIdx.x + i]);
-        }
+        for (int i = 1; i < team && i < 64; i *= 2) x = f(x, __shfl_xor(x, i));
+        if (team <= 64) return x;
         __syncthreads();
-        x = numbers[first];
+        if (threadIdx.x % 64 == 0) numbers[threadIdx.x / 64] = x;
         __syncthreads();
+        x = numbers[first / 64];
+        for (int i = 1; i < team / 64; ++i) x = f(x, numbers[first / 64 + i]);
         return x;
     };
+    // all loads at once: the parts' maxima and sums, and the first of their columns
+    float tops[OWN], sums[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int s = of_team + i * team;
+        tops[i] = s < A.splits ? parts[(int64_t)s * apart + V] : -INFINITY;
+        sums[i] = s < A.splits ? parts[(int64_t)s * apart + V + 1] : 0.0f;
+    }
+    const int turn = of_team / columns;
+    const int c = ((int)(piece % slices) * columns + of_team % columns) * N;      // (V <= slices columns N)
+    Pack<float, N> ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        const int s = turn + i * turns;
+        if (c < V && s < A.splits) ahead[i] = load_pack<float, N>(parts + (int64_t)s * apart + c);
+    }
     float top = -INFINITY, total = 0.0f, any = 0.0f;
-    for (int s = of_team; s < A.splits; s += team) top = fmaxf(top, parts[(int64_t)s * apart + V]);
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) top = fmaxf(top, tops[i]);
     top = over_team(top, fmaxf);
     const float base = top == -INFINITY ? 0.0f : top;
-    for (int s = of_team; s < A.splits; s += team) {
-        const float sum = parts[(int64_t)s * apart + V + 1], share = __builtin_amdgcn_exp2f(parts[(int64_t)s * apart + V] - base);
-        if (sum != 0.0f) any = 1.0f;
-        total = fmaf(sum, share, total);
-        own_shares[s] = sum != 0.0f ? share : -1.0f;      // (a part that has seen nothing is left out)
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const float share = __builtin_amdgcn_exp2f(tops[i] - base);
+        if (sums[i] != 0.0f) any = 1.0f;
+        total = fmaf(sums[i], share, total);
+        if (of_team + i * team < A.splits) own_shares[of_team + i * team] = sums[i] != 0.0f ? share : -1.0f;      // (a part that has seen nothing is left out)
     }
     total = over_team(total, [](float a, float b) { return a + b; });
     any = over_team(any, fmaxf);
-    const int turn = of_team / columns;
-    const int c = ((int)(piece % slices) * columns + of_team % columns) * N;      // (V <= slices columns N)
+    __syncthreads();
     float value[N] = {};
-    if (c < V) {
-#pragma unroll 8
-        for (int s = turn; s < A.splits; s += turns) {
-            const Pack<float, N> part = load_pack<float, N>(parts + (int64_t)s * apart + c);
-            const float share = own_shares[s];
+    auto add = [&](const Pack<float, N> &part, float share) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) value[j] = share < 0.0f ? value[j] : fmaf(part.v[j], share, value[j]);
-        }
+        for (int j = 0; j < N; ++j) value[j] = share < 0.0f ? value[j] : fmaf(part.v[j], share, value[j]);
+    };
+    if (c < V) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (turn + i * turns < A.splits) add(ahead[i], own_shares[turn + i * turns]);
+#pragma unroll 8
+        for (int s = turn + AHEAD * turns; s < A.splits; s += turns) add(load_pack<float, N>(parts + (int64_t)s * apart + c), own_shares[s]);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) joined[threadIdx.x].v[j] = value[j];
