@@ -132,7 +132,8 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
  * with v; sums are float32's.  What a token does not see may be anything, NaN and infinities too; what is not finite spoils the tokens that see it.
  * Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); a scale that is not finite is SIG_ERR_INVALID; 2^31 - 1024 tokens or more, 2^31 heads
  * (B * heads) or more, 2^39 tokens of heads, or 2^30 groups of 16 tokens in the heads that
- * share one, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  No context scratch.
+ * share one, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  Context scratch where queries are few and see many keys, and are cut along them: value_dim + 2 floats for
+ * each query and piece, of at most two workgroups' pieces (64 or 128 queries) for each compute unit.
  */
 typedef struct sig_window_t {
     int64_t B, T;
@@ -152,8 +153,8 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  *   grad_out     DEVICE, [B][T][heads][value_dim] of `type`, contiguous; what stands behind the lengths is not read
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
- * Context scratch of B * heads * T floats; and where sequences are much longer than the window, for the sinks' gradients in up to 64 parts (16 of 64 or 128 keys for each
- * compute unit at most), or where keys are few, for all of them (some four for each unit): key_dim + value_dim floats for each key and part.
+ * Context scratch of B * heads * T floats; beside them the larger of key_dim floats for each query and piece (see above), and, where sequences are much longer than the window, for the sinks' gradients in up to 64 parts (16 of 64 or 128 keys for each
+ * compute unit at most), or where keys are few, for all of them (some two for each unit): key_dim + value_dim floats for each key and part.
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
                                   const void *out, const float *stats, const void *rest, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
@@ -166,8 +167,8 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
  *                value 448): a value stands for itself times its page's and head's scale.  NULL for the other types
  *   table        DEVICE, int32 [sequences][table_pages], rows table_stride apart
  * Places behind the table's end, and places whose page is not one of 0 ... pages - 1, do not exist: nothing is written there and nothing seen.  So
- * pages that a window has left may go to other sequences.  Calls that only read may share pages; a page that two sequences of one call write to
- * holds what either wrote, slot by slot (in 8 bits: with either's scale).
+ * pages that a window has left may go to other sequences.  Calls that only read may share pages; a page that one call writes to twice, because
+ * two sequences or two entries of a table name it, holds what either wrote, slot by slot (in 8 bits: with either's scale).
  */
 typedef struct sig_cache_t {
     int64_t pages, page_tokens;

@@ -59,6 +59,10 @@ struct WindowArgs {
     // [B][shared heads][cut][parts][rows of a tile][K + V].  Either all tiles, evenly, where there are few, or those of the first tokens, which every query sees
     float *sums;
     int cut, parts, joined, even;
+    // Queries that are few are cut along their keys: `splits` pieces of each tile's keys, [B][heads][splits][T] lines of what each adds up to: V values of the output, not yet
+    // divided, with the maximum and the sum that belong to them, or K of the queries' gradient
+    float *pieces;
+    int splits;
     int64_t B;
     int T, heads, group, K, V;
     int window, sinks;                    // at most T
@@ -71,6 +75,7 @@ struct WindowArgs {
 struct WindowPlace {
     int64_t b;
     int head, tile, n;      // n: tokens of the sequence
+    int split;              // which piece of the keys
 };
 
 // Workgroups that follow one another take the last tiles first, which have the most to do where everything is seen.
@@ -78,17 +83,19 @@ struct WindowPlace {
 __device__ inline bool window_place(const WindowArgs &A, int heads, WindowPlace &p)
 {
     const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, lines = A.B * heads;
-    if (id >= lines * A.tiles) return false;
-    int64_t line, tile;
+    const int64_t pieces = (int64_t)A.tiles * A.splits;
+    if (id >= lines * pieces) return false;
+    int64_t line, piece;
     if (lines % 8 == 0) {
         const int64_t turn = id / 8;
-        tile = turn % A.tiles;
-        line = turn / A.tiles * 8 + id % 8;
+        piece = turn % pieces;
+        line = turn / pieces * 8 + id % 8;
     } else {
-        tile = id / lines;
+        piece = id / lines;
         line = id % lines;
     }
-    p.tile = A.tiles - 1 - (int)tile;
+    p.tile = A.tiles - 1 - (int)(piece / A.splits);
+    p.split = (int)(piece % A.splits);
     p.b = line / heads;
     p.head = (int)(line % heads);
     const int64_t n = A.lengths ? A.lengths[p.b] : A.T;
@@ -108,6 +115,8 @@ struct KeyTiles {
         count = front + (hi + N - 1) / N - first;
     }
     __device__ int at(int j) const { return (j < front ? j : first + j - front) * N; }
+    // the first tile of piece number i
+    __device__ int piece(int i, int splits) const { return (int)((int64_t)count * i / splits); }
 };
 
 struct Seen {
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
     T *out = (T *)A.out + ((p.b * A.T) * A.heads + p.head) * A.V;
     const int64_t out_stride = (int64_t)A.heads * A.V;
     if (lo >= p.n) {
-        zero_rows(out, out_stride, A.V, lo, end);
+        if (p.split == 0) zero_rows(out, out_stride, A.V, lo, end);
         return;
     }
     const int hi = min(end, p.n), shared = p.head / A.group;
@@ -235,6 +244,7 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
     fragments_of<X, STEPS>(q, lane, (const T *)A.q + p.b * A.qs[0] + (there ? line : lo) * A.qs[1] + p.head * A.qs[2], A.K, there, A.negated);
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
+    const int begin = tiles.piece(p.split, A.splits), until = tiles.piece(p.split + 1, A.splits);
     TileMover<T, X, D, N, kWindowThreads, WHOLE> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
@@ -301,23 +311,23 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
     // taken by themselves afterwards (a branch in the middle would cost every tile its registers)
     bool left_out = false;
     if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    load(0);
+    if (begin < until) load(begin);
     __syncthreads();
-    store(0);
-    if (tiles.count > 1) load(1);
-    for (int j = 0; j < tiles.count; ++j) {
+    if (begin < until) store(begin);
+    if (begin + 1 < until) load(begin + 1);
+    for (int j = begin; j < until; ++j) {
         const int at = tiles.at(j), half = (j & 1) * SIZE;
         __syncthreads();
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
         if (!skip) weigh(at, keys + half, std::false_type());
-        if (j + 1 < tiles.count) store(j + 1);
-        if (j + 2 < tiles.count) load(j + 2);
+        if (j + 1 < until) store(j + 1);
+        if (j + 2 < until) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, values + half, probabilities, acc, A.V);
     }
     if (left_out) {
 #pragma unroll 1
-        for (int j = 0; j < tiles.count; ++j) {
+        for (int j = begin; j < until; ++j) {
             const int at = tiles.at(j);
             E *tile = values + (j & 1) * SIZE;
             __syncthreads();
@@ -333,6 +343,18 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
         }
     }
     sum = over_column<M>(sum, [](float a, float b) { return a + b; });
+    if (A.splits > 1) {
+        if (there) {
+            float *piece = A.pieces + (((p.b * A.heads + p.head) * A.splits + p.split) * A.T + line) * (A.V + 2);
+            store_line<X, D>(piece, A.V, lane, acc, 1.0f);
+            if (lane < M) {
+                piece[A.V] = m;
+                piece[A.V + 1] = sum;
+            }
+        }
+        if (hi < end && p.split == 0) zero_rows(out, out_stride, A.V, hi, end);
+        return;
+    }
     const float r = 1.0f / sum;
     if (there) {
         store_line<X, D>(out + line * out_stride, A.V, lane, acc, r);
@@ -359,7 +381,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
     T *out = (T *)A.grad_q + ((p.b * A.T) * A.heads + p.head) * A.K;
     const int64_t out_stride = (int64_t)A.heads * A.K;
     if (lo >= p.n) {
-        zero_rows(out, out_stride, A.K, lo, end);
+        if (p.split == 0) zero_rows(out, out_stride, A.K, lo, end);
         return;
     }
     const int hi = min(end, p.n), shared = p.head / A.group;
@@ -406,6 +428,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
     if (there) stats = A.stats[place];
     const Seen seen = {A.window, A.sinks};
     const KeyTiles<N> tiles(A, lo, hi);
+    const int begin = tiles.piece(p.split, A.splits), until = tiles.piece(p.split + 1, A.splits);
     TileMover<T, X, D, N, kWindowThreads, WHOLE, (X::PLANES > 1 && !WHOLE)> key_tile, value_tile;
     auto load = [&](int j) {
         const int at = tiles.at(j);
@@ -462,7 +485,7 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         __syncthreads();
         if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
     }
-    if (there && lane < M) A.delta[place] = delta;
+    if (there && lane < M && p.split == 0) A.delta[place] = delta;
     typename X::Result acc[OUT] = {};
     TermScale scale;
     typename X::Frag terms[N / X::STEP];
@@ -486,23 +509,23 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
         for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
     };
     bool left_out = false;
-    load(0);
+    if (begin < until) load(begin);
     __syncthreads();
-    store(0);
-    if (tiles.count > 1) load(1);
-    for (int j = 0; j < tiles.count; ++j) {
+    if (begin < until) store(begin);
+    if (begin + 1 < until) load(begin + 1);
+    for (int j = begin; j < until; ++j) {
         const int at = tiles.at(j), half = (j & 1) * SIZE;
         __syncthreads();
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
         if (!skip) weigh(at, keys + half, values + half, std::false_type());
-        if (j + 1 < tiles.count) store(j + 1);
-        if (j + 2 < tiles.count) load(j + 2);
+        if (j + 1 < until) store(j + 1);
+        if (j + 2 < until) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, keys + half, terms, acc, A.K);
     }
     if (left_out) {
 #pragma unroll 1
-        for (int j = 0; j < tiles.count; ++j) {
+        for (int j = begin; j < until; ++j) {
             const int at = tiles.at(j);
             E *tile = keys + (j & 1) * SIZE;
             __syncthreads();
@@ -517,8 +540,77 @@ __global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE
             add_not_finite<X, D, N, kWindowThreads, true>(lane, tile, k + at * A.ks[1], A.ks[1], A.K, p.n - at, skip, acc, [&](int r) { return seen(line, at + r); });
         }
     }
-    if (there) store_line<X, D>(out + line * out_stride, A.K, lane, acc, A.scale * scale.back());
-    if (hi < end) zero_rows(out, out_stride, A.K, hi, end);
+    if (there && A.splits > 1) store_line<X, D>(A.pieces + (((p.b * A.heads + p.head) * A.splits + p.split) * A.T + line) * A.K, A.K, lane, acc, A.scale * scale.back());
+    else if (there) store_line<X, D>(out + line * out_stride, A.K, lane, acc, A.scale * scale.back());
+    if (hi < end && p.split == 0) zero_rows(out, out_stride, A.K, hi, end);
+}
+
+// ---------------------------------------------------------------- pieces of the keys
+// The pieces of queries that were cut along their keys, in their order: outputs with the statistics and the rest, or (GRADIENT) the queries' gradients.  `lanes` threads (a power of
+// two) take a token of a head, four columns each.  What a workgroup more of queries would cost in waiting, a launch and these sums cost less of: the rule is in sig_window.hip.
+template <typename T, bool GRADIENT>
+__global__ __launch_bounds__(kWindowThreads) void sig_window_join_pieces_kernel(WindowArgs A, int lanes)
+{
+    const int64_t id = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kWindowThreads / lanes) + threadIdx.x / lanes, line = id / A.T;
+    const int token = (int)(id % A.T), dim = GRADIENT ? A.K : A.V, width = GRADIENT ? A.K : A.V + 2, c = threadIdx.x % lanes * 4;
+    if (line >= A.B * A.heads) return;
+    const int64_t b = line / A.heads, n = A.lengths ? A.lengths[b] : A.T, apart = (int64_t)A.T * width;
+    if (token >= n || c >= dim) return;      // (behind the sequence there are zeros by now)
+    const float *pieces = A.pieces + (line * A.splits * A.T + token) * width;
+    float top = -INFINITY, total = 0.0f, x[4] = {};
+    if (!GRADIENT)
+        for (int i = 0; i < A.splits; ++i) top = fmaxf(top, pieces[i * apart + A.V]);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+    for (int i = 0; i < A.splits; ++i) {
+        const float *piece = pieces + i * apart;
+        float share = 1.0f;
+        if (!GRADIENT) {
+            share = __builtin_amdgcn_exp2f(piece[A.V] - base);
+            total = fmaf(piece[A.V + 1], share, total);
+        }
+        if (c + 4 <= dim) {
+            const Pack<float, 4> four = load_pack<float, 4>(piece + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(four.v[j], share, x[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < dim) x[j] = fmaf(piece[c + j], share, x[j]);
+        }
+    }
+    const float r = GRADIENT ? 1.0f : 1.0f / total;
+    const int64_t row = ((b * A.T + token) * A.heads + line % A.heads) * dim + c;
+    T *to = (T *)(GRADIENT ? A.grad_q : A.out) + row;
+    Pack<T, 4> four;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[j] *= r;
+        four.v[j] = from_float<T>(x[j]);
+    }
+    const bool whole = c + 4 <= dim;
+    if (whole) {
+        store_pack(to, four);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < dim) to[j] = four.v[j];
+    }
+    if constexpr (!GRADIENT) {
+        if (sizeof(T) == 2 && A.rest) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] -= to_float(four.v[j]);
+            const unsigned rest = rest_of(x[2], x[3], rest_of(x[0], x[1], 0, false), true);
+            if (whole) {
+                store_pack(A.rest + row, __builtin_bit_cast(Pack<Rest, 4>, rest));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < dim) A.rest[row + j] = (Rest)(rest >> (8 * j));
+            }
+        }
+        if (A.stats && c == 0) A.stats[line * A.T + token] = make_float2(base - kLift<T>, r);
+    }
 }
 
 // ---------------------------------------------------------------- gradient of keys and values
@@ -824,10 +916,17 @@ hipError_t launch_window(const WindowArgs &A, WindowPass given, hipStream_t st)
         // tokens of a tile
         constexpr int BYTES = D * (int)sizeof(T), ROWS = kWindowWaves * X::M;
         constexpr int N = BYTES > 512 ? 16 : sizeof(T) == 4 || BYTES > (PASS == WINDOW_FORWARD && WHOLE ? 256 : 128) ? 32 : 64;
-        if constexpr (PASS == WINDOW_FORWARD) {
-            sig_window_forward_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
-        } else if constexpr (PASS == WINDOW_QUERY_GRADIENT) {
-            sig_window_query_gradient_kernel<T, X, D, N, WHOLE><<<window_grid(A.B * A.heads * A.tiles), kWindowThreads, 0, st>>>(A);
+        if constexpr (PASS != WINDOW_KEY_GRADIENT) {
+            constexpr bool GRADIENT = PASS == WINDOW_QUERY_GRADIENT;
+            const dim3 grid = window_grid(A.B * A.heads * A.tiles * A.splits);
+            if constexpr (GRADIENT) sig_window_query_gradient_kernel<T, X, D, N, WHOLE><<<grid, kWindowThreads, 0, st>>>(A);
+            else sig_window_forward_kernel<T, X, D, N, WHOLE><<<grid, kWindowThreads, 0, st>>>(A);
+            if (A.splits > 1) {
+                int lanes = 1;
+                while (lanes * 4 < (GRADIENT ? A.K : A.V)) lanes *= 2;
+                const int at_once = kWindowThreads / lanes;
+                sig_window_join_pieces_kernel<T, GRADIENT><<<window_grid((A.B * A.heads * A.T + at_once - 1) / at_once), kWindowThreads, 0, st>>>(A, lanes);
+            }
         } else {
             const int64_t pieces = A.cut * A.parts + A.tiles - A.cut;
             sig_window_key_gradient_kernel<T, X, D, N, WHOLE><<<window_grid(shared * pieces), kKeyThreads, 0, st>>>(A);

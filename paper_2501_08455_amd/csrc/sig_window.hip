@@ -53,7 +53,20 @@ WindowArgs arguments(const sig_window_t &s, const void *q, const void *k, const 
     A.negated = s.scale < 0.0f;
     const int rows = window_rows(s.type, A.K, A.V);
     A.tiles = (A.T + rows - 1) / rows;
+    A.splits = 1;
     return A;
+}
+
+// Queries that are fewer than two workgroups a unit are cut along their keys into as many pieces as give two, of 512 keys or more, or of 256 where half of the units would have
+// nothing to do.  Forward, forward and gradient, us, without and with: 1 x 1,024 tokens, 1 head of 128 bfloat16 32, 102 and 18, 75; 1 x 2,048, 8 heads (2 shared) of 128 58, 207 and 37, 140;
+// 1 x 16,384, 1 head of 128 410, 1,226 and 132, 538; 1 x 1,200, 2 heads of 64 float32 81, 200 and 31, 95; 1 x 2,937, 2 heads of 256 float32 522, 1,400 and 136, 542.  (8 x 512, 8 heads
+// of 128 bfloat16, 256 workgroups, in pieces of 256: 142 and 155 with the gradient)
+int splits_of(const sig_ctx *ctx, const WindowArgs &A, int rows)
+{
+    const int64_t blocks = A.B * A.heads * A.tiles, keys = A.window < A.T ? least(A.T, (int64_t)A.window + rows + A.sinks) : A.T;
+    if (blocks >= 2 * ctx->num_cu) return 1;
+    const int64_t splits = least((2 * ctx->num_cu + blocks - 1) / blocks, keys / (blocks < ctx->num_cu ? 256 : 512));
+    return splits < 1 ? 1 : (int)splits;
 }
 
 hipError_t launch(const WindowArgs &A, int type, WindowPass pass, hipStream_t st)
@@ -76,6 +89,12 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
     A.out = out;
     A.stats = (float2 *)stats;
     A.rest = stats ? (Rest *)rest : nullptr;
+    A.splits = splits_of(ctx, A, window_rows(shape->type, A.K, A.V));
+    Scratch scratch;
+    if (A.splits > 1) {
+        const int got = scratch.get(ctx, (size_t)(A.B * A.heads * A.splits * A.T * (A.V + 2)) * sizeof(float), (hipStream_t)hip_stream, &A.pieces);
+        if (got != SIG_OK) return got;
+    }
     return launch(A, shape->type, WINDOW_FORWARD, (hipStream_t)hip_stream) == hipSuccess ? SIG_OK : SIG_ERR_HIP;
 }
 
@@ -96,7 +115,8 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
     A.grad_k = grad_k;
     A.grad_v = grad_v;
     // The first tokens' tiles are cut where they have more than twice the queries of the others, unless they are so many that they balance by themselves and the parts'
-    // sums would take much memory; else all tiles, where they are fewer than two a unit, into as many parts as give four, of 128 queries or more
+    // sums would take much memory; else all tiles, where they are fewer than two a unit, into as many parts as give two, of 128 queries or more
+    // (four: 2 x 1,024 tokens, 32 heads (8 shared) of 64 bfloat16 149 instead of 136 us, 1 x 8,192, 8 heads (2 shared) of 128, window 1,024, 301 instead of 287)
     const int rows = window_rows(shape->type, A.K, A.V);
     const int64_t usual = 2 * ((int64_t)A.window + rows), deltas = A.B * A.heads * A.T, lines = A.B * shape->shared_heads, all = lines * A.tiles;
     A.parts = 1;
@@ -109,7 +129,7 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
             A.joined = A.sinks;
         }
     } else if (all < 2 * ctx->num_cu) {
-        A.parts = (int)least((4 * ctx->num_cu + all - 1) / all, least(kMostParts, (least(A.T, (int64_t)A.window + rows) * A.group + 127) / 128));
+        A.parts = (int)least((2 * ctx->num_cu + all - 1) / all, least(kMostParts, (least(A.T, (int64_t)A.window + rows) * A.group + 127) / 128));
         if (A.parts > 1) {
             A.cut = A.tiles;
             A.joined = A.T;
@@ -117,10 +137,12 @@ int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const
         }
     }
     const int64_t joined = A.cut * A.parts * (int64_t)rows * (A.K + A.V) * lines;
+    A.splits = splits_of(ctx, A, rows);
+    const int64_t pieces = A.splits > 1 ? A.B * A.heads * A.splits * A.T * A.K : 0;
     Scratch scratch;
-    rc = scratch.get(ctx, (size_t)(deltas + joined) * sizeof(float), st, &A.delta);
+    rc = scratch.get(ctx, (size_t)(deltas + (joined > pieces ? joined : pieces)) * sizeof(float), st, &A.delta);
     if (rc != SIG_OK) return rc;
-    A.sums = A.delta + deltas;
+    A.sums = A.pieces = A.delta + deltas;      // (the pieces are joined before the keys' sums begin)
     hipError_t e = launch(A, shape->type, WINDOW_QUERY_GRADIENT, st);
     if (e == hipSuccess) e = launch(A, shape->type, WINDOW_KEY_GRADIENT, st);
     return e == hipSuccess ? SIG_OK : SIG_ERR_HIP;

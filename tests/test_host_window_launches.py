@@ -59,7 +59,7 @@ def test_every_query_and_key_has_a_workgroup(launches):
 
 
 # B, T, heads, shared, window, sinks (64 components, bfloat16: 128 keys a workgroup): tiles that are cut, and parts.  256 compute units
-CUT = [((4, 2048, 16, 4, 0, 0), (16, 4)),        # fewer than two a unit: four
+CUT = [((4, 2048, 16, 4, 0, 0), (16, 2)),        # fewer than two a unit: two
        ((64, 2048, 16, 4, 0, 0), (0, 1)), ((8, 4096, 16, 16, 1024, 0), (0, 1)),
        ((8, 4096, 16, 16, 1024, 4), (1, 3)),     # the first tokens', whose queries are more than 2 (1,024 + 128)
        ((8, 4096, 16, 16, 1024, 129), (2, 3)), ((8, 2000, 16, 16, 1024, 4), (0, 1)), ((1, 65536, 16, 4, 1024, 4), (1, 30)), ((1, 1 << 20, 16, 4, 1024, 4), (1, 64)),
@@ -89,6 +89,22 @@ def test_places_are_cut_by_their_rule(launches):
             tiles = -(-T * (H // G) // 16)
             assert rc == OK and launched[0].workgroups == B * G * tiles * splits and len(launched) == (2 if splits > 1 else 1)
             assert most == (4 * B * G * tiles * splits * 16 * 66 if splits > 1 else 0)
+
+
+# B, T, heads, components, type, window, sinks: pieces of the keys (two workgroups a unit, pieces of 512 keys or more, or of 256 where workgroups are fewer than units)
+PIECES = [((1, 4096, 1, 64, BF16, 0, 0), 16), ((1, 4096, 8, 64, BF16, 0, 0), 2), ((1, 65536, 1, 64, F32, 0, 0), 1), ((1, 32768, 1, 64, F16, 0, 0), 2), ((1, 4096, 1, 64, BF16, 300, 0), 1),
+          ((1, 4096, 1, 64, BF16, 1000, 0), 4), ((1, 4096, 1, 64, BF16, 300, 2000), 9), ((1, 511, 1, 64, BF16, 0, 0), 1), ((1, 512, 1, 64, BF16, 0, 0), 2), ((16, 4096, 16, 64, BF16, 0, 0), 1),
+          ((8, 512, 8, 64, BF16, 0, 0), 1), ((1, 8192, 3, 64, BF16, 0, 0), 3), ((1, 16384, 2, 256, F32, 0, 0), 1), ((1, 8192, 2, 200, F32, 0, 0), 2), ((1, 12000, 1, 16, BF16, 0, 0), 6)]
+
+
+def test_queries_are_cut_along_their_keys_by_their_rule(launches):
+    got = launches([(way, B, T, H, H, K, K, kind, window, sinks) for (B, T, H, K, kind, window, sinks), _ in PIECES for way in ("forward", "backward")])
+    for i, ((B, T, H, K, kind, *_), splits) in enumerate(PIECES):
+        (rc, most, forward), (rc2, _, backward) = got[2 * i:2 * i + 2]
+        tiles = -(-T // (64 if K > 128 else 128))
+        assert rc == rc2 == OK and forward[0].workgroups == backward[0].workgroups == B * H * tiles * splits, PIECES[i]
+        assert len(forward) == (2 if splits > 1 else 1) and most == (4 * B * H * T * splits * (K + 2) if splits > 1 else 0)
+        assert ("join_pieces" in backward[1].kernel) == (splits > 1)
 
 
 def test_instances_by_size_and_type(launches):
