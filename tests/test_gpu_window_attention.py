@@ -67,7 +67,8 @@ SHAPES = [   # B, T, heads, shared, K, V, window, sinks
     (2, 257, 4, 4, 33, 130, 100, 70), (1, 200, 8, 1, 256, 256, None, 0), (1, 500, 2, 2, 64, 64, 1, 0), (2, 160, 3, 3, 96, 24, 31, 33), (1, 1000, 1, 1, 128, 128, 128, 128),
     (2, 70, 6, 2, 192, 16, 1000, 0), (1, 129, 1, 1, 65, 129, 128, 1), (5, 64, 2, 2, 8, 8, 63, 1), (1, 700, 8, 2, 64, 64, 129, 5), (8, 40, 3, 1, 7, 11, 3, 39),
     (2, 400, 2, 2, 80, 80, 200, 300), (9, 31, 8, 8, 32, 32, 2, 1),
-    (1, 900, 8, 2, 24, 32, None, 0), (2, 1500, 2, 1, 90, 96, 70, 150), (1, 2000, 4, 4, 64, 64, 40, 1)]
+    (1, 900, 8, 2, 24, 32, None, 0), (2, 1500, 2, 1, 90, 96, 70, 150), (1, 2000, 4, 4, 64, 64, 40, 1),
+    (2, 300, 2, 1, 192, 192, 70, 3), (1, 400, 2, 2, 150, 131, None, 0)]
 
 
 @gpu

@@ -108,8 +108,8 @@ def test_queries_are_cut_along_their_keys_by_their_rule(launches):
 
 
 def test_instances_by_size_and_type(launches):
-    """Rows of 32, 64, 96, 128 and 256 components; whole where keys and values have just that."""
-    for dims, size, whole in (((32, 32), 32, 1), ((16, 32), 32, 0), ((33, 64), 64, 0), ((64, 64), 64, 1), ((96, 96), 96, 1), ((97, 5), 128, 0), ((128, 128), 128, 1), ((130, 256), 256, 0)):
+    """Rows of 32, 64, 96, 128, 192 and 256 components; whole where keys and values have just that."""
+    for dims, size, whole in (((32, 32), 32, 1), ((16, 32), 32, 0), ((33, 64), 64, 0), ((64, 64), 64, 1), ((96, 96), 96, 1), ((97, 5), 128, 0), ((128, 128), 128, 1), ((7, 150), 192, 0), ((192, 192), 192, 1), ((130, 256), 256, 0)):
         for kind in (F32, BF16, F16):
             ((rc, _, (forward,)),) = launches([("forward", 1, 10, 1, 1, *dims, kind, 0, 0)])
             found = re.search(r"Li(\d+)ELi(\d+)ELb([01])E", forward.kernel)
