@@ -121,6 +121,13 @@ __device__ inline typename X::Frag operand(Row got)
     }
 }
 
+constexpr int cache_block(int bytes, int least)
+{
+    int block = 64;
+    while (block > least && block * bytes > 8192) block /= 2;
+    return block;
+}
+
 // T: of q and out; C: of the cache in memory (Narrow: 8 bits); X: of the products; PARTS: of X's type that hold one of q's or a probability; WHOLE: keys
 // and values have D components
 template <typename T, typename C, typename X, int D, int QUERY_PARTS, int PARTS, bool WHOLE>
@@ -131,7 +138,7 @@ __global__ __launch_bounds__(kCacheThreads, D * sizeof(typename X::E) <= 256 ? 2
     constexpr bool NARROW = std::is_same_v<C, Narrow>;
     constexpr int M = X::M, STEPS = D / X::STEP, OUT = D / M, GROUP = X::GROUP;
     // places of a block: 8 KB of keys as the products want them (so 64 registers of loads on their way), and as many of values
-    constexpr int BYTES = D * (int)sizeof(E), BLOCK = 8192 / BYTES < X::STEP ? X::STEP : 8192 / BYTES > 64 ? 64 : 8192 / BYTES, KEYS = BLOCK / M, PRODUCTS = BLOCK / X::STEP;
+    constexpr int BLOCK = cache_block(D * (int)sizeof(E), X::STEP), KEYS = BLOCK / M, PRODUCTS = BLOCK / X::STEP;
     constexpr int LOAD = 16 / (int)sizeof(C), OPERANDS = LOAD / GROUP, KEY_LOADS = STEPS / OPERANDS;      // values of a load, operands that they make
     constexpr int ROW_LOADS = D / LOAD, VALUE_LOADS = BLOCK * ROW_LOADS / 64;
     static_assert(M == kQueries && X::REGS == 4 && BLOCK * ROW_LOADS % 64 == 0 && STEPS % OPERANDS == 0);
@@ -585,6 +592,7 @@ hipError_t launch_cache_attention(const CacheAttentionArgs &A, bool narrow, hipS
     const int dim = A.cache.K > A.cache.V ? A.cache.K : A.cache.V;
     if (dim <= 64) go(std::integral_constant<int, 64>());
     else if (dim <= 128) go(std::integral_constant<int, 128>());
+    else if (dim <= 192) go(std::integral_constant<int, 192>());
     else go(std::integral_constant<int, 256>());
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !A.parts) return e;
