@@ -583,14 +583,20 @@ hipError_t launch_cache_attention(const CacheAttentionArgs &A, bool narrow, hipS
         auto launch = [&](auto whole) {
             constexpr bool WHOLE = decltype(whole)::value, WIDE = sizeof(T) == 4;
             // values of 8 bits are bfloat16's, and a query is one, two or three of them
-            if (narrow) sig_cache_attention_kernel<T, Narrow, SmallTiles<bf16>, D, WIDE ? 3 : std::is_same_v<T, f16> ? 2 : 1, WIDE ? 3 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
-            else sig_cache_attention_kernel<T, T, SmallTiles<T>, D, 1, WIDE ? 1 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
+            if constexpr (D % 64 == 0) {
+                if (narrow) sig_cache_attention_kernel<T, Narrow, SmallTiles<bf16>, D, WIDE ? 3 : std::is_same_v<T, f16> ? 2 : 1, WIDE ? 3 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
+            }
+            if (!narrow) sig_cache_attention_kernel<T, T, SmallTiles<T>, D, 1, WIDE ? 1 : 2, WHOLE><<<grid, kCacheThreads, 0, st>>>(A);
         };
         if (A.cache.K == D && A.cache.V == D) launch(std::true_type());
         else launch(std::false_type());
     };
     const int dim = A.cache.K > A.cache.V ? A.cache.K : A.cache.V;
-    if (dim <= 64) go(std::integral_constant<int, 64>());
+    // (rows of up to 32, and of 65 to 96 and 129 to 192 components in instances of their own: 128 x 8,000 places, 4 heads of 32 float32 338 -> 190 us, 32 x 8,192, 8 heads of 80 bfloat16
+    // 160 -> 136, 16 ragged sequences of 2,000, 8 heads of 96 float32 72 -> 33, 32 x 8,192, 8 heads of 192 bfloat16 406 -> 280.  A load of 8-bit keys is two operands, which 32 and 96 are no whole number of)
+    if (dim <= 32 && !narrow) go(std::integral_constant<int, 32>());
+    else if (dim <= 64) go(std::integral_constant<int, 64>());
+    else if (dim <= 96 && !narrow) go(std::integral_constant<int, 96>());
     else if (dim <= 128) go(std::integral_constant<int, 128>());
     else if (dim <= 192) go(std::integral_constant<int, 192>());
     else go(std::integral_constant<int, 256>());

@@ -242,7 +242,9 @@ def assert_near(got, want):
 ATTENTIONS = [   # B, T, H, G, K, V, page, places, window, sinks
     (1, 1, 1, 1, 1, 1, 1, 1, None, 0), (3, 1, 4, 2, 64, 64, 16, 100, None, 0), (2, 1, 8, 1, 128, 128, 64, 700, None, 0), (2, 5, 4, 2, 40, 72, 16, 90, 17, 3),
     (1, 1, 2, 2, 128, 128, 16, 5000, 1000, 4), (2, 3, 3, 3, 33, 130, 7, 60, None, 0), (1, 20, 4, 1, 256, 256, 100, 300, 50, 70), (4, 1, 40, 2, 64, 32, 8, 33, 5, 1),
-    (1, 70, 2, 1, 96, 96, 32, 200, 33, 2), (2, 2, 2, 1, 16, 24, 256, 600, 1, 0), (1, 1, 1, 1, 80, 192, 3, 2000, None, 0)]
+    (1, 70, 2, 1, 96, 96, 32, 200, 33, 2), (2, 2, 2, 1, 16, 24, 256, 600, 1, 0), (1, 1, 1, 1, 80, 192, 3, 2000, None, 0),
+    (2, 1, 4, 4, 32, 32, 16, 900, None, 0), (1, 2, 6, 2, 192, 192, 32, 400, 130, 5), (1, 40, 2, 1, 24, 32, 16, 700, None, 0), (3, 1, 4, 4, 80, 80, 16, 333, None, 0),
+    (1, 1, 4, 1, 96, 96, 64, 3000, None, 0)]
 
 
 @gpu
