@@ -220,7 +220,7 @@ struct TermScale {
 
 // ---------------------------------------------------------------- forward
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::E) <= 384 ? 2 : 1) void sig_window_forward_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::E) <= 512 ? 2 : 1) void sig_window_forward_kernel(WindowArgs A)
 {
     using E = typename X::E;
     constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * X::template Tile<D>::PITCH;
@@ -367,8 +367,13 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
 }
 
 // ---------------------------------------------------------------- gradient of the queries, and D
+// Two workgroups a unit, where their registers fit (one, with the forward pass alike: 4 x 2,048 tokens, 16 heads (4 shared) of 256 bfloat16 495 instead of 310 us, with the gradient 1,621
+// instead of 1,245; of 80 823 instead of 699; 199 x 6 tokens, 44 heads (11 shared) of 256 x 130 305 instead of 155)
+template <typename X, int D, bool WHOLE>
+constexpr bool kQueryPairs = X::PLANES > 1 ? D <= 64 : sizeof(typename X::E) == 2 && (WHOLE || X::M == 16 || D <= 96);
+
 template <typename T, typename X, int D, int N, bool WHOLE>
-__global__ __launch_bounds__(kWindowThreads, D * sizeof(typename X::E) <= (WHOLE && X::PLANES == 1 ? 256 : 128) ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
+__global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1) void sig_window_query_gradient_kernel(WindowArgs A)
 {
     using E = typename X::E;
     constexpr int M = X::M, ROWS = kWindowWaves * M, KEYS = N / M, STEPS = D / X::STEP, OUT = D / M, SIZE = N * X::template Tile<D>::PITCH;
