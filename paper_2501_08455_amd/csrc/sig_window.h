@@ -551,8 +551,8 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
 }
 
 // ---------------------------------------------------------------- pieces of the keys
-// The pieces of queries that were cut along their keys, in their order: outputs with the statistics and the rest, or (GRADIENT) the queries' gradients.  `lanes` threads (a power of
-// two) take a token of a head, four columns each.  What a workgroup more of queries would cost in waiting, a launch and these sums cost less of: the rule is in sig_window.hip.
+// Joins the pieces of queries that were cut along their keys (by the rule in sig_window.hip), in their order: outputs with the statistics and the rest, each piece's sums scaled
+// to the largest maximum, or (GRADIENT) the queries' gradients.  Bound by memory: each piece is read once.  `lanes` threads (a power of two) take a token of a head, four columns each.
 template <typename T, bool GRADIENT>
 __global__ __launch_bounds__(kWindowThreads) void sig_window_join_pieces_kernel(WindowArgs A, int lanes)
 {
