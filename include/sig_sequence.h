@@ -220,7 +220,7 @@ int sig_cache_append(sig_ctx *ctx, const sig_cache_t *cache, const sig_append_t 
  *   counts       DEVICE, int64 [B], queries of each sequence (taken into 0 ... T); NULL: T.  Those behind them are not read and give zeros
  *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous.  A query that sees nothing gives zeros
  * The cache's type is `type`, or SIG_E4M3.  For their product with the values probabilities of 16-bit calls keep 16 digits, over float16 pages 22 (those below e^-12 of the
- * largest: steps of 2^-39 of it); of float32 calls 24.  Sums are float32's.
+ * largest: steps of 2^-39 of it, 2^-24 where scores reach 2^20); of float32 calls 24.  Sums are float32's.
  * Limits of sig_window_attention, and 2^31 - 1024 places at most; more than 2^31 groups of 16 queries are SIG_ERR_TOO_LARGE.  Context scratch where sequences are
  * cut along their places because there are few: (value_dim + 2) floats for each query and part, of at most two workgroups' parts for each compute unit.
  */

@@ -21,11 +21,10 @@ constexpr int kCacheThreads = 256, kCacheWaves = kCacheThreads / 64;
 constexpr int kQueries = 16;      // of a workgroup
 constexpr int kMostSplits = 1024;      // (a workgroup's queries times their parts are at most that)
 
-// What float16 holds is small: probabilities, which are at most 1 here, are lifted by 2^15, and their sum with them.  Down to e^-12 of the largest they then keep the 22 digits
+// Float16's probabilities, which are at most 1 here, are lifted by 2^15, and their sum with them (lifted_base).  Down to e^-12 of the largest they then keep the 22 digits
 // of their two parts, and below steps of 2^-39 of the largest, instead of 2^-24 (one score 12, 15 and 18 above 1,999 others, whose values are all that counts: the output
 // is off by 2.1e-4, its own rounding, instead of 1.1e-3, 2.2e-2 and 0.5; 48 sequences of up to 4,000 places, 16 queries, 32 heads (8 shared) of 128: 252 us both ways).
-template <typename E>
-constexpr float kCacheLift = std::is_same_v<E, f16> ? 15.0f : 0.0f;
+constexpr int kCacheLift = 15;
 
 // 0 ... 2^31 - 1 over a divisor, as a product
 struct Quotient {
@@ -365,16 +364,15 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
             for (int i = 0; i < X::REGS; ++i) most = fmaxf(most, s[t][i]);
         any |= all & there;
         most = over_column<M>(most, fmaxf);
-        const float next = fmaxf(m, most * A.power), base = next == -INFINITY ? 0.0f : next;
-        const float shrink = __builtin_amdgcn_exp2f(m - base);
+        const float next = fmaxf(m, most * A.power), base = next == -INFINITY ? 0.0f : lifted_base<E, kCacheLift>(next);
+        const float shrink = __builtin_amdgcn_exp2f(lifted_base<E, kCacheLift>(m) - base);
         m = next;
-        const float lifted = base - kCacheLift<E>;
         float total = 0.0f;
 #pragma unroll
         for (int t = 0; t < KEYS; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) {
-                s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -lifted));
+                s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], A.power, -base));
                 total += s[t][i];
                 // (the values' scale goes into the probabilities: one number for a place instead of one for each of its values)
                 if constexpr (NARROW) {
@@ -456,6 +454,7 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
     // nothing 0
     sum = over_column<M>(sum, [](float a, float b) { return a + b; });
     any = over_column<M>(any ? 1.0f : 0.0f, fmaxf) > 0.0f;
+    m = lifted_base<E, kCacheLift>(m);
     if (!there) m = -INFINITY, sum = 0.0f;
     if (m == -INFINITY && sum == sum) sum = any ? 1.0f : 0.0f;
     float *own_sums = (float *)room[wave];

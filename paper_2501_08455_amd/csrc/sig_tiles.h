@@ -519,6 +519,14 @@ __device__ inline bool any_infinite(const SplitTiles::Frag *f)
     return __any(bad);
 }
 
+// The base that probabilities are worked out over, 2^(z - base), for a largest score m: float16's are lifted by 2^LIFT, since what that type holds is small.  (Beyond 2^20 m has no
+// digits left for that: a score less its rounded maximum is anything up to 2^-24 of it.)
+template <typename E, int LIFT>
+__device__ inline float lifted_base(float m)
+{
+    return std::is_same_v<E, f16> && fabsf(m) < 0x1p20f ? m - LIFT : m;
+}
+
 // over the lanes that hold one column of a result tile
 template <int M, typename F>
 __device__ inline float over_column(float x, F f)

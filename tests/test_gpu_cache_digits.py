@@ -40,3 +40,27 @@ def test_one_place_above_all_others(G, places, spread, gap, kind, cache):
     floor = 2.0 ** -25 * math.sqrt(G * V) if kind == torch.float16 else 0.0
     lost = 2.0 ** -39 * math.exp(gap) if cache == torch.float16 else 0.0
     assert err <= ((1 + 2.0 ** -7) * UNIT[kind] + 64 * 2.0 ** -24 + lost) * size + floor, (err / size, floor / size)
+
+
+@gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("power", [7, 17, 23, 26])
+def test_scores_up_to_many_millions(power, kind):
+    """The last place's score is the largest by 2^(power - 7): its value is the output.  Scores of 2^power and more are exact, but not over their maximum times log2 e, which
+    is rounded by up to 2^(power - 23)."""
+    n, K, V = 100, 16, 24
+    k = torch.full((n, 1, 1, K), 2.0) * 64 + torch.arange(n).view(n, 1, 1, 1)
+    q = torch.full((n, 1, 1, K), 2.0 ** (power - 11))
+    v = noise(n, 1, 1, V, seed=1)
+    table = torch.arange(n).int().expand(n, n).cuda()
+    got = binding.cache_attention(q.to(kind).cuda(), k.to(kind).cuda(), v.to(kind).cuda(), table, torch.arange(1, n + 1).cuda(), scale=1.0)
+    want = v.to(kind).double()[:, 0, 0]
+    err = (got.cpu().double()[:, 0, 0] - want).norm()
+    # (at 2^7 the place before is e^-1 of the last: that case is the definition's)
+    if power == 7:
+        p = torch.softmax((torch.arange(n) * 1.0).expand(n, n).masked_fill(torch.arange(n) > torch.arange(n)[:, None], -math.inf).double(), -1)
+        want, size = p @ v.to(kind).double()[:, 0, 0], p @ v.to(kind).double().abs()[:, 0, 0]
+        err = (got.cpu().double()[:, 0, 0] - want).norm()
+    else:
+        size = want
+    assert err <= ((1 + 2.0 ** -7) * UNIT[kind] + 64 * 2.0 ** -24) * size.norm(), float(err / size.norm())
