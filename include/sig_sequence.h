@@ -124,8 +124,8 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
  *   lengths      DEVICE, int64 [B], tokens of each sequence (taken into 0 ... T); NULL: T.  The tokens behind them are not read and
  *                give zeros
  *   out          DEVICE, [B][T][heads][value_dim] of `type`, contiguous
- *   stats        DEVICE, float32 [B][heads][T][2], what sig_window_attention_backward needs (the largest z, as a power of two, and one over the
- *                sum of exp(z - largest)); may be NULL.  Nothing is written for the tokens behind the lengths
+ *   stats        DEVICE, float32 [B][heads][T][2], what sig_window_attention_backward needs (a base at or near the largest z, as a power of
+ *                two, and one over the sum of exp(z - base)); may be NULL.  Nothing is written for the tokens behind the lengths
  *   rest         DEVICE, a byte for each value of out, which the backward pass needs too: what out's rounding to 16 bits left (8 bits, 5 of exponent,
  *                times 2^14).  Not used, and may be NULL, with float32 and where stats is NULL
  * 16-bit operands are multiplied as they are, and the probabilities (before they are divided by their sum) rounded to that type for their product
