@@ -184,6 +184,7 @@ typedef struct sig_cache_t {
 /*
  * Keys and values of new tokens into a cache: token t of sequence b, which holds lengths[b], goes to place lengths[b] + t.  Keys are turned on the way
  * as sig_rotary does it, and so are the tokens' queries, into an array of their own.
+ * The cache's keys, values and scales lie apart from one another and from all that is read.
  *   k, v         DEVICE, [B][T][cache heads][key_dim or value_dim] of `type`; strides as everywhere
  *   q, q_out     DEVICE, [B][T][heads][key_dim] of `type`, q_out contiguous and apart from q; both NULL where heads == 0
  *   lengths      DEVICE, int64 [B] (negative ones are taken as 0)

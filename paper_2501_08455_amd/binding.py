@@ -436,8 +436,8 @@ def cache_append(k, v, keys, values, table, lengths, counts=None, q=None, positi
     lengths[b] goes to place p = lengths[b] + t, which is slot p % P of page table[b, p // P].
 
     `keys` [pages, G, P, K] and `values` [pages, G, P, V] have the type of k and v, or are float8_e4m3fn with `key_scales` and `value_scales` (float32
-    [pages, G]): then a page's scale is the smallest power of two that fits what the page holds of a head, and grows with it.  `table` is int32
-    [B, n]; places without a page (behind the table, or whose entry is not a page's number) are not written.  `counts` [B]: new tokens of each
+    [pages, G]): then a page's scale is the smallest power of two that fits what the page holds of a head, and grows with it.  What is written lies apart
+    from all else (keys and values may be views of one buffer that take turns in it).  `table` is int32 [B, n]; places without a page (behind the table, or whose entry is not a page's number) are not written.  `counts` [B]: new tokens of each
     sequence (None: T); those behind them are not read.  With `frequencies` keys are turned by rotary positions on the way (see rotary):
     the places, or `positions`.  `q` [B, T, H, K], the tokens' queries: returns them turned, as a new tensor (zeros behind the counts); else returns None."""
     return (_torch_lib or torch_lib()).cache_append(k, v, keys, values, table, lengths, counts, q, positions, frequencies, interleaved, scale,

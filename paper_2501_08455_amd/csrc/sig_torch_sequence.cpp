@@ -502,6 +502,95 @@ struct DifferentiableWindowAttention : torch::autograd::Function<DifferentiableW
 };
 
 // ---------------------------------------------------------------- paged cache
+// Where an array's bytes lie: pieces of `width` bytes at first + sum x_i strides_i, 0 <= x_i < counts_i
+struct Pieces {
+    const char *first;
+    int64_t width, counts[3], strides[3];
+    int axes = 0;
+
+    explicit Pieces(const at::Tensor &t) : first((const char *)t.const_data_ptr()), width(t.element_size())
+    {
+        if (t.is_contiguous()) {
+            width *= t.numel();
+            return;
+        }
+        // (the last axis is contiguous)
+        width *= t.size(-1);
+        for (int64_t i = 0; i + 1 < t.dim(); ++i) {
+            if (t.size(i) == 1) continue;
+            counts[axes] = t.size(i);
+            strides[axes++] = t.stride(i) * t.element_size();
+        }
+    }
+};
+
+struct Sum {
+    struct Term {
+        int64_t stride, low, high;      // x stride, low <= x <= high
+    };
+    Term terms[6];
+    int count = 0;
+
+    void add(int64_t stride, int64_t low, int64_t high)
+    {
+        for (int i = 0; i < count; ++i) {
+            if (terms[i].stride != stride) continue;
+            terms[i].low += low;
+            terms[i].high += high;
+            return;
+        }
+        terms[count++] = {stride, low, high};
+        for (int i = count - 1; i > 0 && terms[i].stride > terms[i - 1].stride; --i) std::swap(terms[i], terms[i - 1]);
+    }
+
+    static int64_t floor_of(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+
+    // Whether some sum of the terms from number `from` on lies between low and high (exclusive), with `other` one whose x are not all 0.  Largest strides first, so that axes which hold
+    // one another leave an x or two each; arrays that take more than `steps` count as if it did.
+    bool reaches(int64_t low, int64_t high, bool other, int *steps, int from = 0) const
+    {
+        if (from == count) return low < 0 && high > 0 && !other;
+        if (--*steps < 0) return true;
+        const Term &t = terms[from];
+        int64_t least = 0, most = 0;      // of the terms behind
+        for (int i = from + 1; i < count; ++i) {
+            least += terms[i].low * terms[i].stride;
+            most += terms[i].high * terms[i].stride;
+        }
+        const int64_t first = std::max(t.low, floor_of(low - most, t.stride) + 1), last = std::min(t.high, -floor_of(least - high, t.stride) - 1);
+        for (int64_t x = first; x <= last; ++x)
+            if (reaches(low - x * t.stride, high - x * t.stride, other && x == 0, steps, from + 1)) return true;
+        return false;
+    }
+};
+
+constexpr int kMostSteps = 10000;
+
+// whether two of an array's pieces overlap
+bool overlaps_itself(const Pieces &a)
+{
+    Sum sum;
+    for (int i = 0; i < a.axes; ++i) {
+        if (a.strides[i] == 0) return true;
+        for (int j = 0; j < i; ++j)
+            if (a.strides[i] == a.strides[j]) return true;
+        sum.add(a.strides[i], 1 - a.counts[i], a.counts[i] - 1);
+    }
+    int steps = kMostSteps;
+    return sum.reaches(-a.width, a.width, true, &steps);
+}
+
+// whether a piece of one array overlaps one of the other (arrays that do not overlap themselves)
+bool overlap(const Pieces &a, const Pieces &b)
+{
+    Sum sum;
+    for (int i = 0; i < a.axes; ++i) sum.add(a.strides[i], 1 - a.counts[i], 0);
+    for (int i = 0; i < b.axes; ++i) sum.add(b.strides[i], 0, b.counts[i] - 1);
+    int steps = kMostSteps;
+    const int64_t apart = b.first - a.first;
+    return sum.reaches(-b.width - apart, a.width - apart, false, &steps);
+}
+
 struct Cache {
     at::Tensor table, key_scales, value_scales;
     sig_cache_t shape = {};
@@ -518,7 +607,7 @@ struct Cache {
             if (t.scalar_type() != keys.scalar_type()) refuse("keys and values must have the same type");
             if (!narrow && t.scalar_type() != x.scalar_type()) refuse(std::string(name) + " must have the type of the other operands, or float8_e4m3fn");
             if (t.size(3) > 1 && t.stride(3) != 1) refuse("the last axis of " + std::string(name) + " must be contiguous");
-            if (written && t.numel() > 0) at::assert_no_internal_overlap(t);
+            if (written && t.numel() > 0 && overlaps_itself(Pieces(t))) refuse(std::string("pages of ") + name + " overlap one another");
             for (int i = 0; i < 3; ++i)
                 if (t.size(i) != keys.size(i)) refuse("keys and values must have the same pages, heads and tokens");
         }
@@ -604,12 +693,26 @@ at::Tensor cache_append(const at::Tensor &k_, const at::Tensor &v_, const at::Te
     }
     shape.interleaved = interleaved;
     shape.scale = scale;
-    for (const at::Tensor &written : {keys, values, cache.key_scales, cache.value_scales})
-        for (const auto &[t, name] : {std::pair<const at::Tensor &, const char *>{k, "k"}, {v, "v"}, {q, "q"}}) {
-            if (!written.defined() || !t.defined() || written.numel() == 0 || t.numel() == 0) continue;
-            const auto x = span_of(t), y = span_of(written);
+    // What is written lies apart from all else: from what is read by its span, from what else is written (pages may hold keys, values and scales in turn) piece by piece
+    const std::pair<const at::Tensor &, const char *> written[] = {{keys, "keys"}, {values, "values"}, {cache.key_scales, "key_scales"}, {cache.value_scales, "value_scales"}};
+    const std::pair<const at::Tensor &, const char *> read[] = {{k, "k"}, {v, "v"}, {q, "q"}, {cache.table, "table"}, {lengths, "lengths"}, {counts, "counts"},
+                                                                {positions, "positions"}, {frequencies_, "frequencies"}};
+    for (int i = 0; i < 4; ++i) {
+        if (!written[i].first.defined() || written[i].first.numel() == 0) continue;
+        const auto x = span_of(written[i].first);
+        for (const auto &[t, name] : read) {
+            if (!t.defined() || t.numel() == 0) continue;
+            const auto y = span_of(t);
             if (x.first < y.second && y.first < x.second) refuse(std::string(name) + " must lie apart from the cache");
         }
+        for (int j = i + 1; j < 4; ++j) {
+            const auto &[t, name] = written[j];
+            if (!t.defined() || t.numel() == 0) continue;
+            const auto y = span_of(t);
+            if (x.first < y.second && y.first < x.second && overlap(Pieces(written[i].first), Pieces(t)))
+                refuse(std::string(written[i].second) + " and " + name + " must lie apart");
+        }
+    }
     std::optional<RotaryPlace> place;
     if (frequencies_.defined()) {
         // (places, where positions are not given, are not a tensor of the call)
