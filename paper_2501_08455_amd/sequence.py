@@ -154,8 +154,6 @@ class SequenceModel(torch.nn.Module):
         """Attention of one prefix, mixed [B, 1, 3 heads, head_dim]: [B, heads, head_dim]."""
         q, k, v = mixed.split(self.heads, 2)
         if self.mixer == "window":
-            if cache["room"] == 0:
-                raise ValueError("the cache has no room for another point")
             cache["room"] -= 1
             pages = [cache[name] for name in ("keys", "values", "table", "lengths")]
             scales = {name: cache[name] for name in ("key_scales", "value_scales")}
@@ -169,7 +167,9 @@ class SequenceModel(torch.nn.Module):
 
     @torch.no_grad()
     def step(self, x, cache):
-        """The next point, x [B, inputs]: the outputs [B, outputs] of the prefix that ends there.  Updates `cache` in place."""
+        """The next point, x [B, inputs]: the outputs [B, outputs] of the prefix that ends there.  Updates `cache` in place; a full one is refused as it is."""
+        if self.mixer == "window" and cache["room"] == 0:
+            raise ValueError("the cache has no room for another point")
         point = self._points(x)
         segment = binding.signature(torch.stack((cache["point"], point), 1), self.depth)
         if cache["row"] is None:
