@@ -213,8 +213,9 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
     const int first_block = (int)((int64_t)count * p.split / A.splits), last_block = (int)((int64_t)count * (p.split + 1) / A.splits);
     auto at_of = [&](int j) { return (j < front ? j : low + j - front) * BLOCK; };
 
-    // A block's loads: lane l % BLOCK looks up place l, a block ahead; keys go to where the product wants them, values row by row.  What has no page
-    // is read from one that exists, and hidden.
+    // A block's loads: lane l % BLOCK looks up place l, a block ahead; keys go to where the product wants them, values row by row.  In place of what does not
+    // exist the block's first place that does is read, and hidden (another sequence's page may hold anything: NaN there would have the block taken carefully, 128 sequences of up to
+    // 255 places, 4 heads of 64 float32 44 us instead of 15); a block without any reads what the first page holds, and is left out.
     int entry = -1;                          // of the table
     auto look_up = [&](int j) {
         const int page = A.quotient(at_of(j) + lane % BLOCK);
@@ -227,8 +228,10 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
     auto find = [&](int j) {
         const int place = at_of(j) + lane % BLOCK, slot = place - A.quotient(place) * A.cache.page_tokens;
         const bool exists = entry >= 0 && entry < A.cache.pages && place < p.n;
-        const int64_t page = exists ? entry : 0, in_page = exists ? slot : 0;
         existing = __ballot(exists);
+        const int stand_in = __builtin_ctzll(existing | (uint64_t)1 << 63), own_page = exists ? entry : 0, own_slot = exists ? slot : 0;
+        const int other_page = __builtin_amdgcn_readlane(own_page, stand_in), other_slot = __builtin_amdgcn_readlane(own_slot, stand_in);
+        const int64_t page = exists ? own_page : other_page, in_page = exists ? own_slot : other_slot;
         key_row = page * A.cache.keys.page + p.shared * A.cache.keys.head + in_page * A.cache.keys.slot;
         value_row = page * A.cache.values.page + p.shared * A.cache.values.head + in_page * A.cache.values.slot;
         if constexpr (NARROW) {
@@ -335,8 +338,8 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
             if (j + 2 * kCacheWaves < last_block) look_up(j + 2 * kCacheWaves);
         }
         const bool not_finite = !all && __any(spoilt);
-        if (not_finite != CAREFUL) {
-            left_out = true;
+        if (exist == 0 || not_finite != CAREFUL) {
+            left_out |= exist != 0;
             return;
         }
         if constexpr (NARROW) {
