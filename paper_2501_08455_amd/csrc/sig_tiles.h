@@ -185,10 +185,14 @@ struct SplitTiles : NarrowTiles<bf16> {
     template <int D>
     using Tile = LdsTile<bf16, PLANES * D>;
 
-    // FINITE: x is known not to be infinite (an infinity is its first part)
-    template <bool FINITE, int N, typename V>
-    static __device__ void split(const float *x, V *parts)
+    // FINITE: x is known not to be infinite (an infinity is its first part).  NANS: a NaN's first part is NaN, whatever its bits (else one that has none in its upper half reads as
+    // infinity there, and is NaN by its second part)
+    template <bool FINITE, bool NANS, int N, typename V>
+    static __device__ void split(const float *given, V *parts)
     {
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = NANS ? __builtin_canonicalizef(given[e]) : given[e];
         using b2 = __attribute__((ext_vector_type(2))) bf16;
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
@@ -235,7 +239,7 @@ struct SplitTiles : NarrowTiles<bf16> {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = tiles[step / 2][step % 2 * 8 + e];
         Frag f;
-        split<true, 8>(x, f.part);
+        split<true, false, 8>(x, f.part);
         return f;
     }
     static __device__ Result multiply(const Frag &left, const Frag &right, Result sum)
@@ -268,7 +272,7 @@ __device__ inline void set_fragment(SplitTiles::Frag &f, const V &values)
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = values[e];
-    SplitTiles::split<false, 8>(x, f.part);
+    SplitTiles::split<false, true, 8>(x, f.part);
 }
 
 // Rows of D values in LDS, PITCH apart: an odd number of 16 bytes, so that the 16 rows of a 16-byte read (rows) find all 64 banks, and
@@ -373,6 +377,8 @@ struct TileMover {
         }
         return any;
     }
+    // NANS: see SplitTiles
+    template <bool NANS = false>
     __device__ void store(E *tile, int dim, int n) const
     {
         using Tile = typename X::template Tile<D>;
@@ -387,7 +393,7 @@ struct TileMover {
                 using b4 = __attribute__((ext_vector_type(4))) bf16;
                 const float x[] = {bits[0], bits[1], bits[2], bits[3]};
                 b4 parts[X::PLANES];
-                X::template split<false, 4>(x, parts);
+                X::template split<false, NANS, 4>(x, parts);
 #pragma unroll
                 for (int p = 0; p < X::PLANES; ++p)
                     if (EVEN || here(i)) *(b4 *)(to + p * D) = parts[p];

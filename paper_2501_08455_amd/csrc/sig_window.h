@@ -253,9 +253,10 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
         value_tile.load(v + at * A.vs[1], A.vs[1], A.V, p.n - at);
     };
-    auto store = [&](int j) {
+    auto store = [&](int j, auto careful) {
+        constexpr bool NANS = decltype(careful)::value;
         const int at = tiles.at(j);
-        key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
+        key_tile.template store<NANS>(keys + (j & 1) * SIZE, A.K, p.n - at);
         value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
         // (float32's parts: infinities that all see as well, which are no products of theirs)
         if constexpr (X::PLANES > 1) {
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
     if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
     if (begin < until) load(begin);
     __syncthreads();
-    if (begin < until) store(begin);
+    if (begin < until) store(begin, std::false_type());
     if (begin + 1 < until) load(begin + 1);
     for (int j = begin; j < until; ++j) {
         const int at = tiles.at(j), half = (j & 1) * SIZE;
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
         if (!skip) weigh(at, keys + half, std::false_type());
-        if (j + 1 < until) store(j + 1);
+        if (j + 1 < until) store(j + 1, std::false_type());
         if (j + 2 < until) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, values + half, probabilities, acc, A.V);
     }
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
             E *tile = values + (j & 1) * SIZE;
             __syncthreads();
             load(j);
-            store(j);
+            store(j, std::true_type());
             __syncthreads();
             if (spoilt[j & 1] != j + 1) continue;
             const bool skip = none(at);
@@ -441,9 +442,10 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
         key_tile.load(k + at * A.ks[1], A.ks[1], A.K, p.n - at);
         value_tile.load(v + at * A.vs[1], A.vs[1], A.V, p.n - at);
     };
-    auto store = [&](int j) {
+    auto store = [&](int j, auto careful) {
+        constexpr bool NANS = decltype(careful)::value;
         const int at = tiles.at(j);
-        key_tile.store(keys + (j & 1) * SIZE, A.K, p.n - at);
+        key_tile.template store<NANS>(keys + (j & 1) * SIZE, A.K, p.n - at);
         value_tile.store(values + (j & 1) * SIZE, A.V, p.n - at);
         if ((X::PLANES > 1 || !seen.all(lo, hi - 1, at, at + N - 1)) && key_tile.spoilt(A.K, p.n - at)) spoilt[j & 1] = j + 1;
     };
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
             if (!WHOLE) asm volatile("" : "+s"(A.K), "+s"(A.V));      // (else what depends on them is kept over the loop, in more registers than there are)
             __syncthreads();
             load(j);
-            store(j);
+            store(j, std::false_type());
             __syncthreads();
             if (none(tiles.at(j))) continue;
             typename X::Result u[KEYS] = {};
@@ -517,7 +519,7 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
     bool left_out = false;
     if (begin < until) load(begin);
     __syncthreads();
-    if (begin < until) store(begin);
+    if (begin < until) store(begin, std::false_type());
     if (begin + 1 < until) load(begin + 1);
     for (int j = begin; j < until; ++j) {
         const int at = tiles.at(j), half = (j & 1) * SIZE;
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
         const bool bad = __builtin_amdgcn_readfirstlane(spoilt[j & 1]) == j + 1, skip = bad || none(at);
         left_out |= bad;
         if (!skip) weigh(at, keys + half, values + half, std::false_type());
-        if (j + 1 < until) store(j + 1);
+        if (j + 1 < until) store(j + 1, std::false_type());
         if (j + 2 < until) load(j + 2);
         if (!skip) product_along_rows<X, D, N / X::STEP, WHOLE>(lane, keys + half, terms, acc, A.K);
     }
@@ -536,7 +538,7 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
             E *tile = keys + (j & 1) * SIZE;
             __syncthreads();
             load(j);
-            store(j);
+            store(j, std::true_type());
             __syncthreads();
             if (spoilt[j & 1] != j + 1) continue;
             const bool skip = none(at);
@@ -712,8 +714,9 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
         }
     };
     // `room`: of three, j % 3
-    auto store = [&](const Place &w, int j, int room) {
-        query_tile.store(queries + room * SIZE, A.K, n - w.at);
+    auto store = [&](const Place &w, int j, int room, auto careful) {
+        constexpr bool NANS = decltype(careful)::value;
+        query_tile.template store<NANS>(queries + room * SIZE, A.K, n - w.at);
         upstream_tile.store(upstream + room * SIZE, A.V, n - w.at);
         if (threadIdx.x < N) {
             most[room * N + threadIdx.x] = stats_tile.x;
@@ -803,7 +806,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
     Place now = begin, before = now, ahead = now;
     if (count > 0) load(ahead);
     __syncthreads();
-    if (count > 0) store(ahead, 0, 0);
+    if (count > 0) store(ahead, 0, 0, std::false_type());
     next(ahead);
     if (count > 1) load(ahead);
     int room = 0, behind = 2;
@@ -820,7 +823,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
             weigh_keys(before.at, behind, ~j & 1);
             product_along_rows<X, D, N / X::STEP, WHOLE, 2>(lane, queries + behind * SIZE, weights, acc, A.K);
         }
-        if (j + 1 < count) store(ahead, j + 1, following);
+        if (j + 1 < count) store(ahead, j + 1, following, std::false_type());
         next(ahead);
         if (j + 2 < count) load(ahead);
         skipped = skip;
@@ -836,7 +839,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
             const int at = now.at, head = shared * A.group + now.head;
             __syncthreads();
             load(now);
-            store(now, j, 0);
+            store(now, j, 0, std::true_type());
             __syncthreads();
             if (!all_bad && spoilt[0] != j + 1) continue;
             const bool skip = none(at);
