@@ -133,7 +133,7 @@ int sig_linear_attention_backward(sig_ctx *ctx, const sig_attention_t *shape, co
  * Dimensions 1 ... 256 (larger ones are SIG_ERR_UNSUPPORTED); a scale that is not finite is SIG_ERR_INVALID; 2^31 - 1024 tokens or more, 2^31 heads
  * (B * heads) or more, 2^39 tokens of heads, or 2^30 groups of 16 tokens in the heads that
  * share one, SIG_ERR_TOO_LARGE.  B == 0 and T == 0 do nothing.  Context scratch where queries are few and see many keys, and are cut along them: value_dim + 2 floats for
- * each query and piece, of at most two workgroups' pieces (64 or 128 queries) for each compute unit.
+ * each query and piece, of fewer than four workgroups' pieces (64 or 128 queries each) for each compute unit.
  */
 typedef struct sig_window_t {
     int64_t B, T;
@@ -154,7 +154,7 @@ int sig_window_attention(sig_ctx *ctx, const sig_window_t *shape, const void *q,
  *   grad_q, grad_k, grad_v   DEVICE, shapes of q, k and v, contiguous, `type`; zeros behind the lengths; the gradient of a
  *                shared head is the sum over the heads that read it
  * Context scratch of B * heads * T floats; beside them the larger of key_dim floats for each query and piece (see above), and, where sequences are much longer than the window, for the sinks' gradients in up to 64 parts (16 of 64 or 128 keys for each
- * compute unit at most), or where keys are few, for all of them (some two for each unit): key_dim + value_dim floats for each key and part.
+ * compute unit at most), or where keys are few, for all of them (fewer than four for each unit): key_dim + value_dim floats for each key and part.
  */
 int sig_window_attention_backward(sig_ctx *ctx, const sig_window_t *shape, const void *q, const void *k, const void *v, const int64_t *lengths,
                                   const void *out, const float *stats, const void *rest, const void *grad_out, void *grad_q, void *grad_k, void *grad_v, void *hip_stream);
@@ -223,7 +223,7 @@ int sig_cache_append(sig_ctx *ctx, const sig_cache_t *cache, const sig_append_t 
  * The cache's type is `type`, or SIG_E4M3.  For their product with the values probabilities of 16-bit calls keep 16 digits, over float16 pages 22 (those below e^-12 of the
  * largest: steps of 2^-39 of it, 2^-24 where scores reach 2^20); of float32 calls 24.  Sums are float32's.
  * Limits of sig_window_attention, and 2^31 - 1024 places at most; more than 2^31 groups of 16 queries are SIG_ERR_TOO_LARGE.  Context scratch where sequences are
- * cut along their places because there are few: (value_dim + 2) floats for each query and part, of at most two workgroups' parts for each compute unit.
+ * cut along their places because there are few: (value_dim + 2) floats for each query and part, of fewer than four workgroups' parts (16 queries each) for each compute unit.
  */
 typedef struct sig_queries_t {
     int64_t B, T;

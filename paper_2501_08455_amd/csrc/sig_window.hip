@@ -20,7 +20,7 @@ int check(const sig_ctx *ctx, const sig_window_t *s)
         s->window < 0 || s->sinks < 0 || !valid_type(s->type) || !(fabsf(s->scale) <= FLT_MAX))
         return SIG_ERR_INVALID;
     if (s->key_dim > kMostDim || s->value_dim > kMostDim) return SIG_ERR_UNSUPPORTED;
-    // (a grid of 2^24 x 2^15 workgroups of 64 tokens or more)
+    // (2^33 workgroups of 64 tokens or more; a grid of them holds 2^23 - 1 by 2^16 - 1)
     if (s->T >= INT32_MAX - 1023 || s->B > INT32_MAX / s->heads || (s->T > 0 && s->B * s->heads > ((int64_t)1 << 39) / (s->T + 127))) return SIG_ERR_TOO_LARGE;
     // (tiles of 16 queries or more, of all heads that share a key, are counted in 32 bits)
     if ((s->T + 15) / 16 * (s->heads / s->shared_heads) >= INT32_MAX / 2) return SIG_ERR_TOO_LARGE;
