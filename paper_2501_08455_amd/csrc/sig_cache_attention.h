@@ -147,7 +147,8 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
     using Tile = LdsTile<E, D>;
     constexpr bool NARROW = std::is_same_v<C, Narrow>;
     constexpr int M = X::M, STEPS = D / X::STEP, OUT = D / M, GROUP = X::GROUP;
-    // places of a block: 8 KB of keys as the products want them (so 64 registers of loads on their way), and as many of values
+    // places of a block, 16 to 64: 8 KB of keys as the products want them, or the fewest that a product takes where those are more (so that 64 registers of loads are on their way, 128 at most),
+    // and as many of values
     constexpr int BLOCK = cache_block(D * (int)sizeof(E), X::STEP), KEYS = BLOCK / M, PRODUCTS = BLOCK / X::STEP;
     constexpr int LOAD = 16 / (int)sizeof(C), OPERANDS = LOAD / GROUP, KEY_LOADS = STEPS / OPERANDS;      // values of a load, operands that they make
     constexpr int ROW_LOADS = D / LOAD, VALUE_LOADS = BLOCK * ROW_LOADS / 64;
@@ -388,6 +389,7 @@ __global__ __launch_bounds__(kCacheThreads, (kCachePairs<T, C, D, WHOLE>) ? 2 : 
         for (int t = 0; t < OUT; ++t)
 #pragma unroll
             for (int i = 0; i < X::REGS; ++i) acc[t][i] *= shrink;
+        // (16 bits: two parts of 8 or 11 digits each, since here memory is what bounds and a product more costs nothing)
         typename X::Frag probabilities[PARTS][PRODUCTS];
 #pragma unroll
         for (int part = 0; part < PARTS; ++part)

@@ -305,6 +305,9 @@ __global__ __launch_bounds__(kWindowThreads, D * X::PLANES * sizeof(typename X::
                 part += s[t][i];
             }
         sum += part;
+        // 16 bits: rounded to the operands' type for their product, while the sum that divides them stays float32's.  Outputs then are 2.4e-3 off in bfloat16, of which their own rounding is
+        // 1.7e-3 (window 1,024 and 4,096).  A second part of each, as attention over a cache has it, leaves just that, but is a product more beside two: 65,536 tokens, 16 heads (4 shared) of
+        // 128, window 4,096 2,670 -> 3,520 us, 8 x 4,096, 16 heads, window 1,024 482 -> 598.
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) probabilities[step] = X::of_results(s, step);
     };
@@ -468,7 +471,8 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
         }
     };
     if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-    // Where no query sees more than a few tokens, D is also off by what the rounded probabilities made of the output, by as much as its own rounding would be.
+    // Where no query of the workgroup sees more than a few tokens, D is also off by what the rounded probabilities made of the output, by as much as its own rounding would be.  (The first
+    // few tokens of a longer sequence with a larger window see as few, but share their workgroup with others that see more, and go without.)
     // The terms' sum, which should be 0, is that error, so it is found first (window 3 of 24 components, bfloat16: gradients of queries and keys 1.50 of their
     // rounding off without it, 1.42 with it; it costs two of the three products once more, where there are few of them: 16 x 2,048 tokens, 16 heads of 64, both
     // passes 543 us with a window of 8, 493 without this with one of 17)
@@ -513,6 +517,7 @@ __global__ __launch_bounds__(kWindowThreads, (kQueryPairs<X, D, WHOLE>) ? 2 : 1)
 #pragma unroll
                 for (int i = 0; i < X::REGS; ++i) u[t][i] *= scale.factor;
         }
+        // (16 bits: rounded to the operands' type, as the forward pass's probabilities are, and for the same reason: a second part would be a product more beside three)
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) terms[step] = X::of_results(u, step);
     };
@@ -760,6 +765,7 @@ __global__ __launch_bounds__(kKeyThreads, 2) void sig_window_key_gradient_kernel
 #pragma unroll
                 for (int i = 0; i < X::REGS; ++i) s[t][i] *= LIFT;
         }
+        // (rounded for their product, as in the forward pass; the second wavefront has them in float32, and rounds its terms)
 #pragma unroll
         for (int step = 0; step < N / X::STEP; ++step) weights[step] = X::of_results(s, step);
     };
